@@ -63,6 +63,7 @@ typedef enum eta_status {
 #define ETA_DEV_TIMEOUT      1u  /* a bounded wait inside a kernel ran out; outputs are not valid */
 #define ETA_DEV_LEN_CLAMPED  2u  /* some seq_lens[i] exceeded t_cap and was clamped */
 #define ETA_DEV_EMPTY_ROW    4u  /* some seq_lens[i] <= 0: that sequence's output is zero */
+#define ETA_DEV_REFUSED     16u  /* eta_plan_pages could not serve some sequence (granted says which), or more pages came back than exist */
 
 /* flags of eta_params.flags */
 #define ETA_FLAG_DENSE           1u  /* baseline: admit every block and switch the gate off (softmax attention) */
@@ -309,6 +310,32 @@ int eta_decode_paged(const eta_cache_desc* desc, const eta_page_table* pages, co
                      const float* tau, const float* head_const,
                      float* out, uint8_t* sel_mask, int32_t* stats, uint32_t* status_dev,
                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Block tables and slot maps from request lengths (deployment plumbing for the paged cache of the calls above; the paper has no
+ * counterpart).  Device memory throughout, so that a serving loop can capture it with the step it prepares.  In order:
+ *   1. Sequences with release[i] != 0 (release nullable) are over: their ceil(seq_lens[i] / block_size) pages go on top of the free
+ *      stack (free_pages int32 [n_pages], of which the first *n_free are free), sequence after sequence, block after
+ *      block, and their length becomes 0.  A place in the batch can take a new request in the same call.
+ *   2. Sequence i asks for new_lens[i] tokens (negative: none).  It gets all of them or none: all if its length stays within t_cap,
+ *      its rows lie within n_rows, and it needs no page or the stack still holds what it and the sequences before it ask for.
+ *      (Once one goes without for want of pages, so do all later ones that need any.)  Pages come off the top of the stack into
+ *      block_table[i * table_stride + j], in order; the table's other entries stay as they are.
+ *      granted[i] = tokens it got; seq_lens_out[i] = its length with them (seq_lens_out may be seq_lens); *n_free_out (may be n_free).
+ *   3. Rows of the step are packed by sequence: sequence i has rows row_start[i] .. row_start[i] + new_lens[i] - 1 whether it got its
+ *      tokens or not (row_start int32 [batch + 1], saturating).  For every row r < n_rows: positions[r] (int32) the token's position
+ *      in its sequence and slot_map[r] (int64) = page * block_size + token of the page, as eta_append_tokens takes it; 0 and
+ *      -1 for rows without a place (a sequence that got none, and what is left behind the last sequence).
+ * Anything that could not be served sets ETA_DEV_REFUSED.  A release of more pages than are missing from the stack is cut off there.
+ * Page numbers are handed on as they are.  block_size 32, 64 or 128; table_stride * block_size >= t_cap; n_rows <= 2^30.  n_rows = 0:
+ * slot_map and positions may be NULL.
+ * Launched with programmatic dependent launch: waits for everything before it in the stream before it reads or writes, and the rows'
+ * slots are complete before its successors start.  Deterministic.  Two calls that share a stack or a table must not overlap.
+ */
+int eta_plan_pages(int32_t batch, int32_t block_size, int32_t t_cap, const int32_t* new_lens, const int32_t* release,
+                   const int32_t* seq_lens, int32_t* seq_lens_out, int32_t* block_table, int32_t table_stride, int32_t* free_pages,
+                   const int32_t* n_free, int32_t* n_free_out, int32_t n_pages, int32_t n_rows, int64_t* slot_map,
+                   int32_t* positions, int32_t* row_start, int32_t* granted, uint32_t* status_dev, void* stream);
 
 /* Size of the built-in scratch of eta_decode_static, in bytes. */
 size_t eta_static_scratch_bytes(void);

@@ -24,11 +24,12 @@ ETA_FLAG_PACKED_SIGMA = 4
 ETA_BUILD_SIGMA_ENVELOPE = 1
 ETA_BUILD_PACKED_SIGMA = 2
 ETA_DEV_TIMEOUT, ETA_DEV_LEN_CLAMPED, ETA_DEV_EMPTY_ROW = 1, 2, 4
+ETA_DEV_REFUSED = 16
 
 EXPORTS = ("eta_workspace_bytes", "eta_build_block_summaries", "eta_append_summary", "eta_build_block_summaries_paged",
            "eta_append_summary_paged", "eta_decode_paged", "eta_stage_query", "eta_predict_threshold",
            "eta_score_dual", "eta_calibration_workspace_bytes", "eta_calibrate_head_const", "eta_decode", "eta_decode_static", "eta_static_scratch_bytes", "eta_decode_kernel_count", "eta_decode_launches", "eta_profile_enable", "eta_profile_read",
-           "eta_profile_kernel_name", "eta_set_pdl", "eta_strerror", "eta_last_cuda_error")
+           "eta_profile_kernel_name", "eta_set_pdl", "eta_strerror", "eta_last_cuda_error", "eta_plan_pages")
 
 
 class CacheDesc(ctypes.Structure):
@@ -55,7 +56,7 @@ class EtaError(RuntimeError):
 _lib = None
 _native = None          # the compiled marshalling module, or what stands for it where it is missing
 _STEP_CALLS = ("eta_append_summary", "eta_append_summary_paged", "eta_predict_threshold", "eta_decode", "eta_decode_paged",
-               "eta_decode_static")
+               "eta_decode_static", "eta_plan_pages")
 
 
 class _Missing:
@@ -108,6 +109,8 @@ def load(path: str | None = None) -> ctypes.CDLL:
                                                  i32, ctypes.c_float, ctypes.c_float, f32p, f32p, vp, ctypes.c_size_t, vp]
         lib.eta_decode.argtypes = [D, P, vp, vp, vp, i32p, vp, f32p, f32p, f32p, f32p, vp, i32p, vp, vp,
                                    ctypes.c_size_t, vp]
+        lib.eta_plan_pages.argtypes = [i32, i32, i32, i32p, i32p, i32p, i32p, i32p, i32, i32p, i32p, i32p, i32, i32, vp, i32p, i32p,
+                                       i32p, vp, vp]
         lib.eta_decode_static.argtypes = [D, P, vp, vp, vp, i32p, vp, f32p, f32p, f32p, f32p, vp, i32p, vp, vp]
         lib.eta_static_scratch_bytes.restype = ctypes.c_size_t
         lib.eta_decode_kernel_count.restype = ctypes.c_int
@@ -324,6 +327,19 @@ def eta_decode_static(desc, params: DecodeParams, q, K, V, seq_lens, musig, mnor
                                out, sel_mask, stats, status)
     if rc:
         _check(rc, "eta_decode_static")
+
+
+def eta_plan_pages(block_size: int, t_cap: int, new_lens, seq_lens, block_table, free_pages, n_free, slot_map, positions, row_start,
+                   granted, seq_lens_out=None, n_free_out=None, release=None, status=None) -> None:
+    """Block tables and slot maps from request lengths (see include/eta.h): pages of released sequences go back to the free stack, new
+    tokens get pages, `granted`, `row_start`, `slot_map` and `positions` say where they go.  int32 CUDA tensors on the current
+    device, slot_map int64; lengths and the free count are updated in place unless outputs are given."""
+    lib = _lib or load()
+    rc = _native.plan(lib.addresses["eta_plan_pages"], block_size, t_cap, new_lens, release, seq_lens,
+                      seq_lens if seq_lens_out is None else seq_lens_out, block_table, free_pages, n_free,
+                      n_free if n_free_out is None else n_free_out, slot_map, positions, row_start, granted, status)
+    if rc:
+        _check(rc, "eta_plan_pages")
 
 
 def eta_static_scratch_bytes() -> int:

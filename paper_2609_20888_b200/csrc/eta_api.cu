@@ -19,7 +19,8 @@ void set_cuda_error(cudaError_t e, const char* where) {
     snprintf(g_cuda_error, sizeof g_cuda_error, "%s: %s", where, cudaGetErrorString(e));
 }
 
-int validate_desc(const eta_cache_desc* d) {
+// what every call on a cache asks of its shape
+int validate_shape(const eta_cache_desc* d) {
     if (!d) return ETA_ERR_INVALID_ARG;
     if (d->batch <= 0 || d->n_q_heads <= 0 || d->n_kv_heads <= 0 || d->t_cap <= 0 || d->nb_cap <= 0)
         return ETA_ERR_INVALID_ARG;
@@ -28,13 +29,30 @@ int validate_desc(const eta_cache_desc* d) {
     if (G != 1 && G != 2 && G != 4 && G != 8) return ETA_ERR_UNSUPPORTED;
     if (d->head_dim != 64 && d->head_dim != 128) return ETA_ERR_UNSUPPORTED;
     if (d->block_size != 32 && d->block_size != 64 && d->block_size != 128) return ETA_ERR_UNSUPPORTED;
-    if ((int64_t)d->nb_cap * d->block_size < d->t_cap - d->block_size + 1) return ETA_ERR_INVALID_ARG;
-    if (d->nb_cap >= (1 << 24)) return ETA_ERR_UNSUPPORTED;   // block index shares a word with the head bits
-    if ((int64_t)d->batch * d->n_kv_heads > MAX_ROWS) return ETA_ERR_UNSUPPORTED;
+    return ETA_OK;
+}
+
+// a bf16 cache's strides
+int validate_strides(const eta_cache_desc* d) {
     if (d->k_stride_t % 8 || d->k_stride_h % 8 || d->k_stride_b % 8) return ETA_ERR_UNSUPPORTED;
     if (d->v_stride_t % 8 || d->v_stride_h % 8 || d->v_stride_b % 8) return ETA_ERR_UNSUPPORTED;
     if (d->k_stride_t < d->head_dim || d->v_stride_t < d->head_dim) return ETA_ERR_INVALID_ARG;
     return ETA_OK;
+}
+
+// a cache with its block index, as a step sees it
+int validate_index(const eta_cache_desc* d) {
+    const int rc = validate_shape(d);
+    if (rc != ETA_OK) return rc;
+    if ((int64_t)d->nb_cap * d->block_size < d->t_cap - d->block_size + 1) return ETA_ERR_INVALID_ARG;
+    if (d->nb_cap >= (1 << 24)) return ETA_ERR_UNSUPPORTED;   // block index shares a word with the head bits
+    if ((int64_t)d->batch * d->n_kv_heads > MAX_ROWS) return ETA_ERR_UNSUPPORTED;
+    return ETA_OK;
+}
+
+int validate_desc(const eta_cache_desc* d) {
+    const int rc = validate_index(d);
+    return rc != ETA_OK ? rc : validate_strides(d);
 }
 
 // Optional per-kernel timing: host-side CUDA events recorded between the launches of one decode step

@@ -23,7 +23,10 @@ inline int check_launch(const char* where) {
     if (e != cudaSuccess) { set_cuda_error(e, where); return ETA_ERR_CUDA; }
     return ETA_OK;
 }
-int validate_desc(const eta_cache_desc* d);
+int validate_shape(const eta_cache_desc* d);       // head counts, head_dim, block size
+int validate_strides(const eta_cache_desc* d);     // of a bf16 cache
+int validate_index(const eta_cache_desc* d);       // shape and block capacity
+int validate_desc(const eta_cache_desc* d);        // all of it
 int validate_pages(const eta_cache_desc* desc, const eta_page_table* pages);
 // Measurement aid: when profiling is enabled, records timing event k on the stream (see eta_profile_enable).
 void profile_mark(int k, cudaStream_t s);

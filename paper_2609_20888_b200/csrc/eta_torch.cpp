@@ -1,4 +1,4 @@
-// Marshalling of the calls of a decode step (append, predict, decode) for torch: checks the tensors, takes their device
+// Marshalling of the calls of a decode step (page plan, append, predict, decode) for torch: checks the tensors, takes their device
 // pointers and the current stream, and calls the C ABI.  Nothing is computed or kept here.
 //
 // Through ctypes the checks and conversions of a step's 30 arguments took 20 us of Python, more than a small step takes on
@@ -32,6 +32,8 @@ const char* dtype_name(at::ScalarType t) {
         case at::kInt: return "torch.int32";
         case at::kByte: return "torch.uint8";
         case at::kHalf: return "torch.float16";
+        case at::kLong: return "torch.int64";
+        case at::kDouble: return "torch.float64";
         default: return nullptr;
     }
 }
@@ -237,6 +239,74 @@ PyObject* decode(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return PyLong_FromLong(rc);
 }
 
+// A contiguous CUDA tensor of the given type on the current device, of n elements (n < 0: any number); None where `optional`.
+bool vector(PyObject* o, at::ScalarType type, const char* name, int64_t n, void** out, bool optional = false) {
+    if (o == Py_None && !optional) return fail(name, "a tensor, not None");
+    if (!pointer(o, type, name, out)) return false;
+    if (o == Py_None) return true;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.device().index() != c10::cuda::current_device()) return fail(name, "on the current CUDA device");
+    if (!t.is_contiguous()) return fail(name, "contiguous");
+    if (n >= 0 && t.numel() != n) {
+        PyErr_Format(g_error, "%s must have %lld elements, got %lld", name, (long long)n, (long long)t.numel());
+        return false;
+    }
+    return true;
+}
+#define VEC(o, type, name, n) vector(o, type, #name, n, (void**)&name)
+#define OPT(o, type, name, n) vector(o, type, #name, n, (void**)&name, true)
+
+bool int32_of(PyObject* o, int32_t* out) {
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) return false;
+    if (v < INT32_MIN || v > INT32_MAX) {
+        PyErr_SetString(PyExc_OverflowError, "an argument does not fit 32 bits");
+        return false;
+    }
+    *out = (int32_t)v;
+    return true;
+}
+
+// (address, block_size, t_cap, new_lens, release, seq_lens, seq_lens_out, block_table, free_pages, n_free, n_free_out, slot_map,
+//  positions, row_start, granted, status) -> return code
+PyObject* plan(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    using F = int (*)(int32_t, int32_t, int32_t, const int32_t*, const int32_t*, const int32_t*, int32_t*, int32_t*, int32_t, int32_t*,
+                      const int32_t*, int32_t*, int32_t, int32_t, int64_t*, int32_t*, int32_t*, int32_t*, uint32_t*, void*);
+    F fn;
+    int32_t block_size, t_cap, *new_lens, *release, *seq_lens, *seq_lens_out, *block_table, *free_pages, *n_free, *n_free_out, *positions,
+        *row_start, *granted;
+    int64_t* slot_map;
+    uint32_t* status;
+    if (!count(n, 16) || !entry(v[0], &fn) || !int32_of(v[1], &block_size) || !int32_of(v[2], &t_cap)) return nullptr;
+    if (!VEC(v[3], at::kInt, new_lens, -1)) return nullptr;
+    const int64_t batch = THPVariable_Unpack(v[3]).numel();
+    if (!OPT(v[4], at::kInt, release, batch) || !VEC(v[5], at::kInt, seq_lens, batch) || !VEC(v[6], at::kInt, seq_lens_out, batch) ||
+        !VEC(v[8], at::kInt, free_pages, -1) || !VEC(v[9], at::kInt, n_free, 1) || !VEC(v[10], at::kInt, n_free_out, 1) ||
+        !OPT(v[11], at::kLong, slot_map, -1))
+        return nullptr;
+    const int64_t rows = v[11] == Py_None ? 0 : THPVariable_Unpack(v[11]).numel(), pages = THPVariable_Unpack(v[8]).numel();
+    if (!(v[11] == Py_None ? OPT(v[12], at::kInt, positions, -1) : VEC(v[12], at::kInt, positions, rows)) ||
+        !VEC(v[13], at::kInt, row_start, batch + 1) || !VEC(v[14], at::kInt, granted, batch) || !OPT(v[15], at::kInt, status, 1))
+        return nullptr;
+    if (!PTR(v[7], at::kInt, block_table)) return nullptr;
+    if (!block_table && v[7] == Py_None) return fail("block_table", "a tensor, not None"), nullptr;
+    const at::Tensor& table = THPVariable_Unpack(v[7]);
+    if (table.device().index() != c10::cuda::current_device()) return fail("block_table", "on the current CUDA device"), nullptr;
+    if (table.dim() != 2 || table.size(0) != batch || table.stride(1) != 1 || (batch > 1 && table.stride(0) < table.size(1)))
+        return fail("block_table", "[batch, pages of a sequence] with unit stride along its second axis"), nullptr;
+    // the row's stride where there is a next row, its length where not
+    const int64_t stride = batch > 1 ? table.stride(0) : table.size(1);
+    if (table.size(1) * (int64_t)block_size < t_cap) return fail("block_table", "wide enough for t_cap tokens"), nullptr;
+    if (batch > INT32_MAX || rows > INT32_MAX || pages > INT32_MAX || stride > INT32_MAX) return fail("sizes", "below 2^31"), nullptr;
+    void* const s = stream();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn((int32_t)batch, block_size, t_cap, new_lens, release, seq_lens, seq_lens_out, block_table, (int32_t)stride, free_pages, n_free,
+            n_free_out, (int32_t)pages, (int32_t)rows, slot_map, positions, row_start, granted, status, s);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
 // the eta_params a call would get, as bytes (for the tests)
 PyObject* params(PyObject*, PyObject* const* v, Py_ssize_t n) {
     eta_params p;
@@ -273,6 +343,7 @@ PyMethodDef methods[] = {
     {"decode", (PyCFunction)(void (*)(void))guarded<decode<Decode::PLAIN>>, METH_FASTCALL, nullptr},
     {"decode_paged", (PyCFunction)(void (*)(void))guarded<decode<Decode::PAGED>>, METH_FASTCALL, nullptr},
     {"decode_static", (PyCFunction)(void (*)(void))guarded<decode<Decode::STATIC>>, METH_FASTCALL, nullptr},
+    {"plan", (PyCFunction)(void (*)(void))guarded<plan>, METH_FASTCALL, nullptr},
     {"params", (PyCFunction)(void (*)(void))guarded<params>, METH_FASTCALL, nullptr},
     {"set_classes", (PyCFunction)(void (*)(void))set_classes, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
