@@ -63,6 +63,7 @@ typedef enum eta_status {
 #define ETA_DEV_TIMEOUT      1u  /* a bounded wait inside a kernel ran out; outputs are not valid */
 #define ETA_DEV_LEN_CLAMPED  2u  /* some seq_lens[i] exceeded t_cap and was clamped */
 #define ETA_DEV_EMPTY_ROW    4u  /* some seq_lens[i] <= 0: that sequence's output is zero */
+#define ETA_DEV_BAD_SLOT     8u  /* a slot of eta_append_tokens lies past the cache: that row was skipped */
 #define ETA_DEV_REFUSED     16u  /* eta_plan_pages could not serve some sequence (granted says which), or more pages came back than exist */
 
 /* flags of eta_params.flags */
@@ -336,6 +337,83 @@ int eta_plan_pages(int32_t batch, int32_t block_size, int32_t t_cap, const int32
                    const int32_t* seq_lens, int32_t* seq_lens_out, int32_t* block_table, int32_t table_stride, int32_t* free_pages,
                    const int32_t* n_free, int32_t* n_free_out, int32_t n_pages, int32_t n_rows, int64_t* slot_map,
                    int32_t* positions, int32_t* row_start, int32_t* granted, uint32_t* status_dev, void* stream);
+
+/*
+ * New tokens of a step (deployment plumbing around the method; the paper takes "post-RoPE query heads" and a filled cache as given).  A
+ * model's projections of n_rows tokens go in, what the rest of the step reads comes out:
+ *   - queries and keys of every head, normalised where a weight is given (fp32 [head_dim], one for all heads; NULL: no norm):
+ *       y = x * w / sqrt(mean_c x_c^2 + eps),
+ *     and rotated by their token's position in the first rotary_dim channels: the pairs (c, c + rotary_dim / 2), or with
+ *     ETA_TOKENS_INTERLEAVED (2 c, 2 c + 1), turn by positions[r] * inv_freq[c] radians.  inv_freq is fp64 [rotary_dim / 2]; the angle is
+ *     formed and reduced in fp64, so that far positions lose nothing.  Scaled frequencies are the caller's to give.
+ *   - q_out bf16 [n_rows, n_q_heads, head_dim], contiguous: the q of eta_predict_threshold and eta_decode.
+ *   - keys (after norm and rotation) and values (as they are) at their places in the cache, slot_map int64 [n_rows]: page *
+ *     block_size + token of the page where n_pages > 0 (a paged cache, as eta_plan_pages makes them), else sequence * t_cap + token.
+ * A row with a negative slot is skipped: nothing of it is read or written, its row of q_out included.  A slot past the cache is
+ * skipped too and sets ETA_DEV_BAD_SLOT.  The rows of a call have different slots (of two rows with one slot the cache would hold
+ * either, or a mixture).  Places that no row names keep their bytes.
+ * Arithmetic is fp32 with one rounding, to bf16, at the end.  For the 4-bit cache keys are worked out in fp64 up to the quotient that
+ * is rounded to a code, so that a key next to a border between two codes gets the same one whatever the order of the sums: the
+ * same tokens give the same bytes.
+ * q, k, v are [n_rows, heads, head_dim] of one type, unit stride along head_dim, the other strides multiples of 16 bytes; they may be
+ * parts of one projection.  Pointers 16-byte aligned (slot_map and inv_freq 8, positions 4).  Of the cache descriptor n_q_heads, n_kv_heads,
+ * head_dim, block_size, batch, t_cap and strides are used; unlike a step's, batch * n_kv_heads is not limited.  rotary_dim: a
+ * multiple of 16 up to head_dim; 0: no rotation, inv_freq and positions may be NULL.
+ * Launched with programmatic dependent launch: the kernel waits for everything before it in the stream before it reads or
+ * writes, and releases its successors only as it ends.
+ */
+#define ETA_TYPE_BF16 0
+#define ETA_TYPE_FP16 1
+#define ETA_TYPE_FP32 2
+#define ETA_TOKENS_INTERLEAVED 1u
+typedef struct eta_tokens_desc {
+    int32_t n_rows, type, rotary_dim;           /* type: ETA_TYPE_* of q, k and v */
+    uint32_t flags;                             /* ETA_TOKENS_* */
+    int64_t q_stride_r, q_stride_h, k_stride_r, k_stride_h, v_stride_r, v_stride_h;   /* elements: row to row, head to head */
+    float eps;
+} eta_tokens_desc;
+
+int eta_append_tokens(const eta_cache_desc* desc, const eta_tokens_desc* tokens, const void* q, const void* k, const void* v,
+                      const float* q_weight, const float* k_weight, const double* inv_freq, const int32_t* positions,
+                      const int64_t* slot_map, int32_t n_pages, void* q_out, void* K, void* V, uint32_t* status_dev, void* stream);
+
+/*
+ * A cache held in 4 bits (the paper's outlook names low-precision storage; the format is this library's).  A block of block_size
+ * tokens of one KV head is one run of bytes, K and V together:
+ *   K codes [block_size][head_dim / 2], K scales [block_size][head_dim / 16], V codes, V scales (the same shapes).
+ * A code is a 4-bit float (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6; bit 3 the sign), channel 2 j in the low half of byte j; a scale is an 8-bit
+ * float (e4m3, not negative) shared by 16 consecutive channels of a token.  The value is code * scale * k_scale (or v_scale), with one
+ * fp32 number for all of K and one for all of V.  72 bytes per token and tensor at head_dim 128, where bf16 takes 256.
+ * A group x is written with the scale e4m3(max|x| / (6 k_scale)) and the codes e2m1(x / (scale * k_scale)): quotients rounded to fp32,
+ * then to the nearest, ties to even; magnitudes beyond the largest saturate (at 6 * 448 * k_scale); a group that holds a NaN gets
+ * the NaN scale, and with it reads as NaN; a group whose scale rounds to zero gets positive zeros.
+ * Block j of sequence i, KV head hk, is at pool + i * stride_b + hk * stride_h + j * stride_j; in a paged cache (a page table, or n_pages
+ * > 0) page p is at pool + p * stride_b + hk * stride_h.  Strides in bytes, multiples of 16, pool 16-byte aligned; blocks may not overlap.
+ * A contiguous cache has room for ceil(t_cap / block_size) blocks per sequence.  A block that holds a token is read whole.
+ * Of the eta_cache_desc the strides are looked at by eta_unpack_kv4 only.
+ */
+typedef struct eta_kv4_desc {
+    int64_t stride_b, stride_h, stride_j;       /* bytes: sequence (or page), KV head, block of a sequence (paged: not read) */
+    float k_scale, v_scale;                     /* finite, > 0 */
+} eta_kv4_desc;
+
+/* Bytes of a block of one KV head: 2 * block_size * (head_dim / 2 + head_dim / 16); 0 for sizes outside the supported set. */
+size_t eta_kv4_block_bytes(int32_t block_size, int32_t head_dim);
+
+/* eta_append_tokens into a 4-bit cache.  n_pages > 0: paged. */
+int eta_append_tokens_kv4(const eta_cache_desc* desc, const eta_kv4_desc* kv4, const eta_tokens_desc* tokens, const void* q,
+                          const void* k, const void* v, const float* q_weight, const float* k_weight, const double* inv_freq,
+                          const int32_t* positions, const int64_t* slot_map, int32_t n_pages, void* q_out, void* pool,
+                          uint32_t* status_dev, void* stream);
+
+/*
+ * What a 4-bit cache stands for, as a bf16 cache: every token of every block, K and V of the descriptor's strides ([batch, n_kv_heads,
+ * t_cap, head_dim], or with n_pages > 0 [n_pages, n_kv_heads, block_size, head_dim]).  fp32 arithmetic, rounded once: exact where
+ * k_scale and v_scale are powers of two.  Launched with programmatic dependent launch: waits for everything before it before it
+ * reads or writes.
+ */
+int eta_unpack_kv4(const eta_cache_desc* desc, const eta_kv4_desc* kv4, const void* pool, int32_t n_pages, void* K, void* V,
+                   void* stream);
 
 /* Size of the built-in scratch of eta_decode_static, in bytes. */
 size_t eta_static_scratch_bytes(void);

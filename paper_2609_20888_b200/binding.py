@@ -24,12 +24,14 @@ ETA_FLAG_PACKED_SIGMA = 4
 ETA_BUILD_SIGMA_ENVELOPE = 1
 ETA_BUILD_PACKED_SIGMA = 2
 ETA_DEV_TIMEOUT, ETA_DEV_LEN_CLAMPED, ETA_DEV_EMPTY_ROW = 1, 2, 4
-ETA_DEV_REFUSED = 16
+ETA_DEV_BAD_SLOT, ETA_DEV_REFUSED = 8, 16
+ETA_TOKENS_INTERLEAVED = 1
 
 EXPORTS = ("eta_workspace_bytes", "eta_build_block_summaries", "eta_append_summary", "eta_build_block_summaries_paged",
            "eta_append_summary_paged", "eta_decode_paged", "eta_stage_query", "eta_predict_threshold",
            "eta_score_dual", "eta_calibration_workspace_bytes", "eta_calibrate_head_const", "eta_decode", "eta_decode_static", "eta_static_scratch_bytes", "eta_decode_kernel_count", "eta_decode_launches", "eta_profile_enable", "eta_profile_read",
-           "eta_profile_kernel_name", "eta_set_pdl", "eta_strerror", "eta_last_cuda_error", "eta_plan_pages")
+           "eta_profile_kernel_name", "eta_set_pdl", "eta_strerror", "eta_last_cuda_error", "eta_plan_pages",
+           "eta_append_tokens", "eta_append_tokens_kv4", "eta_kv4_block_bytes", "eta_unpack_kv4")
 
 
 class CacheDesc(ctypes.Structure):
@@ -49,6 +51,17 @@ class PageTable(ctypes.Structure):
     _fields_ = [("block_table", ctypes.c_void_p), ("table_stride", ctypes.c_int32), ("n_pages", ctypes.c_int32)]
 
 
+class Kv4Desc(ctypes.Structure):
+    _fields_ = [("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_j", ctypes.c_int64),
+                ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float)]
+
+
+class TokensDesc(ctypes.Structure):
+    _fields_ = [("n_rows", ctypes.c_int32), ("type", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("flags", ctypes.c_uint32),
+                ("q_stride_r", ctypes.c_int64), ("q_stride_h", ctypes.c_int64), ("k_stride_r", ctypes.c_int64),
+                ("k_stride_h", ctypes.c_int64), ("v_stride_r", ctypes.c_int64), ("v_stride_h", ctypes.c_int64), ("eps", ctypes.c_float)]
+
+
 class EtaError(RuntimeError):
     pass
 
@@ -56,7 +69,7 @@ class EtaError(RuntimeError):
 _lib = None
 _native = None          # the compiled marshalling module, or what stands for it where it is missing
 _STEP_CALLS = ("eta_append_summary", "eta_append_summary_paged", "eta_predict_threshold", "eta_decode", "eta_decode_paged",
-               "eta_decode_static", "eta_plan_pages")
+               "eta_decode_static", "eta_plan_pages", "eta_append_tokens", "eta_append_tokens_kv4", "eta_unpack_kv4")
 
 
 class _Missing:
@@ -74,7 +87,7 @@ def _marshalling():
         from . import _eta_torch
     except ImportError as e:
         return _Missing(e)
-    _eta_torch.set_classes(EtaError, CacheDesc, PageTable, DecodeParams, Params)
+    _eta_torch.set_classes(EtaError, CacheDesc, PageTable, DecodeParams, Params, Kv4Desc)
     return _eta_torch
 
 
@@ -111,6 +124,12 @@ def load(path: str | None = None) -> ctypes.CDLL:
                                    ctypes.c_size_t, vp]
         lib.eta_plan_pages.argtypes = [i32, i32, i32, i32p, i32p, i32p, i32p, i32p, i32, i32p, i32p, i32p, i32, i32, vp, i32p, i32p,
                                        i32p, vp, vp]
+        Q4, TD = ctypes.POINTER(Kv4Desc), ctypes.POINTER(TokensDesc)
+        lib.eta_append_tokens.argtypes = [D, TD, vp, vp, vp, f32p, f32p, vp, i32p, vp, i32, vp, vp, vp, vp, vp]
+        lib.eta_append_tokens_kv4.argtypes = [D, Q4, TD, vp, vp, vp, f32p, f32p, vp, i32p, vp, i32, vp, vp, vp, vp]
+        lib.eta_unpack_kv4.argtypes = [D, Q4, vp, i32, vp, vp, vp]
+        lib.eta_kv4_block_bytes.argtypes = [i32, i32]
+        lib.eta_kv4_block_bytes.restype = ctypes.c_size_t
         lib.eta_decode_static.argtypes = [D, P, vp, vp, vp, i32p, vp, f32p, f32p, f32p, f32p, vp, i32p, vp, vp]
         lib.eta_static_scratch_bytes.restype = ctypes.c_size_t
         lib.eta_decode_kernel_count.restype = ctypes.c_int
@@ -125,7 +144,7 @@ def load(path: str | None = None) -> ctypes.CDLL:
         lib.eta_profile_kernel_name.argtypes = [ctypes.c_int]
         for name in EXPORTS:
             if name not in ("eta_strerror", "eta_last_cuda_error", "eta_decode_kernel_count",
-                            "eta_profile_kernel_name", "eta_static_scratch_bytes"):
+                            "eta_profile_kernel_name", "eta_static_scratch_bytes", "eta_kv4_block_bytes"):
                 getattr(lib, name).restype = ctypes.c_int
         lib.addresses = {name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _STEP_CALLS}
         if path is not None:
@@ -340,6 +359,68 @@ def eta_plan_pages(block_size: int, t_cap: int, new_lens, seq_lens, block_table,
                       n_free if n_free_out is None else n_free_out, slot_map, positions, row_start, granted, status)
     if rc:
         _check(rc, "eta_plan_pages")
+
+
+def eta_append_tokens(desc: CacheDesc, q, k, v, slot_map, positions, q_out, K, V, inv_freq=None, q_weight=None, k_weight=None,
+                      eps: float = 1e-6, interleaved: bool = False, paged: bool = False, status=None) -> None:
+    """A step's new tokens (see include/eta.h): q [rows, n_q_heads, head_dim], k and v [rows, n_kv_heads, head_dim] (bf16, fp16 or fp32; parts of one
+    projection will do) are normed per head and rotated by their positions; queries go to q_out (bf16), keys and values to the
+    places of K and V that slot_map (int64 [rows]) names.  inv_freq: float64 [rotary_dim / 2]."""
+    lib = _lib or load()
+    rc = _native.tokens(lib.addresses["eta_append_tokens"], desc, None, q, k, v, q_weight, k_weight, inv_freq, positions, slot_map, paged,
+                        q_out, K, V, status, eps, ETA_TOKENS_INTERLEAVED if interleaved else 0)
+    if rc:
+        _check(rc, "eta_append_tokens")
+
+
+def kv4_block_bytes(block_size: int, head_dim: int) -> int:
+    """Bytes of a block of one KV head of a 4-bit cache, K and V together."""
+    return load().eta_kv4_block_bytes(block_size, head_dim)
+
+
+def kv4_cache_desc(pool: torch.Tensor, n_q_heads: int, head_dim: int, block_size: int, batch: int | None = None, t_cap: int | None = None,
+                   nb_cap: int | None = None, k_scale: float = 1.0, v_scale: float = 1.0) -> tuple[CacheDesc, Kv4Desc]:
+    """Describe a 4-bit cache: pool uint8 [batch, n_kv_heads, blocks, block bytes], or paged [n_pages, n_kv_heads, block bytes] with the batch
+    and the capacity of a sequence (any strides of multiples of 16 bytes, unit stride along the bytes)."""
+    if pool.dim() not in (3, 4) or pool.stride(-1) != 1 or pool.dtype != torch.uint8 or pool.shape[-1] != kv4_block_bytes(block_size, head_dim):
+        raise EtaError("pool must be uint8 [batch, n_kv_heads, blocks, block bytes] or [n_pages, n_kv_heads, block bytes]")
+    paged = pool.dim() == 3
+    if paged and (batch is None or t_cap is None):
+        raise EtaError("a paged cache needs the batch and t_cap")
+    if not paged and batch not in (None, pool.shape[0]):
+        raise EtaError("batch and pool do not agree")
+    batch = pool.shape[0] if batch is None else batch
+    t_cap = pool.shape[2] * block_size if t_cap is None else t_cap
+    if not paged and pool.shape[2] * block_size < t_cap:
+        raise EtaError("pool has too few blocks for t_cap tokens")
+    nb = nb_cap if nb_cap is not None else (t_cap + block_size - 1) // block_size
+    Hkv, tokens = pool.shape[1], block_size if paged else t_cap
+    bf16 = (Hkv * tokens * head_dim, tokens * head_dim, head_dim)          # of the bf16 cache it stands for
+    least = pool.shape[-1]                                                 # where an axis has one element its stride says nothing
+    strides = [pool.stride(k) if pool.shape[k] > 1 else least for k in range(pool.dim() - 1)]
+    return (CacheDesc(batch, n_q_heads, Hkv, head_dim, block_size, t_cap, nb, *bf16, *bf16),
+            Kv4Desc(strides[0], strides[1], 0 if paged else strides[2], k_scale, v_scale))
+
+
+def eta_append_tokens_kv4(desc: CacheDesc, kv4: Kv4Desc, q, k, v, slot_map, positions, q_out, pool, inv_freq=None, q_weight=None,
+                          k_weight=None, eps: float = 1e-6, interleaved: bool = False, status=None) -> None:
+    """eta_append_tokens into a 4-bit cache."""
+    lib = _lib or load()
+    if kv4 is None:
+        raise EtaError("kv4 must be a Kv4Desc")
+    rc = _native.tokens(lib.addresses["eta_append_tokens_kv4"], desc, kv4, q, k, v, q_weight, k_weight, inv_freq, positions, slot_map, None,
+                        q_out, pool, None, status, eps, ETA_TOKENS_INTERLEAVED if interleaved else 0)
+    if rc:
+        _check(rc, "eta_append_tokens_kv4")
+
+
+def eta_unpack_kv4(desc: CacheDesc, kv4: Kv4Desc, pool, K, V) -> None:
+    """What a 4-bit cache stands for, as a bf16 cache K, V [batch, n_kv_heads, t_cap, head_dim] (paged: [n_pages, n_kv_heads, block_size,
+    head_dim]), any strides."""
+    lib = _lib or load()
+    rc = _native.unpack(lib.addresses["eta_unpack_kv4"], desc, kv4, pool, K, V)
+    if rc:
+        _check(rc, "eta_unpack_kv4")
 
 
 def eta_static_scratch_bytes() -> int:

@@ -1,0 +1,389 @@
+// New tokens of a step: norm of every query and key head, rotation by position, the queries stored for the step and the keys and
+// values written to the cache, bf16 or 4-bit, in one pass over the projections; and a 4-bit cache read back as a bf16 one.
+//
+//   y = x * w / sqrt(mean_c x_c^2 + eps);   (a, b) -> (a cos - b sin, a sin + b cos),  angle = position * inv_freq
+//
+// A warp takes one row's heads two (d = 128) or four (64) at a time, a piece of eight channels per lane: a head's sum and a channel's
+// partner are shuffles away, and everything is read once and written once.
+#include <math.h>
+
+#include <type_traits>
+
+#include "eta_kv4.cuh"
+
+namespace eta {
+
+struct TokensArgs {
+    const void *q, *k, *v;
+    const float *q_weight, *k_weight;
+    const double* inv_freq;
+    const int32_t* positions;
+    const int64_t* slot_map;
+    __nv_bfloat16 *q_out, *K, *V;
+    unsigned char* pool;
+    uint32_t* status;
+    int64_t q_sr, q_sh, k_sr, k_sh, v_sr, v_sh;       // elements
+    int64_t ks_b, ks_h, ks_t, vs_b, vs_h, vs_t;       // bf16 cache: elements; 4-bit: ks_* in bytes (page or sequence, head, block)
+    int64_t limit;                                    // slots of the cache
+    int rows, Hq, Hkv, per_page, b, parts, rotary, interleaved;
+    double k_scale, v_scale;
+    float eps;
+};
+
+// eight consecutive channels
+template <typename T>
+struct Piece {
+    uint4 w[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p, bool on) {
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+            w[k] = make_uint4(0, 0, 0, 0);
+            if (on) w[k] = __ldcg(reinterpret_cast<const uint4*>(p) + k);
+        }
+    }
+    template <typename F>
+    __device__ __forceinline__ void get(F (&x)[8]) const {
+        const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if constexpr (sizeof(T) == 4) x[k] = (F)__uint_as_float(u[k]);
+            else if constexpr (std::is_same<T, __half>::value) x[k] = (F)((k & 1) ? f16_hi(u[k / 2]) : f16_lo(u[k / 2]));
+            else x[k] = (F)((k & 1) ? bf16_hi(u[k / 2]) : bf16_lo(u[k / 2]));
+        }
+    }
+};
+
+__device__ __forceinline__ uint4 pack_bf16(const float (&x)[8]) {
+    uint4 o;
+    uint32_t* u = reinterpret_cast<uint32_t*>(&o);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]);
+        u[k] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return o;
+}
+
+// Norm and rotation of a head's piece, in fp32 or fp64.  cs, sn: the row's angles, pair by pair.
+template <int D, typename F, typename CT>
+__device__ __forceinline__ void norm_rotate(F (&x)[8], const float* weight, float eps, int lane, int rotary, bool interleaved,
+                                            const CT* cs, const CT* sn) {
+    constexpr int LPH = D / 8;
+    const int cl = lane % LPH;
+    if (weight) {
+        F ss = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) ss = fma(x[k], x[k], ss);
+#pragma unroll
+        for (int s = 1; s < LPH; s <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, s);
+        const F r = rsqrt(ss * (F)(1.0 / D) + (F)eps);
+        const float4 w0 = *reinterpret_cast<const float4*>(weight + 8 * cl), w1 = *reinterpret_cast<const float4*>(weight + 8 * cl + 4);
+        const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = x[k] * r * (F)w[k];
+    }
+    if (!rotary) return;
+    const bool turns = 8 * cl < rotary;
+    if (interleaved) {
+        if (turns) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const F c = (F)cs[4 * cl + k], s = (F)sn[4 * cl + k], a = x[2 * k], b = x[2 * k + 1];
+                x[2 * k] = a * c - b * s;
+                x[2 * k + 1] = a * s + b * c;
+            }
+        }
+        return;
+    }
+    const int reach = rotary / 16;                     // lanes between the two halves of a pair
+    const bool first = cl < reach;
+    const int partner = turns ? (first ? lane + reach : lane - reach) : lane, at = first ? 8 * cl : 8 * (cl - reach);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const F y = __shfl_sync(0xffffffffu, x[k], partner);
+        if (turns) {
+            const F c = (F)cs[at + k], s = (F)sn[at + k];
+            x[k] = first ? x[k] * c - y * s : y * s + x[k] * c;
+        }
+    }
+}
+
+// Eight channels of a row into a 4-bit block: the two lanes that hold a group agree on its scale.
+__device__ __forceinline__ void store_kv4(const double (&x)[8], double g, unsigned char* codes, unsigned char* scales, int cl, bool on) {
+    double top = 0;
+    bool nan = false;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { top = fmax(top, fabs(x[k])); nan = nan || isnan(x[k]); }
+    top = fmax(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    nan = (__shfl_xor_sync(0xffffffffu, nan ? 1 : 0, 1) != 0) || nan;
+    const float want = nan ? __uint_as_float(0x7fffffffu) : (float)(top / (6.0 * g));
+    unsigned short pair;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(pair) : "f"(0.f), "f"(want));
+    const uint32_t code = pair & 0xffu;
+    const double scale = (double)f16_lo(e4m3x2_to_f16x2(code));
+    const bool any = scale > 0;                                    // (false for a NaN too)
+    const double inv = any ? 1.0 / (scale * g) : 0.0;
+    uint32_t bytes = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float lo = any ? (float)(x[2 * k] * inv) : 0.f, hi = any ? (float)(x[2 * k + 1] * inv) : 0.f;
+        bytes |= f32x2_to_e2m1x2(lo, hi) << (8 * k);
+    }
+    if (!on) return;
+    *reinterpret_cast<uint32_t*>(codes + 4 * cl) = bytes;
+    if ((cl & 1) == 0) scales[cl / 2] = (unsigned char)code;
+}
+
+constexpr int TOK_WARPS = 4, TOK_LOADS = 4;       // warps of a CTA; pieces that a lane has in flight
+
+template <typename T, int D, bool KV4>
+__global__ void __launch_bounds__(32 * TOK_WARPS) append_tokens_kernel(const TokensArgs a) {
+    using CT = typename std::conditional<KV4, double, float>::type;
+    constexpr int LPH = D / 8, HPW = 32 / LPH;         // lanes of a head, heads of a warp
+    __shared__ CT s_cos[TOK_WARPS][D / 2], s_sin[TOK_WARPS][D / 2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    pdl_wait();
+    const int64_t wid = (int64_t)blockIdx.x * TOK_WARPS + warp;
+    const int64_t row = wid / a.parts;
+    const int part = (int)(wid % a.parts);
+    if (row >= a.rows) return;
+    const int64_t slot = __ldcg(reinterpret_cast<const long long*>(a.slot_map) + row);
+    if (slot < 0) return;
+    if (slot >= a.limit) {
+        if (lane == 0 && part == 0 && a.status) atomicOr(a.status, ETA_DEV_BAD_SLOT);
+        return;
+    }
+    const int nq = (a.Hq + HPW - 1) / HPW, nkv = (a.Hkv + HPW - 1) / HPW, all = nq + 2 * nkv;
+    const int begin = part * all / a.parts, end = (part + 1) * all / a.parts;
+    const int hl = lane / LPH, cl = lane % LPH;
+    const T *const q = static_cast<const T*>(a.q) + row * a.q_sr, *const k = static_cast<const T*>(a.k) + row * a.k_sr,
+            *const v = static_cast<const T*>(a.v) + row * a.v_sr;
+    Piece<T> pc[TOK_LOADS];
+    auto load = [&](int it0) {
+#pragma unroll
+        for (int u = 0; u < TOK_LOADS; ++u) {
+            const int it = it0 + u;
+            const bool is_q = it < nq, is_k = it < nq + nkv;
+            const int head = (is_q ? it : (is_k ? it - nq : it - nq - nkv)) * HPW + hl;
+            const T* p = (is_q ? q + head * a.q_sh : (is_k ? k + head * a.k_sh : v + head * a.v_sh)) + 8 * cl;
+            pc[u].load(p, it < end && head < (is_q ? a.Hq : a.Hkv));
+        }
+    };
+    load(begin);
+    // ---- the row's angles, reduced by whole turns with a two-part 2 pi (Cody and Waite): any 32-bit position keeps its 64-bit angle
+    if (a.rotary && begin < nq + nkv) {
+        const double pos = (double)__ldcg(a.positions + row);
+        for (int c = lane; c < a.rotary / 2; c += 32) {
+            const double x = pos * __ldcg(a.inv_freq + c), n = rint(x * 0.15915494309189535);
+            const double r = fma(-n, 2.4492935982947064e-16, fma(-n, 6.283185307179586, x));
+            CT sn, cs;
+            if constexpr (KV4) sincos(r, &sn, &cs);
+            else sincosf((float)r, &sn, &cs);
+            s_cos[warp][c] = cs; s_sin[warp][c] = sn;
+        }
+        __syncwarp();
+    }
+    const int64_t page = slot / a.per_page;
+    const int off = (int)(slot - page * a.per_page);
+    const Kv4Block at(a.b, D);
+    for (int it0 = begin; it0 < end; it0 += TOK_LOADS) {
+        if (it0 != begin) load(it0);
+#pragma unroll
+        for (int u = 0; u < TOK_LOADS; ++u) {
+            const int it = it0 + u;
+            if (it >= end) break;                      // the same for the whole warp
+            if (it < nq) {
+                const int head = it * HPW + hl;
+                float x[8];
+                pc[u].get(x);
+                norm_rotate<D>(x, a.q_weight, a.eps, lane, a.rotary, a.interleaved != 0, s_cos[warp], s_sin[warp]);
+                if (head < a.Hq) *reinterpret_cast<uint4*>(a.q_out + (row * a.Hq + head) * D + 8 * cl) = pack_bf16(x);
+                continue;
+            }
+            const bool is_k = it < nq + nkv;
+            const int head = (is_k ? it - nq : it - nq - nkv) * HPW + hl;
+            const bool on = head < a.Hkv;
+            if constexpr (KV4) {
+                double x[8];
+                pc[u].get(x);
+                if (is_k) norm_rotate<D>(x, a.k_weight, a.eps, lane, a.rotary, a.interleaved != 0, s_cos[warp], s_sin[warp]);
+                unsigned char* blk = a.pool + page * a.ks_b + head * a.ks_h + (int64_t)(off / a.b) * a.ks_t;
+                const int t = off % a.b;
+                store_kv4(x, is_k ? a.k_scale : a.v_scale, blk + (is_k ? 0 : at.v_codes) + t * (D / 2),
+                          blk + (is_k ? at.k_scales : at.v_scales) + t * (D / KV4_GROUP), cl, on);
+            } else {
+                float x[8];
+                pc[u].get(x);
+                if (is_k) norm_rotate<D>(x, a.k_weight, a.eps, lane, a.rotary, a.interleaved != 0, s_cos[warp], s_sin[warp]);
+                __nv_bfloat16* to = is_k ? a.K + page * a.ks_b + head * a.ks_h + off * a.ks_t : a.V + page * a.vs_b + head * a.vs_h + off * a.vs_t;
+                if (on) *reinterpret_cast<uint4*>(to + 8 * cl) = pack_bf16(x);
+            }
+        }
+    }
+}
+
+// A thread per group of sixteen channels: 9 bytes in, 32 out.
+struct UnpackArgs {
+    const unsigned char* pool;
+    int64_t sb, sh, sj;
+    float k_scale, v_scale;
+    int Hkv, b, nb, t_end;
+    int64_t groups;
+    __nv_bfloat16 *K, *V;
+    int64_t ks_b, ks_h, ks_t, vs_b, vs_h, vs_t;
+};
+template <int D>
+__global__ void __launch_bounds__(256) unpack_kv4_kernel(const UnpackArgs a) {
+    constexpr int GPT = D / KV4_GROUP;                 // groups of a token
+    pdl_wait();
+    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (n >= a.groups) return;
+    // block after block (sequence or page, head, block of the sequence), K then V, token after token
+    const int b = a.b, per_block = 2 * b * GPT;
+    const int64_t blk = n / per_block;
+    int m = (int)(n - blk * per_block);
+    const bool is_v = m >= b * GPT;
+    if (is_v) m -= b * GPT;
+    const int t = m / GPT, gr = m % GPT;
+    const int j = (int)(blk % a.nb), hk = (int)(blk / a.nb % a.Hkv);
+    const int64_t i = blk / a.nb / a.Hkv, tok = (int64_t)j * b + t;
+    if (tok >= a.t_end) return;
+    const unsigned char* from = a.pool + i * a.sb + hk * a.sh + j * a.sj + (is_v ? Kv4Block(b, D).v_codes : 0);
+    const uint2 codes = __ldcg(reinterpret_cast<const uint2*>(from + t * (D / 2)) + gr);
+    const float s = f16_lo(e4m3x2_to_f16x2(__ldcg(from + b * (D / 2) + t * GPT + gr))) * (is_v ? a.v_scale : a.k_scale);
+    __nv_bfloat16* to = (is_v ? a.V + i * a.vs_b + hk * a.vs_h + tok * a.vs_t : a.K + i * a.ks_b + hk * a.ks_h + tok * a.ks_t) + gr * 16;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const uint32_t w = half ? codes.y : codes.x;
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t p = e2m1x2_to_f16x2((w >> (8 * k)) & 0xffu);
+            x[2 * k] = f16_lo(p) * s;
+            x[2 * k + 1] = f16_hi(p) * s;
+        }
+        reinterpret_cast<uint4*>(to)[half] = pack_bf16(x);
+    }
+}
+
+// ------------------------------------------------------------------ host side
+
+int validate_kv4(const eta_cache_desc* d, const eta_kv4_desc* kv4, const void* pool, bool paged) {
+    if (!kv4 || !pool) return ETA_ERR_INVALID_ARG;
+    if (!(kv4->k_scale > 0.f) || !(kv4->v_scale > 0.f) || !isfinite(kv4->k_scale) || !isfinite(kv4->v_scale)) return ETA_ERR_INVALID_ARG;
+    if (((kv4->stride_b | kv4->stride_h | (paged ? 0 : kv4->stride_j)) & 15) || (reinterpret_cast<uintptr_t>(pool) & 15))
+        return ETA_ERR_UNSUPPORTED;
+    const int64_t bytes = Kv4Block(d->block_size, d->head_dim).bytes;
+    if (kv4->stride_b < bytes || kv4->stride_h < bytes || (!paged && kv4->stride_j < bytes)) return ETA_ERR_INVALID_ARG;
+    return ETA_OK;
+}
+
+static bool misaligned(std::initializer_list<const void*> pointers, uintptr_t to) {
+    for (const void* p : pointers)
+        if (reinterpret_cast<uintptr_t>(p) & (to - 1)) return true;
+    return false;
+}
+
+// eta_append_tokens, and with `kv4` eta_append_tokens_kv4 (K is the pool then)
+static int append_tokens(const eta_cache_desc* desc, const eta_kv4_desc* kv4, const eta_tokens_desc* tok, const void* q, const void* k,
+                         const void* v, const float* q_weight, const float* k_weight, const double* inv_freq, const int32_t* positions,
+                         const int64_t* slot_map, int32_t n_pages, void* q_out, void* K, void* V, uint32_t* status, void* stream) {
+    int rc = validate_shape(desc);
+    if (rc != ETA_OK) return rc;
+    if (!tok || tok->n_rows < 0 || n_pages < 0 || tok->type < ETA_TYPE_BF16 || tok->type > ETA_TYPE_FP32) return ETA_ERR_INVALID_ARG;
+    if ((tok->flags & ~ETA_TOKENS_INTERLEAVED) || !(tok->eps >= 0.f)) return ETA_ERR_INVALID_ARG;
+    if (tok->rotary_dim < 0 || tok->rotary_dim > desc->head_dim) return ETA_ERR_INVALID_ARG;
+    if (tok->rotary_dim % 16) return ETA_ERR_UNSUPPORTED;
+    if ((rc = kv4 ? validate_kv4(desc, kv4, K, n_pages > 0) : validate_strides(desc)) != ETA_OK) return rc;
+    if (!q || !k || !v || !slot_map || !q_out || !K || !V) return ETA_ERR_INVALID_ARG;
+    if (tok->rotary_dim && (!inv_freq || !positions)) return ETA_ERR_INVALID_ARG;
+    const int64_t vec = tok->type == ETA_TYPE_FP32 ? 4 : 8;
+    for (int64_t stride : {tok->q_stride_r, tok->q_stride_h, tok->k_stride_r, tok->k_stride_h, tok->v_stride_r, tok->v_stride_h})
+        if (stride % vec) return ETA_ERR_UNSUPPORTED;
+    if (misaligned({q, k, v, q_out, K, V, q_weight, k_weight}, 16) || misaligned({slot_map, inv_freq}, 8) || misaligned({positions}, 4))
+        return ETA_ERR_UNSUPPORTED;
+    if (tok->n_rows == 0) return ETA_OK;
+
+    TokensArgs a;
+    a.q = q; a.k = k; a.v = v;
+    a.q_weight = q_weight; a.k_weight = k_weight; a.inv_freq = inv_freq; a.positions = positions; a.slot_map = slot_map;
+    a.q_out = static_cast<__nv_bfloat16*>(q_out);
+    a.K = static_cast<__nv_bfloat16*>(K); a.V = static_cast<__nv_bfloat16*>(V);
+    a.pool = static_cast<unsigned char*>(K);
+    a.status = status;
+    a.q_sr = tok->q_stride_r; a.q_sh = tok->q_stride_h; a.k_sr = tok->k_stride_r; a.k_sh = tok->k_stride_h;
+    a.v_sr = tok->v_stride_r; a.v_sh = tok->v_stride_h;
+    a.ks_b = desc->k_stride_b; a.ks_h = desc->k_stride_h; a.ks_t = desc->k_stride_t;
+    a.vs_b = desc->v_stride_b; a.vs_h = desc->v_stride_h; a.vs_t = desc->v_stride_t;
+    if (kv4) { a.ks_b = kv4->stride_b; a.ks_h = kv4->stride_h; a.ks_t = n_pages > 0 ? 0 : kv4->stride_j; }
+    a.k_scale = kv4 ? kv4->k_scale : 1; a.v_scale = kv4 ? kv4->v_scale : 1;
+    a.per_page = n_pages > 0 ? desc->block_size : desc->t_cap;
+    a.limit = (int64_t)a.per_page * (n_pages > 0 ? n_pages : desc->batch);
+    a.rows = tok->n_rows; a.Hq = desc->n_q_heads; a.Hkv = desc->n_kv_heads; a.b = desc->block_size;
+    a.rotary = tok->rotary_dim; a.interleaved = (tok->flags & ETA_TOKENS_INTERLEAVED) != 0;
+    a.eps = tok->eps;
+    // A row is one warp's work where there are rows enough to fill the GPU, and split as far as it goes where there are not.
+    const int per_warp = 32 / (desc->head_dim / 8);
+    const int items = (a.Hq + per_warp - 1) / per_warp + 2 * ((a.Hkv + per_warp - 1) / per_warp);
+    const int64_t want = ((int64_t)148 * 16 + a.rows - 1) / a.rows;
+    a.parts = (int)(want > items ? items : want);
+    const int64_t ctas = ((int64_t)a.rows * a.parts + TOK_WARPS - 1) / TOK_WARPS;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const char* what = kv4 ? "eta_append_tokens_kv4" : "eta_append_tokens";
+#define ETA_TOK(T, DD, Q4) launch_pdl(what, append_tokens_kernel<T, DD, Q4>, dim3((unsigned)ctas), dim3(32 * TOK_WARPS), 0, s, a)
+#define ETA_TOK_D(T) (desc->head_dim == 128 ? (kv4 ? ETA_TOK(T, 128, true) : ETA_TOK(T, 128, false)) : (kv4 ? ETA_TOK(T, 64, true) : ETA_TOK(T, 64, false)))
+    return tok->type == ETA_TYPE_BF16 ? ETA_TOK_D(__nv_bfloat16) : (tok->type == ETA_TYPE_FP16 ? ETA_TOK_D(__half) : ETA_TOK_D(float));
+#undef ETA_TOK_D
+#undef ETA_TOK
+}
+
+}  // namespace eta
+
+extern "C" {
+
+size_t eta_kv4_block_bytes(int32_t block_size, int32_t head_dim) {
+    if ((block_size != 32 && block_size != 64 && block_size != 128) || (head_dim != 64 && head_dim != 128)) return 0;
+    return (size_t)eta::Kv4Block(block_size, head_dim).bytes;
+}
+
+int eta_append_tokens(const eta_cache_desc* desc, const eta_tokens_desc* tokens, const void* q, const void* k, const void* v,
+                      const float* q_weight, const float* k_weight, const double* inv_freq, const int32_t* positions,
+                      const int64_t* slot_map, int32_t n_pages, void* q_out, void* K, void* V, uint32_t* status_dev, void* stream) {
+    return eta::append_tokens(desc, nullptr, tokens, q, k, v, q_weight, k_weight, inv_freq, positions, slot_map, n_pages, q_out, K, V,
+                              status_dev, stream);
+}
+
+int eta_append_tokens_kv4(const eta_cache_desc* desc, const eta_kv4_desc* kv4, const eta_tokens_desc* tokens, const void* q,
+                          const void* k, const void* v, const float* q_weight, const float* k_weight, const double* inv_freq,
+                          const int32_t* positions, const int64_t* slot_map, int32_t n_pages, void* q_out, void* pool,
+                          uint32_t* status_dev, void* stream) {
+    if (!kv4) return ETA_ERR_INVALID_ARG;
+    return eta::append_tokens(desc, kv4, tokens, q, k, v, q_weight, k_weight, inv_freq, positions, slot_map, n_pages, q_out, pool, pool,
+                              status_dev, stream);
+}
+
+int eta_unpack_kv4(const eta_cache_desc* desc, const eta_kv4_desc* kv4, const void* pool, int32_t n_pages, void* K, void* V, void* stream) {
+    using namespace eta;
+    int rc = validate_shape(desc);
+    if (rc != ETA_OK) return rc;
+    if (n_pages < 0 || !K || !V) return ETA_ERR_INVALID_ARG;
+    if ((rc = validate_kv4(desc, kv4, pool, n_pages > 0)) != ETA_OK || (rc = validate_strides(desc)) != ETA_OK) return rc;
+    if (misaligned({K, V}, 16)) return ETA_ERR_UNSUPPORTED;
+    UnpackArgs a;
+    a.pool = static_cast<const unsigned char*>(pool);
+    a.sb = kv4->stride_b; a.sh = kv4->stride_h; a.sj = n_pages > 0 ? 0 : kv4->stride_j;
+    a.k_scale = kv4->k_scale; a.v_scale = kv4->v_scale;
+    a.Hkv = desc->n_kv_heads; a.b = desc->block_size;
+    a.t_end = n_pages > 0 ? a.b : desc->t_cap;
+    a.nb = (int)(((int64_t)a.t_end + a.b - 1) / a.b);
+    a.groups = (int64_t)(n_pages > 0 ? n_pages : desc->batch) * a.Hkv * a.nb * 2 * a.b * (desc->head_dim / KV4_GROUP);
+    a.K = static_cast<__nv_bfloat16*>(K); a.V = static_cast<__nv_bfloat16*>(V);
+    a.ks_b = desc->k_stride_b; a.ks_h = desc->k_stride_h; a.ks_t = desc->k_stride_t;
+    a.vs_b = desc->v_stride_b; a.vs_h = desc->v_stride_h; a.vs_t = desc->v_stride_t;
+    const int64_t ctas = (a.groups + 255) / 256;
+    if (ctas > INT32_MAX) return ETA_ERR_UNSUPPORTED;
+    return launch_pdl("eta_unpack_kv4", desc->head_dim == 128 ? unpack_kv4_kernel<128> : unpack_kv4_kernel<64>, dim3((unsigned)ctas), dim3(256), 0,
+                      static_cast<cudaStream_t>(stream), a);
+}
+
+}  // extern "C"

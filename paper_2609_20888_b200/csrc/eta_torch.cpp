@@ -1,4 +1,4 @@
-// Marshalling of the calls of a decode step (page plan, append, predict, decode) for torch: checks the tensors, takes their device
+// Marshalling of the calls of a decode step (page plan, new tokens, append, predict, decode) for torch: checks the tensors, takes their device
 // pointers and the current stream, and calls the C ABI.  Nothing is computed or kept here.
 //
 // Through ctypes the checks and conversions of a step's 30 arguments took 20 us of Python, more than a small step takes on
@@ -11,6 +11,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <exception>
+#include <initializer_list>
 
 #include "../../include/eta.h"
 
@@ -18,7 +19,7 @@ namespace {
 
 // classes of the binding: the exception, the ctypes structures
 PyObject* g_error = nullptr;
-PyObject *g_desc = nullptr, *g_pages = nullptr, *g_decode_params = nullptr, *g_params = nullptr;
+PyObject *g_desc = nullptr, *g_pages = nullptr, *g_decode_params = nullptr, *g_params = nullptr, *g_kv4 = nullptr;
 
 bool fail(const char* name, const char* what) {
     PyErr_Format(g_error, "%s must be %s", name, what);
@@ -307,6 +308,155 @@ PyObject* plan(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return PyLong_FromLong(rc);
 }
 
+// A CUDA tensor on the current device with unit stride along its last axis and the given sizes (-1: any).
+bool shaped(PyObject* o, at::ScalarType type, const char* name, std::initializer_list<int64_t> sizes, void** out) {
+    if (o == Py_None) return fail(name, "a tensor, not None");
+    if (!pointer(o, type, name, out)) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.device().index() != c10::cuda::current_device()) return fail(name, "on the current CUDA device");
+    bool ok = t.dim() == (int64_t)sizes.size() && t.stride(-1) == 1;
+    int64_t k = 0;
+    for (int64_t n : sizes) {
+        ok = ok && (n < 0 || t.size(k) == n);
+        ++k;
+    }
+    return ok || fail(name, "of the shape that the call's descriptors say, with unit stride along its last axis");
+}
+// the stride of an axis, 0 where it has one element and torch may say anything
+int64_t stride_of(const at::Tensor& t, int64_t axis) { return t.size(axis) > 1 ? t.stride(axis) : 0; }
+
+// K or V as the descriptor has it: contiguous [batch, n_kv_heads, t_cap, head_dim], paged [n_pages, n_kv_heads, block_size, head_dim]
+bool cache_tensor(PyObject* o, const char* name, const eta_cache_desc* d, bool paged, void** out) {
+    return shaped(o, at::kBFloat16, name, {paged ? -1 : d->batch, d->n_kv_heads, paged ? d->block_size : d->t_cap, d->head_dim}, out);
+}
+bool same_strides(PyObject* o, const char* name, std::initializer_list<int64_t> strides) {
+    const at::Tensor& t = THPVariable_Unpack(o);
+    int64_t k = 0;
+    for (int64_t s : strides) {
+        if (t.size(k) > 1 && t.stride(k) != s) return fail(name, "the tensor that its descriptor was made for (other strides)");
+        ++k;
+    }
+    return true;
+}
+// the pool of a 4-bit cache: [n_pages, n_kv_heads, bytes] (paged) or [batch, n_kv_heads, blocks, bytes]; *n_pages: 0 where not paged
+bool pool_tensor(PyObject* o, const eta_cache_desc* d, const eta_kv4_desc* q4, void** out, int32_t* n_pages) {
+    if (!pointer(o, at::kByte, "pool", out)) return false;
+    if (o == Py_None) return fail("pool", "a tensor, not None");
+    const at::Tensor& t = THPVariable_Unpack(o);
+    const int64_t bytes = 2 * (int64_t)d->block_size * (d->head_dim / 2 + d->head_dim / 16);
+    const bool paged = t.dim() == 3;
+    *n_pages = 0;
+    if (paged) {
+        if (!shaped(o, at::kByte, "pool", {-1, d->n_kv_heads, bytes}, out) || !same_strides(o, "pool", {q4->stride_b, q4->stride_h})) return false;
+        if (t.size(0) > INT32_MAX || t.size(0) < 1) return fail("pool", "of 1 to 2^31 - 1 pages");
+        *n_pages = (int32_t)t.size(0);
+        return true;
+    }
+    if (!shaped(o, at::kByte, "pool", {d->batch, d->n_kv_heads, -1, bytes}, out) ||
+        !same_strides(o, "pool", {q4->stride_b, q4->stride_h, q4->stride_j}))
+        return false;
+    return t.size(2) * (int64_t)d->block_size >= d->t_cap || fail("pool", "large enough for t_cap tokens");
+}
+
+// (address, desc, kv4 or None, q, k, v, q_weight, k_weight, inv_freq, positions, slot_map, paged, q_out, K or pool, V or None, status, eps,
+//  flags) -> return code
+PyObject* tokens(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    using Plain = int (*)(const eta_cache_desc*, const eta_tokens_desc*, const void*, const void*, const void*, const float*, const float*,
+                          const double*, const int32_t*, const int64_t*, int32_t, void*, void*, void*, uint32_t*, void*);
+    using Kv4 = int (*)(const eta_cache_desc*, const eta_kv4_desc*, const eta_tokens_desc*, const void*, const void*, const void*, const float*,
+                        const float*, const double*, const int32_t*, const int64_t*, int32_t, void*, void*, uint32_t*, void*);
+    void *fn, *q, *k, *x, *q_out, *K, *V = nullptr;
+    Struct<eta_cache_desc> ds;
+    Struct<eta_kv4_desc> qs;
+    if (!count(n, 18) || !entry(v[0], &fn)) return nullptr;
+    const eta_cache_desc* desc = ds.get(v[1], g_desc);
+    if (!desc) return nullptr;
+    const eta_kv4_desc* q4 = nullptr;
+    if (v[2] != Py_None && !(q4 = qs.get(v[2], g_kv4))) return nullptr;
+    if (!THPVariable_Check(v[3])) { PyErr_SetString(PyExc_TypeError, "q must be a torch.Tensor"); return nullptr; }
+    const at::ScalarType type = THPVariable_Unpack(v[3]).scalar_type();
+    if (type != at::kBFloat16 && type != at::kHalf && type != at::kFloat) return fail("q", "bfloat16, float16 or float32"), nullptr;
+    if (!shaped(v[3], type, "q", {-1, desc->n_q_heads, desc->head_dim}, &q)) return nullptr;
+    const at::Tensor& tq = THPVariable_Unpack(v[3]);
+    const int64_t rows = tq.size(0);
+    if (rows > INT32_MAX) return fail("q", "of fewer than 2^31 rows"), nullptr;
+    if (!shaped(v[4], type, "k", {rows, desc->n_kv_heads, desc->head_dim}, &k) || !shaped(v[5], type, "v", {rows, desc->n_kv_heads, desc->head_dim}, &x))
+        return nullptr;
+    const at::Tensor &tk = THPVariable_Unpack(v[4]), &tv = THPVariable_Unpack(v[5]);
+    float *q_weight, *k_weight;
+    double* inv_freq;
+    int32_t *positions, n_pages = 0;
+    int64_t* slot_map;
+    uint32_t* status;
+    if (!OPT(v[6], at::kFloat, q_weight, desc->head_dim) || !OPT(v[7], at::kFloat, k_weight, desc->head_dim) || !OPT(v[8], at::kDouble, inv_freq, -1) ||
+        !OPT(v[9], at::kInt, positions, rows) || !VEC(v[10], at::kLong, slot_map, rows) ||
+        !VEC(v[12], at::kBFloat16, q_out, rows * desc->n_q_heads * desc->head_dim) || !OPT(v[15], at::kInt, status, 1))
+        return nullptr;
+    if (q4) {
+        if (!pool_tensor(v[13], desc, q4, &K, &n_pages)) return nullptr;
+    } else {
+        const int paged = PyObject_IsTrue(v[11]);
+        if (paged < 0) return nullptr;
+        if (!cache_tensor(v[13], "K", desc, paged != 0, &K) || !same_strides(v[13], "K", {desc->k_stride_b, desc->k_stride_h, desc->k_stride_t}) ||
+            !cache_tensor(v[14], "V", desc, paged != 0, &V) || !same_strides(v[14], "V", {desc->v_stride_b, desc->v_stride_h, desc->v_stride_t}))
+            return nullptr;
+        if (paged) {
+            const int64_t pk = THPVariable_Unpack(v[13]).size(0);
+            if (pk != THPVariable_Unpack(v[14]).size(0) || pk < 1 || pk > INT32_MAX) return fail("K and V", "pools of the same number of pages"), nullptr;
+            n_pages = (int32_t)pk;
+        }
+    }
+    eta_tokens_desc t;
+    t.n_rows = (int32_t)rows;
+    t.type = type == at::kBFloat16 ? ETA_TYPE_BF16 : (type == at::kHalf ? ETA_TYPE_FP16 : ETA_TYPE_FP32);
+    const int64_t half = v[8] == Py_None ? 0 : THPVariable_Unpack(v[8]).numel();
+    if (2 * half > desc->head_dim) return fail("inv_freq", "of at most head_dim / 2 elements"), nullptr;
+    t.rotary_dim = (int32_t)(2 * half);
+    t.q_stride_r = stride_of(tq, 0); t.q_stride_h = stride_of(tq, 1);
+    t.k_stride_r = stride_of(tk, 0); t.k_stride_h = stride_of(tk, 1);
+    t.v_stride_r = stride_of(tv, 0); t.v_stride_h = stride_of(tv, 1);
+    t.eps = (float)PyFloat_AsDouble(v[16]);
+    t.flags = (uint32_t)PyLong_AsUnsignedLongMask(v[17]);
+    if (PyErr_Occurred()) return nullptr;
+    if (rows == 0) return PyLong_FromLong(ETA_OK);           // empty tensors have no address
+    void* const s = stream();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    if (q4)
+        rc = reinterpret_cast<Kv4>(fn)(desc, q4, &t, q, k, x, q_weight, k_weight, inv_freq, positions, slot_map, n_pages, q_out, K, status, s);
+    else
+        rc = reinterpret_cast<Plain>(fn)(desc, &t, q, k, x, q_weight, k_weight, inv_freq, positions, slot_map, n_pages, q_out, K, V, status, s);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+// (address, desc, kv4, pool, K, V) -> return code; K and V of any strides
+PyObject* unpack(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    using F = int (*)(const eta_cache_desc*, const eta_kv4_desc*, const void*, int32_t, void*, void*, void*);
+    F fn;
+    void *pool, *K, *V;
+    int32_t n_pages;
+    Struct<eta_cache_desc> ds;
+    Struct<eta_kv4_desc> qs;
+    if (!count(n, 6) || !entry(v[0], &fn)) return nullptr;
+    const eta_cache_desc* from = ds.get(v[1], g_desc);
+    if (!from) return nullptr;
+    const eta_kv4_desc* q4 = qs.get(v[2], g_kv4);
+    if (!q4 || !pool_tensor(v[3], from, q4, &pool, &n_pages)) return nullptr;
+    if (!cache_tensor(v[4], "K", from, n_pages > 0, &K) || !cache_tensor(v[5], "V", from, n_pages > 0, &V)) return nullptr;
+    const at::Tensor &k = THPVariable_Unpack(v[4]), &x = THPVariable_Unpack(v[5]);
+    if (n_pages && (k.size(0) != n_pages || x.size(0) != n_pages)) return fail("K and V", "of as many pages as the pool"), nullptr;
+    eta_cache_desc d = *from;
+    d.k_stride_b = stride_of(k, 0); d.k_stride_h = stride_of(k, 1); d.k_stride_t = k.size(2) > 1 ? k.stride(2) : d.head_dim;
+    d.v_stride_b = stride_of(x, 0); d.v_stride_h = stride_of(x, 1); d.v_stride_t = x.size(2) > 1 ? x.stride(2) : d.head_dim;
+    void* const s = stream();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn(&d, q4, pool, n_pages, K, V, s);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
 // the eta_params a call would get, as bytes (for the tests)
 PyObject* params(PyObject*, PyObject* const* v, Py_ssize_t n) {
     eta_params p;
@@ -314,11 +464,11 @@ PyObject* params(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return PyBytes_FromStringAndSize(reinterpret_cast<const char*>(&p), sizeof p);
 }
 
-// (EtaError, CacheDesc, PageTable, DecodeParams, Params)
+// (EtaError, CacheDesc, PageTable, DecodeParams, Params, Kv4Desc)
 PyObject* set_classes(PyObject*, PyObject* const* v, Py_ssize_t n) {
-    if (!count(n, 5)) return nullptr;
-    PyObject** const to[5] = {&g_error, &g_desc, &g_pages, &g_decode_params, &g_params};
-    for (int k = 0; k < 5; ++k) {
+    if (!count(n, 6)) return nullptr;
+    PyObject** const to[6] = {&g_error, &g_desc, &g_pages, &g_decode_params, &g_params, &g_kv4};
+    for (int k = 0; k < 6; ++k) {
         Py_INCREF(v[k]);
         Py_XSETREF(*to[k], v[k]);
     }
@@ -343,6 +493,8 @@ PyMethodDef methods[] = {
     {"decode", (PyCFunction)(void (*)(void))guarded<decode<Decode::PLAIN>>, METH_FASTCALL, nullptr},
     {"decode_paged", (PyCFunction)(void (*)(void))guarded<decode<Decode::PAGED>>, METH_FASTCALL, nullptr},
     {"decode_static", (PyCFunction)(void (*)(void))guarded<decode<Decode::STATIC>>, METH_FASTCALL, nullptr},
+    {"tokens", (PyCFunction)(void (*)(void))guarded<tokens>, METH_FASTCALL, nullptr},
+    {"unpack", (PyCFunction)(void (*)(void))guarded<unpack>, METH_FASTCALL, nullptr},
     {"plan", (PyCFunction)(void (*)(void))guarded<plan>, METH_FASTCALL, nullptr},
     {"params", (PyCFunction)(void (*)(void))guarded<params>, METH_FASTCALL, nullptr},
     {"set_classes", (PyCFunction)(void (*)(void))set_classes, METH_FASTCALL, nullptr},
