@@ -415,6 +415,32 @@ int eta_append_tokens_kv4(const eta_cache_desc* desc, const eta_kv4_desc* kv4, c
 int eta_unpack_kv4(const eta_cache_desc* desc, const eta_kv4_desc* kv4, const void* pool, int32_t n_pages, void* K, void* V,
                    void* stream);
 
+/*
+ * The block index of a 4-bit cache: what eta_build_block_summaries and eta_append_summary (or, with `pages` not NULL, their paged
+ * forms) write for the keys as the cache holds them, code * scale * k_scale.  Same records, flags and rules about lengths; sums of the
+ * codes' exact values in fp32, sigma from the plain moments (exact or nearly so: a key's coordinate has six significant bits), so
+ * sigma is exactly 0 for identical keys.  A NaN key makes its coordinates' records and the norm NaN, and the block is always admitted.
+ * Append writes the bytes that the build would.  Both are launched with programmatic dependent launch and wait for
+ * everything before them before they read or write; the append releases its successors then, the build as it ends.
+ */
+int eta_build_block_summaries_kv4(const eta_cache_desc* desc, const eta_kv4_desc* kv4, const eta_page_table* pages, const void* pool,
+                                  const int32_t* seq_lens, void* musig, float* mnorm, uint32_t flags, void* stream);
+int eta_append_summary_kv4(const eta_cache_desc* desc, const eta_kv4_desc* kv4, const eta_page_table* pages, const void* pool,
+                           const int32_t* seq_lens_after, void* musig, float* mnorm, uint32_t flags, void* stream);
+
+/*
+ * eta_decode over a 4-bit cache, contiguous or, with `pages` not NULL, paged: the same screening, rescue, gate, masks, tail, statistics
+ * and status, on the keys and values as the cache holds them.  musig and mnorm come from the calls above.  A code times its scale is
+ * exact in fp16, products are exact and sums fp32; probabilities are held to 22 bits for the second product.  Always the general path
+ * (three kernels, four with a long rescue window).  A NaN in a block reaches the heads that attend the block and no others.
+ * Launch order, determinism, errors: as eta_decode.  workspace: eta_kv4_workspace_bytes() bytes, 256-byte aligned.
+ */
+int eta_kv4_workspace_bytes(const eta_cache_desc* desc, size_t* out_bytes);
+int eta_decode_kv4(const eta_cache_desc* desc, const eta_kv4_desc* kv4, const eta_page_table* pages, const eta_params* params, const void* q,
+                   const void* pool, const int32_t* seq_lens, const void* musig, const float* mnorm, const float* tau,
+                   const float* head_const, float* out, uint8_t* sel_mask, int32_t* stats, uint32_t* status_dev, void* workspace,
+                   size_t workspace_bytes, void* stream);
+
 /* Size of the built-in scratch of eta_decode_static, in bytes. */
 size_t eta_static_scratch_bytes(void);
 

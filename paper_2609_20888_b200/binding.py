@@ -31,7 +31,8 @@ EXPORTS = ("eta_workspace_bytes", "eta_build_block_summaries", "eta_append_summa
            "eta_append_summary_paged", "eta_decode_paged", "eta_stage_query", "eta_predict_threshold",
            "eta_score_dual", "eta_calibration_workspace_bytes", "eta_calibrate_head_const", "eta_decode", "eta_decode_static", "eta_static_scratch_bytes", "eta_decode_kernel_count", "eta_decode_launches", "eta_profile_enable", "eta_profile_read",
            "eta_profile_kernel_name", "eta_set_pdl", "eta_strerror", "eta_last_cuda_error", "eta_plan_pages",
-           "eta_append_tokens", "eta_append_tokens_kv4", "eta_kv4_block_bytes", "eta_unpack_kv4")
+           "eta_append_tokens", "eta_append_tokens_kv4", "eta_kv4_block_bytes", "eta_unpack_kv4",
+           "eta_build_block_summaries_kv4", "eta_append_summary_kv4", "eta_decode_kv4", "eta_kv4_workspace_bytes")
 
 
 class CacheDesc(ctypes.Structure):
@@ -69,7 +70,8 @@ class EtaError(RuntimeError):
 _lib = None
 _native = None          # the compiled marshalling module, or what stands for it where it is missing
 _STEP_CALLS = ("eta_append_summary", "eta_append_summary_paged", "eta_predict_threshold", "eta_decode", "eta_decode_paged",
-               "eta_decode_static", "eta_plan_pages", "eta_append_tokens", "eta_append_tokens_kv4", "eta_unpack_kv4")
+               "eta_decode_static", "eta_plan_pages", "eta_append_tokens", "eta_append_tokens_kv4", "eta_unpack_kv4",
+               "eta_build_block_summaries_kv4", "eta_append_summary_kv4", "eta_decode_kv4")
 
 
 class _Missing:
@@ -128,6 +130,10 @@ def load(path: str | None = None) -> ctypes.CDLL:
         lib.eta_append_tokens.argtypes = [D, TD, vp, vp, vp, f32p, f32p, vp, i32p, vp, i32, vp, vp, vp, vp, vp]
         lib.eta_append_tokens_kv4.argtypes = [D, Q4, TD, vp, vp, vp, f32p, f32p, vp, i32p, vp, i32, vp, vp, vp, vp]
         lib.eta_unpack_kv4.argtypes = [D, Q4, vp, i32, vp, vp, vp]
+        lib.eta_build_block_summaries_kv4.argtypes = [D, Q4, PT, vp, i32p, vp, f32p, ctypes.c_uint32, vp]
+        lib.eta_append_summary_kv4.argtypes = [D, Q4, PT, vp, i32p, vp, f32p, ctypes.c_uint32, vp]
+        lib.eta_decode_kv4.argtypes = [D, Q4, PT, P, vp, vp, i32p, vp, f32p, f32p, f32p, f32p, vp, i32p, vp, vp, ctypes.c_size_t, vp]
+        lib.eta_kv4_workspace_bytes.argtypes = [D, ctypes.POINTER(ctypes.c_size_t)]
         lib.eta_kv4_block_bytes.argtypes = [i32, i32]
         lib.eta_kv4_block_bytes.restype = ctypes.c_size_t
         lib.eta_decode_static.argtypes = [D, P, vp, vp, vp, i32p, vp, f32p, f32p, f32p, f32p, vp, i32p, vp, vp]
@@ -421,6 +427,40 @@ def eta_unpack_kv4(desc: CacheDesc, kv4: Kv4Desc, pool, K, V) -> None:
     rc = _native.unpack(lib.addresses["eta_unpack_kv4"], desc, kv4, pool, K, V)
     if rc:
         _check(rc, "eta_unpack_kv4")
+
+
+def eta_build_block_summaries_kv4(desc: CacheDesc, kv4: Kv4Desc, pool, seq_lens, musig, mnorm, flags: int = 0,
+                                  pages: PageTable | None = None) -> None:
+    """The block index of a 4-bit cache, of all full blocks; paged with a page table."""
+    lib = _lib or load()
+    rc = _native.index_kv4(lib.addresses["eta_build_block_summaries_kv4"], desc, kv4, pages, pool, seq_lens, musig, mnorm, flags)
+    if rc:
+        _check(rc, "eta_build_block_summaries_kv4")
+
+
+def eta_append_summary_kv4(desc: CacheDesc, kv4: Kv4Desc, pool, seq_lens_after, musig, mnorm, flags: int = 0,
+                           pages: PageTable | None = None) -> None:
+    """The same, of the blocks that the newest tokens completed."""
+    lib = _lib or load()
+    rc = _native.index_kv4(lib.addresses["eta_append_summary_kv4"], desc, kv4, pages, pool, seq_lens_after, musig, mnorm, flags)
+    if rc:
+        _check(rc, "eta_append_summary_kv4")
+
+
+def eta_kv4_workspace_bytes(desc: CacheDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().eta_kv4_workspace_bytes(ctypes.byref(desc), ctypes.byref(n)), "eta_kv4_workspace_bytes")
+    return n.value
+
+
+def eta_decode_kv4(desc: CacheDesc, kv4: Kv4Desc, params: DecodeParams, q, pool, seq_lens, musig, mnorm, tau, head_const, out, sel_mask,
+                   workspace, stats=None, status=None, pages: PageTable | None = None) -> None:
+    """eta_decode over a 4-bit cache; paged with a page table.  musig and mnorm may be None with ETA_FLAG_DENSE."""
+    lib = _lib or load()
+    rc = _native.decode_kv4(lib.addresses["eta_decode_kv4"], desc, kv4, pages, params, q, pool, seq_lens, musig, mnorm, tau, head_const, out,
+                            sel_mask, stats, status, workspace)
+    if rc:
+        _check(rc, "eta_decode_kv4")
 
 
 def eta_static_scratch_bytes() -> int:

@@ -31,6 +31,7 @@
 #include <cuda.h>
 
 #include "eta_attend.cuh"
+#include "eta_attend_kv4.cuh"
 #include "eta_step.h"
 #include "eta_timeline.h"
 
@@ -55,6 +56,9 @@ struct DecodeArgs {
     const int32_t* block_table;   // paged cache: [batch, table_stride] page of every block of tokens; null: contiguous
     int table_stride;
     int read_once;       // K and V leave the L2 first
+    const unsigned char* pool;    // 4-bit cache: its blocks, strides in bytes (sequence or page, KV head, block of a sequence)
+    int64_t sb, sh, sj;
+    float out_scale;     // 4-bit cache: what its V is scaled by
     FastDiv div_gpr, div_hkv, div_grid;
     unsigned long long* timeline;
 };
@@ -77,11 +81,27 @@ __device__ __forceinline__ int granule_sum(const uint4& v) {
     return (int)__dp4a(v.x, 0x01010101u, __dp4a(v.y, 0x01010101u, __dp4a(v.z, 0x01010101u, __dp4a(v.w, 0x01010101u, 0u))));
 }
 
-template <int D, int TS, int NSTAGE, int NGROUPS>
-struct DecodeSmem {
+// What a stage of the ring holds and who computes on it: a tile of TS tokens of a bf16 cache ...
+template <int D, int TS_>
+struct Bf16Tile {
+    static constexpr int TS = TS_;
+    static constexpr bool KV4 = false;
     static constexpr int HALVES = D / 64;
     static constexpr int TILE_BYTES = TS * 128;                 // one 64-column half tile
     static constexpr int STAGE_BYTES = 2 * HALVES * TILE_BYTES; // K halves then V halves
+    using Math = Attend<D, TS>;
+};
+// ... or a block of a 4-bit one
+template <int D, int TS_, bool WIDE>
+struct Kv4Tile {
+    static constexpr int TS = TS_;
+    static constexpr bool KV4 = true;
+    static constexpr int STAGE_BYTES = Kv4Block(TS, D).bytes;
+    using Math = AttendKv4<D, TS, WIDE>;
+};
+
+template <int D, int STAGE_BYTES, int NSTAGE, int NGROUPS>
+struct DecodeSmem {
     static constexpr int BAR_OFF = NSTAGE * STAGE_BYTES;        // full[NSTAGE], empty[NSTAGE], flush[NGROUPS], layout
     static constexpr int DESC_OFF = (BAR_OFF + 8 * (2 * NSTAGE + NGROUPS + 1) + 15) / 16 * 16;
     static constexpr int WIN_OFF = DESC_OFF + 16 * NSTAGE;      // uint4 [32]: the producer's window of granules
@@ -101,11 +121,11 @@ struct DecodeSmem {
 // consumes the stage fills k, k + NGROUPS, ...; with two or three groups every scheduler holds several warps in
 // different phases of a tile, which hides the fixed latencies of the MMA / shuffle / exp chains.  Each group
 // keeps its own running (m, l, O) and writes its own partial per (CTA, row) piece.
-template <int D, int TS, int NSTAGE, int NGROUPS>
+template <int D, typename Tile, int NSTAGE, int NGROUPS>
 __global__ void __launch_bounds__(32 * (WARPS_PER_GROUP * NGROUPS + 1), 1)
 decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const DecodeArgs a) {
-    using L = DecodeSmem<D, TS, NSTAGE, NGROUPS>;
-    constexpr int HALVES = L::HALVES;
+    constexpr int TS = Tile::TS, STAGE_BYTES = Tile::STAGE_BYTES;
+    using L = DecodeSmem<D, STAGE_BYTES, NSTAGE, NGROUPS>;
     constexpr int PRODUCER_WARP = WARPS_PER_GROUP * NGROUPS;
 
     extern __shared__ unsigned char smem_raw[];
@@ -129,8 +149,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         for (int k = 0; k < NGROUPS; ++k) mbar_init(&flushbar[k], 32 * WARPS_PER_GROUP);
         mbar_init(laybar, 1);
         fence_barrier_init();
-        prefetch_tmap(&tmK);
-        prefetch_tmap(&tmV);
+        if constexpr (!Tile::KV4) { prefetch_tmap(&tmK); prefetch_tmap(&tmV); }
     }
     // what is known before the predecessor kernel is through: which rows have tokens and which a tail (a caller input)
     constexpr int NWARPS = WARPS_PER_GROUP * NGROUPS + 1;
@@ -567,7 +586,9 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             // cache: token offset in the page)
             const int my_y = a.block_table ? usub * TS : (c_ent & 0xffffff) * a.b + usub * TS;
             const int my_w = a.block_table ? c_page : my_i;
-            unsigned char* const my_smem = smem + stage * L::STAGE_BYTES;
+            unsigned char* const my_smem = smem + stage * STAGE_BYTES;
+            const unsigned char* const my_block = !Tile::KV4 ? nullptr
+                : a.pool + my_hk * a.sh + (a.block_table ? c_page * a.sb : my_i * a.sb + (c_ent & 0xffffff) * a.sj);
             const int nvalid = min(TS, nrows - usub * TS);
             // bits 8..15: row of the tile whose token stays ungated, 0xff: none
             const int urow = ((c_nrows >> 16) != 0 && (usub + 1) * TS >= nrows) ? nvalid - 1 : 0xff;
@@ -583,14 +604,18 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
                 if (ready) {
                     done = true;
                     desc[stage] = my_desc;
-                    mbar_arrive_expect_tx(&full[stage], L::STAGE_BYTES);
+                    mbar_arrive_expect_tx(&full[stage], STAGE_BYTES);
                 }
-                // one copy per tensor: 64 columns x TS tokens x HALVES half tiles, each half swizzled.  Tile after tile, so that
-                // the first is complete as early as can be.
+                // one copy per tensor: 64 columns x TS tokens x HALVES half tiles, each half swizzled; of a 4-bit block one copy of
+                // its bytes.  Tile after tile, so that the first is complete as early as can be.
                 for (unsigned rm = __ballot_sync(0xffffffffu, ready); rm; rm &= rm - 1) {
                     if (lane == __ffs(rm) - 1) {
-                        tma_load_5d(my_smem, &tmK, 0, my_y, 0, my_hk, my_w, &full[stage], once);
-                        tma_load_5d(my_smem + HALVES * L::TILE_BYTES, &tmV, 0, my_y, 0, my_hk, my_w, &full[stage], once);
+                        if constexpr (Tile::KV4) {
+                            tma_load_1d_hint(my_smem, my_block, STAGE_BYTES, &full[stage], once);
+                        } else {
+                            tma_load_5d(my_smem, &tmK, 0, my_y, 0, my_hk, my_w, &full[stage], once);
+                            tma_load_5d(my_smem + Tile::HALVES * Tile::TILE_BYTES, &tmV, 0, my_y, 0, my_hk, my_w, &full[stage], once);
+                        }
                     }
                 }
                 return __any_sync(0xffffffffu, !done) != 0;
@@ -659,7 +684,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
     float* sm_o = reinterpret_cast<float*>(smem + L::MO_OFF) + group * WARPS_PER_GROUP * fheads * D;
     const int gtid = tid - group * 32 * WARPS_PER_GROUP;    // thread index inside the group
     const float LOG2E = 1.4426950408889634f;
-    Attend<D, TS> at(lane, wq, a.G);
+    typename Tile::Math at(lane, wq, a.G);
     int row = -1, piece = -1, q_row = -1;
     uint32_t flush_phase = 0;
     bool ok = true;
@@ -668,9 +693,9 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
     auto load_q = [&](int r) {
         int i, hk;
         a.div_hkv.divmod(r, i, hk);
-        const int h = hk * a.G + (at.head ? at.g : 0);
-        at.load_q(a.q + ((int64_t)i * a.Hq + h) * D);
-        at.te = at.head ? __ldcg(a.tau_eff + (int64_t)i * a.Hq + h) : 0.f;
+        const int64_t h = (int64_t)i * a.Hq + hk * a.G;
+        at.load_q(a.q + (h + (at.head ? at.qh : 0)) * D);
+        at.load_te(a.tau_eff + h);
         q_row = r;
     };
     if (!mbar_wait(laybar, 0)) {
@@ -697,22 +722,10 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         if (!end && new_piece != piece && ds.x != q_row) load_q(ds.x);
         if ((end || new_piece != piece) && piece >= 0) {
             // ---- this group's part of a piece is complete: combine its four warps and store (m, l, O) per head
-            float lsum = at.l_run + __shfl_xor_sync(0xffffffffu, at.l_run, 1);
-            lsum += __shfl_xor_sync(0xffffffffu, lsum, 2);
-            if (at.t == 0) { sm_m[wq * 8 + at.g] = at.m_run; sm_l[wq * 8 + at.g] = lsum; }
+            at.store_ml(sm_m + wq * 8, sm_l + wq * 8);
             const int64_t slot = ((int64_t)blockIdx.x + row) * NGROUPS + group;
             for (int h0 = 0; h0 < a.G && ok; h0 += fheads) {
-                const int ha = 2 * at.t - h0, hb = ha + 1;         // this lane's two heads within the round
-#pragma unroll
-                for (int hf = 0; hf < HALVES; ++hf)
-#pragma unroll
-                    for (int mt = 0; mt < 4; ++mt) {
-                        const int dcol = 64 * hf + 8 * at.vchunk + 2 * mt;
-                        if (ha >= 0 && ha < fheads)
-                            *reinterpret_cast<float2*>(sm_o + ((wq * fheads + ha) * D + dcol)) = make_float2(at.o[hf][mt][0], at.o[hf][mt][2]);
-                        if (hb >= 0 && hb < fheads)
-                            *reinterpret_cast<float2*>(sm_o + ((wq * fheads + hb) * D + dcol)) = make_float2(at.o[hf][mt][1], at.o[hf][mt][3]);
-                    }
+                at.store_o(sm_o + wq * fheads * D, h0, fheads);
 #ifdef ETA_TEST_SKIP_FLUSH_ARRIVE
                 // test build only: one warp of the first CTA never arrives, so that the group's bounded wait runs out and
                 // the give-up path (status flag, orderly exit of the whole CTA) executes
@@ -738,6 +751,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
                             lacc = fmaf(sm_l[w * 8 + hh], sc, lacc);
                         }
                     }
+                    if constexpr (Tile::KV4) { acc.x *= a.out_scale; acc.y *= a.out_scale; acc.z *= a.out_scale; acc.w *= a.out_scale; }
                     *reinterpret_cast<float4*>(a.part_o + (slot * a.G + hh) * D + 4 * dq) = acc;
                     if (dq == 0) a.part_ml[slot * a.G + hh] = make_float2(M, lacc);
                 }
@@ -753,7 +767,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         }
 
         const int hmask = ds.z & 0xff, urow = (ds.z >> 8) & 0xff, nvalid = ds.w;
-        const uint32_t kbase = smem_u32(smem + stage * L::STAGE_BYTES);
+        const uint32_t kbase = smem_u32(smem + stage * STAGE_BYTES);
 
         if (new_piece != piece) {
             piece = new_piece;
@@ -948,12 +962,23 @@ static int make_tmap(CUtensorMap* tm, const void* base, const eta_cache_desc* d,
     return encode_tiles(tm, base, 5, dims, strides, box);
 }
 
-template <int D, int TS, int NSTAGE, int NGROUPS>
+template <int D, typename Tile, int NSTAGE>
 static int launch_decode_t(const CUtensorMap& tmK, const CUtensorMap& tmV, const DecodeArgs& a, int n_ctas,
                            cudaStream_t s) {
-    const size_t smem = DecodeSmem<D, TS, NSTAGE, NGROUPS>::bytes(a.G);
-    return launch_pdl("decode launch", decode_kernel<D, TS, NSTAGE, NGROUPS>, dim3(n_ctas),
-                      dim3(32 * (WARPS_PER_GROUP * NGROUPS + 1)), smem, s, tmK, tmV, a);
+    const size_t smem = DecodeSmem<D, Tile::STAGE_BYTES, NSTAGE, DECODE_GROUPS>::bytes(a.G);
+    return launch_pdl("decode launch", decode_kernel<D, Tile, NSTAGE, DECODE_GROUPS>, dim3(n_ctas),
+                      dim3(32 * (WARPS_PER_GROUP * DECODE_GROUPS + 1)), smem, s, tmK, tmV, a);
+}
+
+// A 4-bit cache: a block is a stage.
+template <int D>
+static int launch_decode_kv4(const DecodeArgs& a, int n_ctas, cudaStream_t s) {
+    const CUtensorMap none = {};
+#define ETA_KV4(TS, N) (a.G > 4 ? launch_decode_t<D, Kv4Tile<D, TS, true>, N>(none, none, a, n_ctas, s) \
+                                : launch_decode_t<D, Kv4Tile<D, TS, false>, N>(none, none, a, n_ctas, s))
+    constexpr int F = D == 128 ? 1 : 2;              // 166 KB of stages
+    return a.b == 32 ? ETA_KV4(32, 36) : (a.b == 64 ? ETA_KV4(64, 18 * F) : ETA_KV4(128, 9 * F));
+#undef ETA_KV4
 }
 
 // Streaming multiprocessors of the current device; negative: an eta_status
@@ -976,14 +1001,15 @@ static int step_ctas(const eta_cache_desc* desc, const eta_params* params) {
                         desc->n_q_heads / desc->n_kv_heads, (params->flags & ETA_FLAG_PACKED_SIGMA) != 0);
 }
 
-// eta_decode and eta_decode_paged: `pages` null selects the contiguous cache
-static int decode_impl(const eta_cache_desc* desc, const eta_page_table* pages, const eta_params* params, const void* q,
-                       const void* K, const void* V, const int32_t* seq_lens, const void* musig, const float* mnorm,
+// eta_decode and its forms: `pages` null selects the contiguous cache, `kv4` null the bf16 one (else K and V are the pool)
+static int decode_impl(const eta_cache_desc* desc, const eta_kv4_desc* kv4, const eta_page_table* pages, const eta_params* params,
+                       const void* q, const void* K, const void* V, const int32_t* seq_lens, const void* musig, const float* mnorm,
                        const float* tau, const float* head_const, float* out, uint8_t* sel_mask, int32_t* stats,
                        uint32_t* status_dev, void* workspace, size_t workspace_bytes, void* stream) {
-    int rc = validate_desc(desc);
+    int rc = kv4 ? validate_index(desc) : validate_desc(desc);
     if (rc != ETA_OK) return rc;
     if (pages && (rc = validate_pages(desc, pages)) != ETA_OK) return rc;
+    if (kv4 && (rc = validate_kv4(desc, kv4, K, pages != nullptr)) != ETA_OK) return rc;
     if (!params || !q || !K || !V || !seq_lens || !out || !sel_mask) return ETA_ERR_INVALID_ARG;
     const bool dense = (params->flags & ETA_FLAG_DENSE) != 0;
     if (!dense && (!musig || !mnorm)) return ETA_ERR_INVALID_ARG;
@@ -1032,14 +1058,16 @@ static int decode_impl(const eta_cache_desc* desc, const eta_page_table* pages, 
     sa.timeline = debug_timeline();
 #endif
     sa.status = status_dev;
-    CUtensorMap tmK, tmV;
+    CUtensorMap tmK = {}, tmV = {};
     const int n_pages = pages ? pages->n_pages : 0;
-    rc = make_tmap(&tmK, K, desc, desc->k_stride_b, desc->k_stride_h, desc->k_stride_t, TS, n_pages);
-    if (rc != ETA_OK) return rc;
-    rc = make_tmap(&tmV, V, desc, desc->v_stride_b, desc->v_stride_h, desc->v_stride_t, TS, n_pages);
-    if (rc != ETA_OK) return rc;
+    if (!kv4) {
+        rc = make_tmap(&tmK, K, desc, desc->k_stride_b, desc->k_stride_h, desc->k_stride_t, TS, n_pages);
+        if (rc != ETA_OK) return rc;
+        rc = make_tmap(&tmV, V, desc, desc->v_stride_b, desc->v_stride_h, desc->v_stride_t, TS, n_pages);
+        if (rc != ETA_OK) return rc;
+    }
 
-    if (const int ctas = step_ctas(desc, params)) {
+    if (const int ctas = kv4 ? 0 : step_ctas(desc, params)) {
         StepArgs st;
         st.q = sa.q; st.musig = sa.musig; st.mnorm = mnorm; st.seq_lens = seq_lens; st.tau = tau; st.head_const = head_const;
         st.z = params->z; st.a = params->a; st.scale = scale; st.beta = params->beta;
@@ -1069,10 +1097,10 @@ static int decode_impl(const eta_cache_desc* desc, const eta_page_table* pages, 
     // where most gain, it is not sharp.  It goes by the capacity, which the host knows; of a cache of 128K x 4 that holds little,
     // a step takes without and with both, 4K x 4 21.3, 21.4; 16K x 4 26.2, 27.1; 32K x 4 34.9, 32.7.  Lengths added up on the device
     // win the second and cost 0.5 to 2 us on the large steps, 8 where 183 MB are held in 419 (76.6 against 71.3 with both).
-    const int64_t unit_bytes = (int64_t)4 * b * D, segs = (int64_t)L.rows * L.nseg;
+    const int64_t unit_bytes = kv4 ? (int64_t)Kv4Block(b, D).bytes : (int64_t)4 * b * D, segs = (int64_t)L.rows * L.nseg;
     const bool large = (int64_t)L.rows * desc->nb_cap * unit_bytes > LARGE_CACHE_BYTES;
     const int64_t share = (PREFETCH_BYTES + segs * unit_bytes - 1) / (segs * unit_bytes);
-    sa.prefetch = !large ? 0 : (int)(share < SEG ? share : SEG);
+    sa.prefetch = !large || kv4 ? 0 : (int)(share < SEG ? share : SEG);
     profile_mark(2, s);
     rc = launch_screen(sa, tmK, tmV, L.rows, D, G, n_sm, s);
     profile_mark(3, s);
@@ -1097,14 +1125,21 @@ static int decode_impl(const eta_cache_desc* desc, const eta_page_table* pages, 
     da.read_once = large ? 1 : 0;
     da.div_gpr = FastDiv(L.gpr); da.div_hkv = FastDiv(desc->n_kv_heads); da.div_grid = FastDiv(n_ctas);
     da.timeline = debug_timeline();
-    if (D == 128 && TS == 64) {
-        rc = launch_decode_t<128, 64, 6, DECODE_GROUPS>(tmK, tmV, da, n_ctas, s);
+    da.pool = nullptr;
+    if (kv4) {
+        da.pool = static_cast<const unsigned char*>(K);
+        da.sb = kv4->stride_b; da.sh = kv4->stride_h; da.sj = pages ? 0 : kv4->stride_j;
+        da.scale = scale * kv4->k_scale;
+        da.out_scale = kv4->v_scale;
+        rc = D == 128 ? launch_decode_kv4<128>(da, n_ctas, s) : launch_decode_kv4<64>(da, n_ctas, s);
+    } else if (D == 128 && TS == 64) {
+        rc = launch_decode_t<128, Bf16Tile<128, 64>, 6>(tmK, tmV, da, n_ctas, s);
     } else if (D == 128 && TS == 32) {
-        rc = launch_decode_t<128, 32, 12, DECODE_GROUPS>(tmK, tmV, da, n_ctas, s);
+        rc = launch_decode_t<128, Bf16Tile<128, 32>, 12>(tmK, tmV, da, n_ctas, s);
     } else if (D == 64 && TS == 64) {
-        rc = launch_decode_t<64, 64, 12, DECODE_GROUPS>(tmK, tmV, da, n_ctas, s);
+        rc = launch_decode_t<64, Bf16Tile<64, 64>, 12>(tmK, tmV, da, n_ctas, s);
     } else {
-        rc = launch_decode_t<64, 32, 24, DECODE_GROUPS>(tmK, tmV, da, n_ctas, s);
+        rc = launch_decode_t<64, Bf16Tile<64, 32>, 24>(tmK, tmV, da, n_ctas, s);
     }
     if (rc != ETA_OK) return rc;
     profile_mark(4, s);
@@ -1146,7 +1181,7 @@ int eta_decode(const eta_cache_desc* desc, const eta_params* params, const void*
                const int32_t* seq_lens, const void* musig, const float* mnorm, const float* tau,
                const float* head_const, float* out, uint8_t* sel_mask, int32_t* stats, uint32_t* status_dev,
                void* workspace, size_t workspace_bytes, void* stream) {
-    return eta::decode_impl(desc, nullptr, params, q, K, V, seq_lens, musig, mnorm, tau, head_const, out, sel_mask, stats,
+    return eta::decode_impl(desc, nullptr, nullptr, params, q, K, V, seq_lens, musig, mnorm, tau, head_const, out, sel_mask, stats,
                             status_dev, workspace, workspace_bytes, stream);
 }
 
@@ -1155,8 +1190,25 @@ int eta_decode_paged(const eta_cache_desc* desc, const eta_page_table* pages, co
                      const float* mnorm, const float* tau, const float* head_const, float* out, uint8_t* sel_mask,
                      int32_t* stats, uint32_t* status_dev, void* workspace, size_t workspace_bytes, void* stream) {
     if (!pages) return ETA_ERR_INVALID_ARG;
-    return eta::decode_impl(desc, pages, params, q, K_pool, V_pool, seq_lens, musig, mnorm, tau, head_const, out, sel_mask,
+    return eta::decode_impl(desc, nullptr, pages, params, q, K_pool, V_pool, seq_lens, musig, mnorm, tau, head_const, out, sel_mask,
                             stats, status_dev, workspace, workspace_bytes, stream);
+}
+
+int eta_kv4_workspace_bytes(const eta_cache_desc* desc, size_t* out_bytes) {
+    if (!out_bytes) return ETA_ERR_INVALID_ARG;
+    const int rc = eta::validate_index(desc);
+    if (rc != ETA_OK) return rc;
+    *out_bytes = eta::ws_layout(desc).total;
+    return ETA_OK;
+}
+
+int eta_decode_kv4(const eta_cache_desc* desc, const eta_kv4_desc* kv4, const eta_page_table* pages, const eta_params* params, const void* q,
+                   const void* pool, const int32_t* seq_lens, const void* musig, const float* mnorm, const float* tau,
+                   const float* head_const, float* out, uint8_t* sel_mask, int32_t* stats, uint32_t* status_dev, void* workspace,
+                   size_t workspace_bytes, void* stream) {
+    if (!kv4) return ETA_ERR_INVALID_ARG;
+    return eta::decode_impl(desc, kv4, pages, params, q, pool, pool, seq_lens, musig, mnorm, tau, head_const, out, sel_mask, stats,
+                            status_dev, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -38,6 +38,15 @@ __device__ __forceinline__ uint32_t f32x2_to_e2m1x2(float lo, float hi) {
 }
 __device__ __forceinline__ float f16_lo(uint32_t p) { return __low2float(*reinterpret_cast<const __half2*>(&p)); }
 __device__ __forceinline__ float f16_hi(uint32_t p) { return __high2float(*reinterpret_cast<const __half2*>(&p)); }
+// fp16 pairs held as words
+__device__ __forceinline__ uint32_t hmul2_u(uint32_t a, uint32_t b) {
+    const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t hfma2_u(uint32_t a, uint32_t b, uint32_t c) {
+    const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b), *reinterpret_cast<const __half2*>(&c));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
 
 #endif  // __CUDACC__
 }  // namespace eta

@@ -457,6 +457,91 @@ PyObject* unpack(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return PyLong_FromLong(rc);
 }
 
+// the page table of a 4-bit cache's call, or none: what the pool says
+bool pages_of(PyObject* o, Struct<eta_page_table>& ps, int32_t n_pages, const eta_page_table** out) {
+    *out = nullptr;
+    if (o != Py_None && !(*out = ps.get(o, g_pages))) return false;
+    if ((n_pages > 0) != (*out != nullptr)) return fail("pages", n_pages ? "the page table of the paged pool" : "None: the pool is contiguous");
+    return !*out || (*out)->n_pages <= n_pages || fail("pages", "of a pool with no more pages than this one");
+}
+
+// (address, desc, kv4, pages or None, pool, seq_lens, musig, mnorm, flags) -> return code; the build and the append
+PyObject* index_kv4(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    using F = int (*)(const eta_cache_desc*, const eta_kv4_desc*, const eta_page_table*, const void*, const int32_t*, void*, float*, uint32_t,
+                      void*);
+    F fn;
+    Struct<eta_cache_desc> ds;
+    Struct<eta_kv4_desc> qs;
+    Struct<eta_page_table> ps;
+    void *pool, *musig;
+    int32_t n_pages, *seq_lens;
+    float* mnorm;
+    const eta_page_table* pages;
+    if (!count(n, 9) || !entry(v[0], &fn)) return nullptr;
+    const eta_cache_desc* desc = ds.get(v[1], g_desc);
+    if (!desc) return nullptr;
+    const eta_kv4_desc* q4 = qs.get(v[2], g_kv4);
+    if (!q4 || !pool_tensor(v[4], desc, q4, &pool, &n_pages) || !pages_of(v[3], ps, n_pages, &pages)) return nullptr;
+    const uint32_t flags = (uint32_t)PyLong_AsUnsignedLongMask(v[8]);
+    if (PyErr_Occurred()) return nullptr;
+    const int64_t blocks = (int64_t)desc->batch * desc->n_kv_heads * desc->nb_cap;
+    const bool packed = (flags & ETA_BUILD_PACKED_SIGMA) != 0;
+    if (!VEC(v[5], at::kInt, seq_lens, desc->batch) ||
+        !vector(v[6], packed ? at::kByte : at::kHalf, "musig", blocks * desc->head_dim * (packed ? 3 : 2), &musig) || !VEC(v[7], at::kFloat, mnorm, blocks))
+        return nullptr;
+    void* const s = stream();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn(desc, q4, pages, pool, seq_lens, musig, mnorm, flags, s);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+// (address, desc, kv4, pages or None, params, q, pool, seq_lens, musig, mnorm, tau, head_const, out, sel_mask, stats, status, workspace)
+// -> return code
+PyObject* decode_kv4(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    using F = int (*)(const eta_cache_desc*, const eta_kv4_desc*, const eta_page_table*, const eta_params*, const void*, const void*,
+                      const int32_t*, const void*, const float*, const float*, const float*, float*, uint8_t*, int32_t*, uint32_t*, void*, size_t,
+                      void*);
+    F fn;
+    Struct<eta_cache_desc> ds;
+    Struct<eta_kv4_desc> qs;
+    Struct<eta_page_table> ps;
+    eta_params p;
+    void *q, *pool, *musig, *workspace, *out;
+    int32_t n_pages, *seq_lens, *stats;
+    float *mnorm, *tau, *head_const;
+    uint8_t* sel_mask;
+    uint32_t* status;
+    const eta_page_table* pages;
+    if (!count(n, 17) || !entry(v[0], &fn)) return nullptr;
+    const eta_cache_desc* d = ds.get(v[1], g_desc);
+    if (!d) return nullptr;
+    const eta_kv4_desc* q4 = qs.get(v[2], g_kv4);
+    if (!q4 || !params_of(v[4], &p) || !pool_tensor(v[6], d, q4, &pool, &n_pages) || !pages_of(v[3], ps, n_pages, &pages)) return nullptr;
+    const int64_t rows = (int64_t)d->batch * d->n_kv_heads, heads = (int64_t)d->batch * d->n_q_heads, blocks = rows * d->nb_cap;
+    const bool packed = (p.flags & ETA_FLAG_PACKED_SIGMA) != 0, index = (p.flags & ETA_FLAG_DENSE) == 0;
+    if (!VEC(v[5], at::kBFloat16, q, heads * d->head_dim) || !VEC(v[7], at::kInt, seq_lens, d->batch) ||
+        !vector(v[8], packed ? at::kByte : at::kHalf, "musig", blocks * d->head_dim * (packed ? 3 : 2), &musig, !index) ||
+        !vector(v[9], at::kFloat, "mnorm", blocks, (void**)&mnorm, !index) || !OPT(v[10], at::kFloat, tau, heads) ||
+        !OPT(v[11], at::kFloat, head_const, d->n_q_heads) || !VEC(v[13], at::kByte, sel_mask, blocks) || !OPT(v[14], at::kInt, stats, rows) ||
+        !OPT(v[15], at::kInt, status, 1) || !VEC(v[16], at::kByte, workspace, -1))
+        return nullptr;
+    // the output may be page-locked host memory
+    if (!pointer(v[12], at::kFloat, "out", &out, true)) return nullptr;
+    if (v[12] == Py_None) return fail("out", "a tensor, not None"), nullptr;
+    const at::Tensor& o = THPVariable_Unpack(v[12]);
+    if (!o.is_contiguous() || o.numel() != heads * d->head_dim || (o.is_cuda() && o.device().index() != c10::cuda::current_device()))
+        return fail("out", "contiguous [batch, n_q_heads, head_dim] on the current CUDA device or in page-locked memory"), nullptr;
+    const size_t bytes = (size_t)THPVariable_Unpack(v[16]).numel();
+    void* const s = stream();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn(d, q4, pages, &p, q, pool, seq_lens, musig, mnorm, tau, head_const, (float*)out, sel_mask, stats, status, workspace, bytes, s);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
 // the eta_params a call would get, as bytes (for the tests)
 PyObject* params(PyObject*, PyObject* const* v, Py_ssize_t n) {
     eta_params p;
@@ -494,6 +579,8 @@ PyMethodDef methods[] = {
     {"decode_paged", (PyCFunction)(void (*)(void))guarded<decode<Decode::PAGED>>, METH_FASTCALL, nullptr},
     {"decode_static", (PyCFunction)(void (*)(void))guarded<decode<Decode::STATIC>>, METH_FASTCALL, nullptr},
     {"tokens", (PyCFunction)(void (*)(void))guarded<tokens>, METH_FASTCALL, nullptr},
+    {"index_kv4", (PyCFunction)(void (*)(void))guarded<index_kv4>, METH_FASTCALL, nullptr},
+    {"decode_kv4", (PyCFunction)(void (*)(void))guarded<decode_kv4>, METH_FASTCALL, nullptr},
     {"unpack", (PyCFunction)(void (*)(void))guarded<unpack>, METH_FASTCALL, nullptr},
     {"plan", (PyCFunction)(void (*)(void))guarded<plan>, METH_FASTCALL, nullptr},
     {"params", (PyCFunction)(void (*)(void))guarded<params>, METH_FASTCALL, nullptr},

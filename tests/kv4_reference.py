@@ -75,3 +75,21 @@ def rotate(x, positions, inv_freq, interleaved):
     y[..., a] = x[..., a] * c - x[..., b] * s
     y[..., b] = x[..., a] * s + x[..., b] * c
     return y
+
+
+def scatter(blocks, rng):
+    """Blocks [B, Hkv, nb, bytes] as a paged pool [B * nb, Hkv, bytes] and its table."""
+    B, Hkv, nb, size = blocks.shape
+    perm = rng.permutation(B * nb).astype(np.int32)
+    pool = np.empty((B * nb, Hkv, size), np.uint8)
+    pool[perm] = blocks.transpose(0, 2, 1, 3).reshape(B * nb, Hkv, size)
+    return pool, perm.reshape(B, nb)
+
+
+def output_bound(q, K, V, beta, scale):
+    """How far fp32 arithmetic may take an output.  A score is a sum of exact products in at most eight accumulation steps: off by 2^-20 of
+    A = s |q| |k|.  The gate S sigmoid(beta (S - tau)) has a slope of at most 1 + beta |S| / 4 + 1, and adds 2^-21 of |S| by its own
+    approximations.  A weight off by a factor 1 + e, and a sum of weights off as much, move an average of V by at most 2 e max|V|."""
+    A = scale * np.sqrt((q ** 2).sum(-1).max()) * np.sqrt((K ** 2).sum(-1).max())
+    e = (2 + beta * A / 4) * 2.0 ** -20 * A + 2.0 ** -21 * A + 2.0 ** -20
+    return 2 * e * np.abs(V).max()
