@@ -86,25 +86,32 @@ template <int D, int TS_>
 struct Bf16Tile {
     static constexpr int TS = TS_;
     static constexpr bool KV4 = false;
+    static constexpr int UNITS = 1;                             // copies that share a stage
     static constexpr int HALVES = D / 64;
     static constexpr int TILE_BYTES = TS * 128;                 // one 64-column half tile
     static constexpr int STAGE_BYTES = 2 * HALVES * TILE_BYTES; // K halves then V halves
     using Math = Attend<D, TS>;
 };
-// ... or a block of a 4-bit one
-template <int D, int TS_, bool WIDE>
+// ... or blocks of a 4-bit one, up to 128 tokens (256 of head_dim 64) of one row: with a block a stage, the four warps of a group took a slab
+// of sixteen tokens each (half a slab of blocks of 32), and the wait, the description and the release of a stage were a fifth of the
+// instructions
+template <int D, int b, bool WIDE>
 struct Kv4Tile {
-    static constexpr int TS = TS_;
+    static constexpr int TS = b;
     static constexpr bool KV4 = true;
-    static constexpr int STAGE_BYTES = Kv4Block(TS, D).bytes;
-    using Math = AttendKv4<D, TS, WIDE>;
+    static constexpr int UNITS = 128 * (128 / D) / b;
+    static constexpr int UNIT_BYTES = Kv4Block(b, D).bytes;
+    static constexpr int STAGE_BYTES = UNITS * UNIT_BYTES;
+    using Math = AttendKv4<D, b, WIDE>;
 };
 
-template <int D, int STAGE_BYTES, int NSTAGE, int NGROUPS>
+template <int D, typename Tile, int NSTAGE, int NGROUPS>
 struct DecodeSmem {
+    static constexpr int STAGE_BYTES = Tile::STAGE_BYTES;
     static constexpr int BAR_OFF = NSTAGE * STAGE_BYTES;        // full[NSTAGE], empty[NSTAGE], flush[NGROUPS], layout
     static constexpr int DESC_OFF = (BAR_OFF + 8 * (2 * NSTAGE + NGROUPS + 1) + 15) / 16 * 16;
-    static constexpr int WIN_OFF = DESC_OFF + 16 * NSTAGE;      // uint4 [32]: the producer's window of granules
+    static constexpr int UDESC_OFF = DESC_OFF + 16 * NSTAGE;    // int2 [NSTAGE][UNITS]: a 4-bit cache's units
+    static constexpr int WIN_OFF = UDESC_OFF + (Tile::KV4 ? (8 * Tile::UNITS * NSTAGE + 15) / 16 * 16 : 0);      // uint4 [32]: the producer's window of granules
     static constexpr int GRAN_OFF = WIN_OFF + 16 * 32;          // uint4 [CHUNK]: all granules (one chunk), else int2 [MAX_SUPER]: sums
     static constexpr int BEFORE_OFF = GRAN_OFF + 16 * CHUNK;    // int2 [CHUNK + 1] (+ pad): units and live rows before a granule (one chunk)
     static constexpr int SPAN_OFF = BEFORE_OFF + 8 * (CHUNK + 2);      // int2 [SPAN_ROWS + 1] (+ pad): units and live rows before a row
@@ -125,7 +132,7 @@ template <int D, typename Tile, int NSTAGE, int NGROUPS>
 __global__ void __launch_bounds__(32 * (WARPS_PER_GROUP * NGROUPS + 1), 1)
 decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const DecodeArgs a) {
     constexpr int TS = Tile::TS, STAGE_BYTES = Tile::STAGE_BYTES;
-    using L = DecodeSmem<D, STAGE_BYTES, NSTAGE, NGROUPS>;
+    using L = DecodeSmem<D, Tile, NSTAGE, NGROUPS>;
     constexpr int PRODUCER_WARP = WARPS_PER_GROUP * NGROUPS;
 
     extern __shared__ unsigned char smem_raw[];
@@ -135,6 +142,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
     uint64_t* flushbar = empty + NSTAGE;
     uint64_t* laybar = flushbar + NGROUPS;
     int4* desc = reinterpret_cast<int4*>(smem + L::DESC_OFF);
+    int2* const udesc = reinterpret_cast<int2*>(smem + L::UDESC_OFF);
     uint8_t* rowinfo = smem + L::INFO_OFF;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -570,16 +578,21 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             const int un = u + nb;
             const int nrows = c_nrows & 0xffff;
             const bool valid = c_row >= 0 && usub * TS < nrows;
-            const unsigned vmask = __ballot_sync(0xffffffffu, valid);
-            const uint32_t my_fill = fill + (uint32_t)__popc(vmask & ((1u << lane) - 1u));
             // pieces: a new one starts where the row changes
             const int left = __shfl_up_sync(0xffffffffu, c_row, 1);
             unsigned starts = __ballot_sync(0xffffffffu, c_row >= 0 && c_row != (lane == 0 ? prev_row : left));
+            // stages: one per tile, or one per Tile::UNITS consecutive units of a row (of the batch); `first` fills it
+            const int in_run = Tile::UNITS > 1 ? lane - (31 - __clz((starts | 1u) & (0xffffffffu >> (31 - lane)))) : 0;
+            const bool first_of_stage = valid && in_run % Tile::UNITS == 0;
+            const unsigned vmask = __ballot_sync(0xffffffffu, first_of_stage);
+            const uint32_t my_fill = fill + (uint32_t)__popc(vmask & (0xffffffffu >> (31 - lane))) - (valid ? 1u : 0u);
+            const unsigned later = lane < 31 ? vmask >> (lane + 1) : 0u;
+            const int n_units = Tile::UNITS > 1 ? min(later ? __ffs(later) : 32, nb - lane) : 1;       // of the stage that starts here
             const int my_piece = piece + __popc(starts & (0xffffffffu >> (31 - lane)));
             piece += __popc(starts);
             const int stage = (int)(my_fill % NSTAGE);
             const uint32_t parity = ((my_fill / NSTAGE) & 1) ^ 1;
-            bool done = !valid;
+            bool done = !first_of_stage;
             int my_i, my_hk;
             a.div_hkv.divmod(max(c_row, 0), my_i, my_hk);
             // The outermost coordinate is the sequence (contiguous cache: token offset in the sequence) or the page (paged
@@ -592,7 +605,9 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             const int nvalid = min(TS, nrows - usub * TS);
             // bits 8..15: row of the tile whose token stays ungated, 0xff: none
             const int urow = ((c_nrows >> 16) != 0 && (usub + 1) * TS >= nrows) ? nvalid - 1 : 0xff;
-            const int4 my_desc = make_int4(c_row, my_piece << 1, ((c_ent >> 24) & 0xff) | (urow << 8), nvalid);
+            // (of a stage of several units the number of its slabs: only a row's last unit, its tail, may have fewer than the others)
+            const int n_slabs = !Tile::KV4 ? 0 : (n_units - 1) * (TS / 16) + (__shfl_sync(0xffffffffu, nvalid, (lane + n_units - 1) & 31) + 15) / 16;
+            const int4 my_desc = make_int4(c_row, my_piece << 1, Tile::KV4 ? n_slabs : ((c_ent >> 24) & 0xff) | (urow << 8), nvalid);
             // One pass: lanes whose stage is free issue.  A lane looks at its stage's barrier only when the tile that used the
             // stage before it is on its way (parity tells two rounds apart, not three), that is, within NSTAGE tiles of
             // the first one that is not.
@@ -601,18 +616,30 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
                 const int first = __ffs(open) - 1;
                 const uint32_t f_first = __shfl_sync(0xffffffffu, my_fill, first < 0 ? 0 : first);
                 const bool ready = !done && my_fill < f_first + NSTAGE && mbar_test(&empty[stage], parity);
+                if constexpr (Tile::KV4) {
+                    // the stage's other units follow its first: their descriptions before its arrival, their copies with its own
+                    const unsigned firsts = __ballot_sync(0xffffffffu, ready);
+                    const bool go = valid && ((firsts >> (lane - in_run % Tile::UNITS)) & 1);
+                    if (go) udesc[stage * Tile::UNITS + in_run % Tile::UNITS] = make_int2(((c_ent >> 24) & 0xff) | (urow << 8), nvalid);
+                    __syncwarp();
+                    if (ready) {
+                        done = true;
+                        desc[stage] = my_desc;
+                        mbar_arrive_expect_tx(&full[stage], n_units * Tile::UNIT_BYTES);
+                    }
+                    if (go) tma_load_1d_hint(my_smem + (in_run % Tile::UNITS) * Tile::UNIT_BYTES, my_block, Tile::UNIT_BYTES, &full[stage], once);
+                    return __any_sync(0xffffffffu, !done) != 0;
+                }
                 if (ready) {
                     done = true;
                     desc[stage] = my_desc;
                     mbar_arrive_expect_tx(&full[stage], STAGE_BYTES);
                 }
-                // one copy per tensor: 64 columns x TS tokens x HALVES half tiles, each half swizzled; of a 4-bit block one copy of
-                // its bytes.  Tile after tile, so that the first is complete as early as can be.
+                // one copy per tensor: 64 columns x TS tokens x HALVES half tiles, each half swizzled.  Tile after tile, so that
+                // the first is complete as early as can be.
                 for (unsigned rm = __ballot_sync(0xffffffffu, ready); rm; rm &= rm - 1) {
                     if (lane == __ffs(rm) - 1) {
-                        if constexpr (Tile::KV4) {
-                            tma_load_1d_hint(my_smem, my_block, STAGE_BYTES, &full[stage], once);
-                        } else {
+                        if constexpr (!Tile::KV4) {
                             tma_load_5d(my_smem, &tmK, 0, my_y, 0, my_hk, my_w, &full[stage], once);
                             tma_load_5d(my_smem + Tile::HALVES * Tile::TILE_BYTES, &tmV, 0, my_y, 0, my_hk, my_w, &full[stage], once);
                         }
@@ -641,7 +668,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
                 if (more && it >= 2) __nanosleep(20);
             }
             if (!ok) {                    // give up: time for this batch's copies to land (those before it are waited for below)
-                if (valid && done) mbar_wait(&full[stage], parity ^ 1);
+                if (first_of_stage && done) mbar_wait(&full[stage], parity ^ 1);
                 __syncwarp();
                 break;
             }
@@ -705,6 +732,87 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
     if (s_row0 < 0) return;
     load_q(s_row0);       // the row of the CTA's first unit: fetched while its first tiles are on their way
 
+    // A group's part of a piece is complete: combine its four warps and store (m, l, O) per head.
+    auto flush_piece = [&]() {
+                    at.store_ml(sm_m + wq * 8, sm_l + wq * 8);
+        const int64_t slot = ((int64_t)blockIdx.x + row) * NGROUPS + group;
+        for (int h0 = 0; h0 < a.G && ok; h0 += fheads) {
+            at.store_o(sm_o + wq * fheads * D, h0, fheads);
+#ifdef ETA_TEST_SKIP_FLUSH_ARRIVE
+            // test build only: one warp of the first CTA never arrives, so that the group's bounded wait runs out and
+            // the give-up path (status flag, orderly exit of the whole CTA) executes
+            if (!(blockIdx.x == 0 && group == 0 && wq == 1))
+#endif
+            mbar_arrive(&flushbar[group]);
+            if (!mbar_wait(&flushbar[group], flush_phase)) { ok = false; break; }
+            flush_phase ^= 1;
+            for (int idx = gtid; idx < fheads * D / 4; idx += 32 * WARPS_PER_GROUP) {
+                const int hr = idx / (D / 4), dq = idx % (D / 4), hh = h0 + hr;
+                float mw[WARPS_PER_GROUP], M = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < WARPS_PER_GROUP; ++w) { mw[w] = sm_m[w * 8 + hh]; M = fmaxf(M, mw[w]); }
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                float lacc = 0.f;
+                if (M != -INFINITY) {
+#pragma unroll
+                    for (int w = 0; w < WARPS_PER_GROUP; ++w) {
+                        const float sc = exp2f((mw[w] - M) * LOG2E);
+                        const float4 x = *reinterpret_cast<const float4*>(sm_o + (w * fheads + hr) * D + 4 * dq);
+                        acc.x = fmaf(x.x, sc, acc.x); acc.y = fmaf(x.y, sc, acc.y);
+                        acc.z = fmaf(x.z, sc, acc.z); acc.w = fmaf(x.w, sc, acc.w);
+                        lacc = fmaf(sm_l[w * 8 + hh], sc, lacc);
+                    }
+                }
+                if constexpr (Tile::KV4) { acc.x *= a.out_scale; acc.y *= a.out_scale; acc.z *= a.out_scale; acc.w *= a.out_scale; }
+                *reinterpret_cast<float4*>(a.part_o + (slot * a.G + hh) * D + 4 * dq) = acc;
+                if (dq == 0) a.part_ml[slot * a.G + hh] = make_float2(M, lacc);
+            }
+            mbar_arrive(&flushbar[group]);
+            if (!mbar_wait(&flushbar[group], flush_phase)) { ok = false; break; }
+            flush_phase ^= 1;
+        }
+    };
+    if constexpr (Tile::KV4) {
+        // Piece after piece, the stages of a piece in a loop of their own: with the flush inside that loop the accumulators were moved
+        // between registers once a slab, 53 of 396 instructions.
+        constexpr int SPU = TS / 16;                       // slabs of a unit
+        uint32_t fill = group;
+        ok = mbar_wait(&full[fill % NSTAGE], (fill / NSTAGE) & 1);
+        while (ok) {
+            int4 ds = desc[fill % NSTAGE];
+            if (ds.y & (int)UF_END) { pdl_trigger(); break; }
+            piece = ds.y >> 1;
+            row = ds.x;
+            if (row != q_row) load_q(row);
+            at.reset();
+            do {
+                const int stage = fill % NSTAGE;
+                const uint32_t base = smem_u32(smem + stage * STAGE_BYTES);
+                // the stage's slabs in equal shares
+                const int end_slab = (wq + 1) * ds.z / WARPS_PER_GROUP;
+#pragma unroll 1
+                for (int sl = wq * ds.z / WARPS_PER_GROUP; sl < end_slab; ++sl) {
+                    const int unit = sl / SPU, r0 = (sl % SPU) * 16;
+                    const int2 ud = udesc[stage * Tile::UNITS + unit];
+                    at.slab(base + unit * Tile::UNIT_BYTES, r0, ud.x & 0xff, (ud.x >> 8) & 0xff, ud.y, a.scale, a.beta);
+                }
+                // the arrive (release) orders the warp's reads of the stage before the producer's next copy into it
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&empty[stage]);
+                fill += NGROUPS;
+                ok = mbar_wait(&full[fill % NSTAGE], (fill / NSTAGE) & 1);
+                if (!ok) break;
+                ds = desc[fill % NSTAGE];
+            } while (!(ds.y & (int)UF_END) && (ds.y >> 1) == piece);
+            if (!ok) break;
+            // the next piece's query is on its way during the flush, which does not read the query registers
+            if (ds.y & (int)UF_END) pdl_trigger();
+            else if (ds.x != q_row) load_q(ds.x);
+            flush_piece();
+        }
+        if (!ok && lane == 0 && a.status) atomicOr(a.status, ETA_DEV_TIMEOUT);
+        return;
+    } else {
     for (uint32_t fill = group;; fill += NGROUPS) {
         const int stage = fill % NSTAGE;
         if (!mbar_wait(&full[stage], (fill / NSTAGE) & 1)) { ok = false; break; }
@@ -721,44 +829,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         // query registers, and its barriers and stores hide the load's latency
         if (!end && new_piece != piece && ds.x != q_row) load_q(ds.x);
         if ((end || new_piece != piece) && piece >= 0) {
-            // ---- this group's part of a piece is complete: combine its four warps and store (m, l, O) per head
-            at.store_ml(sm_m + wq * 8, sm_l + wq * 8);
-            const int64_t slot = ((int64_t)blockIdx.x + row) * NGROUPS + group;
-            for (int h0 = 0; h0 < a.G && ok; h0 += fheads) {
-                at.store_o(sm_o + wq * fheads * D, h0, fheads);
-#ifdef ETA_TEST_SKIP_FLUSH_ARRIVE
-                // test build only: one warp of the first CTA never arrives, so that the group's bounded wait runs out and
-                // the give-up path (status flag, orderly exit of the whole CTA) executes
-                if (!(blockIdx.x == 0 && group == 0 && wq == 1))
-#endif
-                mbar_arrive(&flushbar[group]);
-                if (!mbar_wait(&flushbar[group], flush_phase)) { ok = false; break; }
-                flush_phase ^= 1;
-                for (int idx = gtid; idx < fheads * D / 4; idx += 32 * WARPS_PER_GROUP) {
-                    const int hr = idx / (D / 4), dq = idx % (D / 4), hh = h0 + hr;
-                    float mw[WARPS_PER_GROUP], M = -INFINITY;
-#pragma unroll
-                    for (int w = 0; w < WARPS_PER_GROUP; ++w) { mw[w] = sm_m[w * 8 + hh]; M = fmaxf(M, mw[w]); }
-                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-                    float lacc = 0.f;
-                    if (M != -INFINITY) {
-#pragma unroll
-                        for (int w = 0; w < WARPS_PER_GROUP; ++w) {
-                            const float sc = exp2f((mw[w] - M) * LOG2E);
-                            const float4 x = *reinterpret_cast<const float4*>(sm_o + (w * fheads + hr) * D + 4 * dq);
-                            acc.x = fmaf(x.x, sc, acc.x); acc.y = fmaf(x.y, sc, acc.y);
-                            acc.z = fmaf(x.z, sc, acc.z); acc.w = fmaf(x.w, sc, acc.w);
-                            lacc = fmaf(sm_l[w * 8 + hh], sc, lacc);
-                        }
-                    }
-                    if constexpr (Tile::KV4) { acc.x *= a.out_scale; acc.y *= a.out_scale; acc.z *= a.out_scale; acc.w *= a.out_scale; }
-                    *reinterpret_cast<float4*>(a.part_o + (slot * a.G + hh) * D + 4 * dq) = acc;
-                    if (dq == 0) a.part_ml[slot * a.G + hh] = make_float2(M, lacc);
-                }
-                mbar_arrive(&flushbar[group]);
-                if (!mbar_wait(&flushbar[group], flush_phase)) { ok = false; break; }
-                flush_phase ^= 1;
-            }
+            flush_piece();
             if (!ok) break;
         }
         if (end) {
@@ -766,7 +837,6 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             break;
         }
 
-        const int hmask = ds.z & 0xff, urow = (ds.z >> 8) & 0xff, nvalid = ds.w;
         const uint32_t kbase = smem_u32(smem + stage * STAGE_BYTES);
 
         if (new_piece != piece) {
@@ -777,9 +847,10 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         }
 
         // the arrive (release) orders the warp's reads of the stage before the producer's next copy into it
-        at.tile(kbase, hmask, urow, nvalid, a.scale, a.beta, [&]() { if (lane == 0) mbar_arrive(&empty[stage]); });
+        at.tile(kbase, ds.z & 0xff, (ds.z >> 8) & 0xff, ds.w, a.scale, a.beta, [&]() { if (lane == 0) mbar_arrive(&empty[stage]); });
     }
     if (!ok && lane == 0 && a.status) atomicOr(a.status, ETA_DEV_TIMEOUT);
+    }
 }
 
 // Associative merge of the pieces of one (sequence, query head): Algorithm 3, global reduction.
@@ -965,19 +1036,18 @@ static int make_tmap(CUtensorMap* tm, const void* base, const eta_cache_desc* d,
 template <int D, typename Tile, int NSTAGE>
 static int launch_decode_t(const CUtensorMap& tmK, const CUtensorMap& tmV, const DecodeArgs& a, int n_ctas,
                            cudaStream_t s) {
-    const size_t smem = DecodeSmem<D, Tile::STAGE_BYTES, NSTAGE, DECODE_GROUPS>::bytes(a.G);
+    const size_t smem = DecodeSmem<D, Tile, NSTAGE, DECODE_GROUPS>::bytes(a.G);
     return launch_pdl("decode launch", decode_kernel<D, Tile, NSTAGE, DECODE_GROUPS>, dim3(n_ctas),
                       dim3(32 * (WARPS_PER_GROUP * DECODE_GROUPS + 1)), smem, s, tmK, tmV, a);
 }
 
-// A 4-bit cache: a block is a stage.
+// A 4-bit cache: stages of 18 KB, 166 KB in all.
 template <int D>
 static int launch_decode_kv4(const DecodeArgs& a, int n_ctas, cudaStream_t s) {
     const CUtensorMap none = {};
-#define ETA_KV4(TS, N) (a.G > 4 ? launch_decode_t<D, Kv4Tile<D, TS, true>, N>(none, none, a, n_ctas, s) \
-                                : launch_decode_t<D, Kv4Tile<D, TS, false>, N>(none, none, a, n_ctas, s))
-    constexpr int F = D == 128 ? 1 : 2;              // 166 KB of stages
-    return a.b == 32 ? ETA_KV4(32, 36) : (a.b == 64 ? ETA_KV4(64, 18 * F) : ETA_KV4(128, 9 * F));
+#define ETA_KV4(B) (a.G > 4 ? launch_decode_t<D, Kv4Tile<D, B, true>, 9>(none, none, a, n_ctas, s) \
+                            : launch_decode_t<D, Kv4Tile<D, B, false>, 9>(none, none, a, n_ctas, s))
+    return a.b == 32 ? ETA_KV4(32) : (a.b == 64 ? ETA_KV4(64) : ETA_KV4(128));
 #undef ETA_KV4
 }
 

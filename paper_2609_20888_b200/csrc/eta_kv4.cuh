@@ -24,11 +24,12 @@ int validate_kv4(const eta_cache_desc* d, const eta_kv4_desc* kv4, const void* p
 
 #ifdef __CUDACC__
 
-// the two codes of a byte (channel 2 j low, 2 j + 1 high) as fp16
-__device__ __forceinline__ uint32_t e2m1x2_to_f16x2(uint32_t byte) {
-    uint32_t r;
-    asm("{\n\t.reg .b8 c;\n\tcvt.u8.u32 c, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, c;\n\t}" : "=r"(r) : "r"(byte));
-    return r;
+// Eight codes as four fp16 pairs, byte by byte (channel 2 j low, 2 j + 1 high).  The bytes are named in place: a conversion then takes its
+// byte itself and costs two cycles of a scheduler, where cutting the byte out first costs four more.
+__device__ __forceinline__ void e2m1x8_to_f16x2(uint32_t w, uint32_t (&h)[4]) {
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
 }
 // two fp32 -> a byte of codes, `lo` in the low half: nearest, ties to even, saturating
 __device__ __forceinline__ uint32_t f32x2_to_e2m1x2(float lo, float hi) {

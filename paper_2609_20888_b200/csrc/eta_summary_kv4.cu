@@ -15,11 +15,11 @@ namespace eta {
 
 // Sixteen codes of a lane as fp16 pairs, unscaled
 __device__ __forceinline__ void codes_to_f16(const uint2& w, uint32_t (&h)[8]) {
+    uint32_t x[4], y[4];
+    e2m1x8_to_f16x2(w.x, x);
+    e2m1x8_to_f16x2(w.y, y);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        h[k] = e2m1x2_to_f16x2((w.x >> (8 * k)) & 0xffu);
-        h[4 + k] = e2m1x2_to_f16x2((w.y >> (8 * k)) & 0xffu);
-    }
+    for (int k = 0; k < 4; ++k) { h[k] = x[k]; h[4 + k] = y[k]; }
 }
 // the larger of two numbers; a NaN if either is one
 __device__ __forceinline__ float max_nan(float a, float b) {

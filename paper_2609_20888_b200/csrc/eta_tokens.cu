@@ -255,12 +255,13 @@ __global__ void __launch_bounds__(256) unpack_kv4_kernel(const UnpackArgs a) {
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         const uint32_t w = half ? codes.y : codes.x;
+        uint32_t p[4];
         float x[8];
+        e2m1x8_to_f16x2(w, p);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t p = e2m1x2_to_f16x2((w >> (8 * k)) & 0xffu);
-            x[2 * k] = f16_lo(p) * s;
-            x[2 * k + 1] = f16_hi(p) * s;
+            x[2 * k] = f16_lo(p[k]) * s;
+            x[2 * k + 1] = f16_hi(p[k]) * s;
         }
         reinterpret_cast<uint4*>(to)[half] = pack_bf16(x);
     }
