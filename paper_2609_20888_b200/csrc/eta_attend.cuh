@@ -93,7 +93,8 @@ struct Attend {
         lsum += __shfl_xor_sync(0xffffffffu, lsum, 2);
         if (t == 0) { m[g] = m_run; l[g] = lsum; }
     }
-    // the accumulators of heads h0 .. h0 + n - 1 to sm [n][D]
+    // the accumulators of heads h0 .. h0 + n - 1 to sm [n][O_STRIDE]
+    static constexpr int O_STRIDE = D;
     __device__ __forceinline__ void store_o(float* sm, int h0, int n) const {
         const int ha = 2 * t - h0, hb = ha + 1;         // this lane's two heads within the round
 #pragma unroll

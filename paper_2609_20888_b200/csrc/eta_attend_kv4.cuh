@@ -170,7 +170,11 @@ struct AttendKv4 {
             l[c0] = nx ? 1.f : x; l[c0 + 1] = ny ? 1.f : y;
         }
     }
-    // the accumulators of heads h0 .. h0 + n - 1 to sm [n][D]
+    // The accumulators of heads h0 .. h0 + n - 1 to sm [n][O_STRIDE], channel (D / 8) g + 2 mt + c at 16 mt + 2 g + c: the sixteen lanes of a
+    // phase write to all banks once (by channel they met four and eight at a time: 2 us of a flush's 4).
+    static constexpr int O_STRIDE = D + 4;
+    // where four consecutive channels 4 k .. are: two pairs, 16 floats apart
+    __device__ __forceinline__ static int o_at(int k) { return 16 * (2 * k % MT) + 2 * (2 * k / MT); }
     __device__ __forceinline__ void store_o(float* sm, int h0, int n) const {
         const int ha = c0 - h0, hb = ha + 1;
 #pragma unroll
@@ -181,10 +185,10 @@ struct AttendKv4 {
                 x[c] = o[mt][c];
                 if (!WIDE) x[c] = __shfl_xor_sync(0xffffffffu, x[c], 2) - x[c];       // remainders' columns less the (negated) values'
             }
-            const int dcol = (D / 8) * g + 2 * mt;
+            const int at = 16 * mt + 2 * g;
             if (!WIDE && t >= 2) continue;
-            if (ha >= 0 && ha < n) *reinterpret_cast<float2*>(sm + ha * D + dcol) = make_float2(x[0], x[2]);
-            if (hb >= 0 && hb < n) *reinterpret_cast<float2*>(sm + hb * D + dcol) = make_float2(x[1], x[3]);
+            if (ha >= 0 && ha < n) *reinterpret_cast<float2*>(sm + ha * O_STRIDE + at) = make_float2(x[0], x[2]);
+            if (hb >= 0 && hb < n) *reinterpret_cast<float2*>(sm + hb * O_STRIDE + at) = make_float2(x[1], x[3]);
         }
     }
     __device__ __forceinline__ float gated(float S, float te, float beta) const {
@@ -324,9 +328,9 @@ struct AttendKv4 {
         for (int w = 0; w < VW; ++w) {
             // bytes of (row 2 t, row 2 t + 1) codes: even channels, odd channels
             uint32_t e01[4], d01[4], e23[4], d23[4];
-            e2m1x8_to_f16x2((vw[0][w] & 0x0f0f0f0fu) | ((vw[1][w] << 4) & 0xf0f0f0f0u), e01);
+            e2m1x8_to_f16x2((vw[0][w] & 0x0f0f0f0fu) | ((vw[1][w] * 16u) & 0xf0f0f0f0u), e01);
             e2m1x8_to_f16x2(((vw[0][w] >> 4) & 0x0f0f0f0fu) | (vw[1][w] & 0xf0f0f0f0u), d01);
-            e2m1x8_to_f16x2((vw[2][w] & 0x0f0f0f0fu) | ((vw[3][w] << 4) & 0xf0f0f0f0u), e23);
+            e2m1x8_to_f16x2((vw[2][w] & 0x0f0f0f0fu) | ((vw[3][w] * 16u) & 0xf0f0f0f0u), e23);
             e2m1x8_to_f16x2(((vw[2][w] >> 4) & 0x0f0f0f0fu) | (vw[3][w] & 0xf0f0f0f0u), d23);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {

@@ -121,7 +121,7 @@ struct DecodeSmem {
     static constexpr int MO_OFF = ML_OFF + 4 * 2 * NGROUPS * WARPS_PER_GROUP * 8;
     // heads whose accumulators a flush parks at a time: eight heads of 128 columns would cost the ring a stage
     static constexpr int FLUSH_HEADS = 512 / D;
-    static size_t bytes(int G) { return 1024 + MO_OFF + sizeof(float) * NGROUPS * WARPS_PER_GROUP * (G < FLUSH_HEADS ? G : FLUSH_HEADS) * D; }
+    static size_t bytes(int G) { return 1024 + MO_OFF + sizeof(float) * NGROUPS * WARPS_PER_GROUP * (G < FLUSH_HEADS ? G : FLUSH_HEADS) * Tile::Math::O_STRIDE; }
 };
 
 // The streaming kernel.  Warp roles: NGROUPS consumer groups of four warps, then one producer warp.  Group k
@@ -665,7 +665,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             for (uint32_t it = 0; more; ++it) {
                 more = issue_pass();
                 if (it >= WAIT_LIMIT) { ok = false; break; }
-                if (more && it >= 2) __nanosleep(20);
+                if (more && it >= 2) __nanosleep(Tile::KV4 ? 150 : 20);      // (4-bit: a stage is free every half a microsecond)
             }
             if (!ok) {                    // give up: time for this batch's copies to land (those before it are waited for below)
                 if (first_of_stage && done) mbar_wait(&full[stage], parity ^ 1);
@@ -708,7 +708,8 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
     float* sm_m = reinterpret_cast<float*>(smem + L::ML_OFF) + group * 2 * WARPS_PER_GROUP * 8;
     float* sm_l = sm_m + WARPS_PER_GROUP * 8;
     const int fheads = min(a.G, L::FLUSH_HEADS);       // heads per round of a flush
-    float* sm_o = reinterpret_cast<float*>(smem + L::MO_OFF) + group * WARPS_PER_GROUP * fheads * D;
+    constexpr int OS = Tile::Math::O_STRIDE;
+    float* sm_o = reinterpret_cast<float*>(smem + L::MO_OFF) + group * WARPS_PER_GROUP * fheads * OS;
     const int gtid = tid - group * 32 * WARPS_PER_GROUP;    // thread index inside the group
     const float LOG2E = 1.4426950408889634f;
     typename Tile::Math at(lane, wq, a.G);
@@ -734,10 +735,10 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
 
     // A group's part of a piece is complete: combine its four warps and store (m, l, O) per head.
     auto flush_piece = [&]() {
-                    at.store_ml(sm_m + wq * 8, sm_l + wq * 8);
+        at.store_ml(sm_m + wq * 8, sm_l + wq * 8);
         const int64_t slot = ((int64_t)blockIdx.x + row) * NGROUPS + group;
         for (int h0 = 0; h0 < a.G && ok; h0 += fheads) {
-            at.store_o(sm_o + wq * fheads * D, h0, fheads);
+            at.store_o(sm_o + wq * fheads * OS, h0, fheads);
 #ifdef ETA_TEST_SKIP_FLUSH_ARRIVE
             // test build only: one warp of the first CTA never arrives, so that the group's bounded wait runs out and
             // the give-up path (status flag, orderly exit of the whole CTA) executes
@@ -757,7 +758,14 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
 #pragma unroll
                     for (int w = 0; w < WARPS_PER_GROUP; ++w) {
                         const float sc = exp2f((mw[w] - M) * LOG2E);
-                        const float4 x = *reinterpret_cast<const float4*>(sm_o + (w * fheads + hr) * D + 4 * dq);
+                        float4 x;
+                        const float* const from = sm_o + (w * fheads + hr) * OS;
+                        if constexpr (Tile::KV4) {
+                            const float2 lo = *reinterpret_cast<const float2*>(from + Tile::Math::o_at(dq)), hi = *reinterpret_cast<const float2*>(from + Tile::Math::o_at(dq) + 16);
+                            x = make_float4(lo.x, lo.y, hi.x, hi.y);
+                        } else {
+                            x = *reinterpret_cast<const float4*>(from + 4 * dq);
+                        }
                         acc.x = fmaf(x.x, sc, acc.x); acc.y = fmaf(x.y, sc, acc.y);
                         acc.z = fmaf(x.z, sc, acc.z); acc.w = fmaf(x.w, sc, acc.w);
                         lacc = fmaf(sm_l[w * 8 + hh], sc, lacc);
@@ -776,33 +784,36 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         // Piece after piece, the stages of a piece in a loop of their own: with the flush inside that loop the accumulators were moved
         // between registers once a slab, 53 of 396 instructions.
         constexpr int SPU = TS / 16;                       // slabs of a unit
-        uint32_t fill = group;
-        ok = mbar_wait(&full[fill % NSTAGE], (fill / NSTAGE) & 1);
+        // a group's stages are group, group + NGROUPS, .. round by round
+        int stage = group;
+        uint32_t parity = 0;
+        ok = mbar_wait(&full[stage], 0);
         while (ok) {
-            int4 ds = desc[fill % NSTAGE];
+            int4 ds = desc[stage];
             if (ds.y & (int)UF_END) { pdl_trigger(); break; }
             piece = ds.y >> 1;
             row = ds.x;
             if (row != q_row) load_q(row);
             at.reset();
             do {
-                const int stage = fill % NSTAGE;
                 const uint32_t base = smem_u32(smem + stage * STAGE_BYTES);
+                const int2* const units = udesc + stage * Tile::UNITS;
                 // the stage's slabs in equal shares
                 const int end_slab = (wq + 1) * ds.z / WARPS_PER_GROUP;
 #pragma unroll 1
                 for (int sl = wq * ds.z / WARPS_PER_GROUP; sl < end_slab; ++sl) {
                     const int unit = sl / SPU, r0 = (sl % SPU) * 16;
-                    const int2 ud = udesc[stage * Tile::UNITS + unit];
+                    const int2 ud = units[unit];
                     at.slab(base + unit * Tile::UNIT_BYTES, r0, ud.x & 0xff, (ud.x >> 8) & 0xff, ud.y, a.scale, a.beta);
                 }
                 // the arrive (release) orders the warp's reads of the stage before the producer's next copy into it
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&empty[stage]);
-                fill += NGROUPS;
-                ok = mbar_wait(&full[fill % NSTAGE], (fill / NSTAGE) & 1);
+                stage += NGROUPS;
+                if (stage >= NSTAGE) { stage -= NSTAGE; parity ^= 1; }
+                ok = mbar_wait(&full[stage], parity);
                 if (!ok) break;
-                ds = desc[fill % NSTAGE];
+                ds = desc[stage];
             } while (!(ds.y & (int)UF_END) && (ds.y >> 1) == piece);
             if (!ok) break;
             // the next piece's query is on its way during the flush, which does not read the query registers
