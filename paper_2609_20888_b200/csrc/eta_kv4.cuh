@@ -39,6 +39,12 @@ __device__ __forceinline__ uint32_t f32x2_to_e2m1x2(float lo, float hi) {
 }
 __device__ __forceinline__ float f16_lo(uint32_t p) { return __low2float(*reinterpret_cast<const __half2*>(&p)); }
 __device__ __forceinline__ float f16_hi(uint32_t p) { return __high2float(*reinterpret_cast<const __half2*>(&p)); }
+// the larger of two numbers; a NaN if either is one
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 // fp16 pairs held as words
 __device__ __forceinline__ uint32_t hmul2_u(uint32_t a, uint32_t b) {
     const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));

@@ -21,13 +21,6 @@ __device__ __forceinline__ void codes_to_f16(const uint2& w, uint32_t (&h)[8]) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) { h[k] = x[k]; h[4 + k] = y[k]; }
 }
-// the larger of two numbers; a NaN if either is one
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
-
 template <int D, bool ENVELOPE>
 __device__ __forceinline__ void summarize_kv4(const unsigned char* blk, int b, float g, unsigned char* rec, bool packed, float* mn) {
     constexpr int LPR = D / KV4_GROUP;        // lanes per row

@@ -41,6 +41,12 @@ struct Piece {
             if (on) w[k] = __ldcg(reinterpret_cast<const uint4*>(p) + k);
         }
     }
+    // the piece of another lane
+    __device__ __forceinline__ void exchange(int from) {
+        uint32_t* u = reinterpret_cast<uint32_t*>(w);
+#pragma unroll
+        for (int k = 0; k < 2 * (int)sizeof(T); ++k) u[k] = __shfl_sync(0xffffffffu, u[k], from);
+    }
     template <typename F>
     __device__ __forceinline__ void get(F (&x)[8]) const {
         const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
@@ -64,59 +70,51 @@ __device__ __forceinline__ uint4 pack_bf16(const float (&x)[8]) {
     return o;
 }
 
-// Norm and rotation of a head's piece, in fp32 or fp64.  cs, sn: the row's angles, pair by pair.
-template <int D, typename F, typename CT>
-__device__ __forceinline__ void norm_rotate(F (&x)[8], const float* weight, float eps, int lane, int rotary, bool interleaved,
-                                            const CT* cs, const CT* sn) {
-    constexpr int LPH = D / 8;
-    const int cl = lane % LPH;
-    if (weight) {
-        F ss = 0;
+// What a lane's eight channels are multiplied with, norm weight and rotation in one: y = (x C + x_partner S) r, where x_partner are the pairs'
+// other channels as they came, C = w cos, S = -+ w_partner sin, and r = 1 / sqrt(mean x^2 + eps) (1 without a norm).
+template <typename F>
+struct Turn {
+    F C[8], S[8];
+    // cs, sn: the row's angles, pair by pair
+    template <int D>
+    __device__ __forceinline__ void set(const float* weight, int cl, int rotary, bool interleaved, const F* cs, const F* sn) {
+        const int reach = rotary / 16;                     // lanes between the two halves of a pair
+        const bool turns = 8 * cl < rotary, first = cl < reach;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) ss = fma(x[k], x[k], ss);
-#pragma unroll
-        for (int s = 1; s < LPH; s <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, s);
-        const F r = rsqrt(ss * (F)(1.0 / D) + (F)eps);
-        const float4 w0 = *reinterpret_cast<const float4*>(weight + 8 * cl), w1 = *reinterpret_cast<const float4*>(weight + 8 * cl + 4);
-        const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = x[k] * r * (F)w[k];
-    }
-    if (!rotary) return;
-    const bool turns = 8 * cl < rotary;
-    if (interleaved) {
-        if (turns) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const F c = (F)cs[4 * cl + k], s = (F)sn[4 * cl + k], a = x[2 * k], b = x[2 * k + 1];
-                x[2 * k] = a * c - b * s;
-                x[2 * k + 1] = a * s + b * c;
-            }
-        }
-        return;
-    }
-    const int reach = rotary / 16;                     // lanes between the two halves of a pair
-    const bool first = cl < reach;
-    const int partner = turns ? (first ? lane + reach : lane - reach) : lane, at = first ? 8 * cl : 8 * (cl - reach);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const F y = __shfl_sync(0xffffffffu, x[k], partner);
-        if (turns) {
-            const F c = (F)cs[at + k], s = (F)sn[at + k];
-            x[k] = first ? x[k] * c - y * s : y * s + x[k] * c;
+        for (int k = 0; k < 8; ++k) {
+            const int c = 8 * cl + k, other = interleaved ? c ^ 1 : (first ? c + rotary / 2 : c - rotary / 2);
+            const int pair = interleaved ? c / 2 : (first ? c : c - rotary / 2);
+            const bool minus = interleaved ? !(k & 1) : first;
+            const F w = weight ? (F)weight[c] : (F)1, wp = weight && turns ? (F)weight[other] : (F)1;
+            C[k] = turns ? w * cs[pair] : w;
+            S[k] = turns ? (minus ? -wp : wp) * sn[pair] : (F)0;
         }
     }
-}
+    // x: the lane's channels, y: their partners
+    template <int D>
+    __device__ __forceinline__ void apply(F (&x)[8], const F (&y)[8], bool norm, float eps) const {
+        F r = 1;
+        if (norm) {
+            F ss = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) ss = fma(x[k], x[k], ss);
+#pragma unroll
+            for (int s = 1; s < D / 8; s <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, s);
+            r = rsqrt(ss * (F)(1.0 / D) + (F)eps);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = fma(x[k], C[k], y[k] * S[k]) * r;
+    }
+};
 
 // Eight channels of a row into a 4-bit block: the two lanes that hold a group agree on its scale.
 __device__ __forceinline__ void store_kv4(const double (&x)[8], double g, unsigned char* codes, unsigned char* scales, int cl, bool on) {
-    double top = 0;
-    bool nan = false;
+    // (rounding is monotonic: the largest of the rounded quotients is the largest quotient rounded)
+    const double sixth = 1.0 / (6.0 * g);
+    float want = 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) { top = fmax(top, fabs(x[k])); nan = nan || isnan(x[k]); }
-    top = fmax(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    nan = (__shfl_xor_sync(0xffffffffu, nan ? 1 : 0, 1) != 0) || nan;
-    const float want = nan ? __uint_as_float(0x7fffffffu) : (float)(top / (6.0 * g));
+    for (int k = 0; k < 8; ++k) want = max_nan(want, fabsf((float)(x[k] * sixth)));
+    want = max_nan(want, __shfl_xor_sync(0xffffffffu, want, 1));
     unsigned short pair;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(pair) : "f"(0.f), "f"(want));
     const uint32_t code = pair & 0xffu;
@@ -136,11 +134,13 @@ __device__ __forceinline__ void store_kv4(const double (&x)[8], double g, unsign
 
 constexpr int TOK_WARPS = 4, TOK_LOADS = 4;       // warps of a CTA; pieces that a lane has in flight
 
+// A warp takes items (two or four heads of the row each) one after the other, four on their way at any time: queries, keys, values.
 template <typename T, int D, bool KV4>
-__global__ void __launch_bounds__(32 * TOK_WARPS) append_tokens_kernel(const TokensArgs a) {
-    using CT = typename std::conditional<KV4, double, float>::type;
+__global__ void __launch_bounds__(32 * TOK_WARPS, (sizeof(T) == 4 ? 4 : 5) - (KV4 ? 1 : 0)) append_tokens_kernel(const TokensArgs a) {
+    using F = typename std::conditional<KV4, double, float>::type;       // what keys are worked out in
     constexpr int LPH = D / 8, HPW = 32 / LPH;         // lanes of a head, heads of a warp
-    __shared__ CT s_cos[TOK_WARPS][D / 2], s_sin[TOK_WARPS][D / 2];
+    __shared__ F s_cos[TOK_WARPS][D / 2], s_sin[TOK_WARPS][D / 2];
+    __shared__ float s_cosf[KV4 ? TOK_WARPS : 1][D / 2], s_sinf[KV4 ? TOK_WARPS : 1][D / 2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     pdl_wait();
     const int64_t wid = (int64_t)blockIdx.x * TOK_WARPS + warp;
@@ -156,67 +156,96 @@ __global__ void __launch_bounds__(32 * TOK_WARPS) append_tokens_kernel(const Tok
     const int nq = (a.Hq + HPW - 1) / HPW, nkv = (a.Hkv + HPW - 1) / HPW, all = nq + 2 * nkv;
     const int begin = part * all / a.parts, end = (part + 1) * all / a.parts;
     const int hl = lane / LPH, cl = lane % LPH;
-    const T *const q = static_cast<const T*>(a.q) + row * a.q_sr, *const k = static_cast<const T*>(a.k) + row * a.k_sr,
-            *const v = static_cast<const T*>(a.v) + row * a.v_sr;
+    const T *const q = static_cast<const T*>(a.q) + row * a.q_sr + 8 * cl, *const k = static_cast<const T*>(a.k) + row * a.k_sr + 8 * cl,
+            *const v = static_cast<const T*>(a.v) + row * a.v_sr + 8 * cl;
     Piece<T> pc[TOK_LOADS];
-    auto load = [&](int it0) {
-#pragma unroll
-        for (int u = 0; u < TOK_LOADS; ++u) {
-            const int it = it0 + u;
-            const bool is_q = it < nq, is_k = it < nq + nkv;
-            const int head = (is_q ? it : (is_k ? it - nq : it - nq - nkv)) * HPW + hl;
-            const T* p = (is_q ? q + head * a.q_sh : (is_k ? k + head * a.k_sh : v + head * a.v_sh)) + 8 * cl;
-            pc[u].load(p, it < end && head < (is_q ? a.Hq : a.Hkv));
-        }
+    auto load = [&](Piece<T>& p, int it) {
+        const bool is_q = it < nq, is_k = it < nq + nkv;
+        const int head = (is_q ? it : (is_k ? it - nq : it - nq - nkv)) * HPW + hl;
+        p.load(is_q ? q + head * a.q_sh : (is_k ? k + head * a.k_sh : v + head * a.v_sh), it < end && head < (is_q ? a.Hq : a.Hkv));
     };
-    load(begin);
+#pragma unroll
+    for (int u = 0; u < TOK_LOADS; ++u) load(pc[u], begin + u);
     // ---- the row's angles, reduced by whole turns with a two-part 2 pi (Cody and Waite): any 32-bit position keeps its 64-bit angle
     if (a.rotary && begin < nq + nkv) {
         const double pos = (double)__ldcg(a.positions + row);
         for (int c = lane; c < a.rotary / 2; c += 32) {
             const double x = pos * __ldcg(a.inv_freq + c), n = rint(x * 0.15915494309189535);
             const double r = fma(-n, 2.4492935982947064e-16, fma(-n, 6.283185307179586, x));
-            CT sn, cs;
-            if constexpr (KV4) sincos(r, &sn, &cs);
-            else sincosf((float)r, &sn, &cs);
+            F sn, cs;
+            if constexpr (KV4) {
+                sincos(r, &sn, &cs);
+                s_cosf[warp][c] = (float)cs; s_sinf[warp][c] = (float)sn;
+            } else {
+                sincosf((float)r, &sn, &cs);
+            }
             s_cos[warp][c] = cs; s_sin[warp][c] = sn;
         }
         __syncwarp();
     }
+    const float *const csf = KV4 ? s_cosf[KV4 ? warp : 0] : reinterpret_cast<const float*>(s_cos[warp]),
+                *const snf = KV4 ? s_sinf[KV4 ? warp : 0] : reinterpret_cast<const float*>(s_sin[warp]);
     const int64_t page = slot / a.per_page;
     const int off = (int)(slot - page * a.per_page);
-    const Kv4Block at(a.b, D);
-    for (int it0 = begin; it0 < end; it0 += TOK_LOADS) {
-        if (it0 != begin) load(it0);
+    // the pairs' other halves are in lane `partner`, or in the lane's own neighbours
+    const int reach = a.rotary / 16;
+    const int partner = a.interleaved || 8 * cl >= a.rotary ? lane : (cl < reach ? lane + reach : lane - reach);
+    auto others = [&](const Piece<T>& p, auto& y) {
+        Piece<T> o = p;
+        if (a.rotary && !a.interleaved) o.exchange(partner);
+        o.get(y);
+        if (a.interleaved) {
+#pragma unroll
+            for (int c = 0; c < 8; c += 2) { const auto t = y[c]; y[c] = y[c + 1]; y[c + 1] = t; }
+        }
+        if (a.rotary < D && 8 * cl >= a.rotary) {      // channels that do not turn have no part in anything: not even an infinity times 0
+#pragma unroll
+            for (int c = 0; c < 8; ++c) y[c] = 0;
+        }
+    };
+    Turn<float> turn;
+    if (begin < nq) turn.template set<D>(a.q_weight, cl, a.rotary, a.interleaved != 0, csf, snf);
+    // ---- queries
+    int it = begin;
+    for (; it < end && it < nq; it += TOK_LOADS) {
 #pragma unroll
         for (int u = 0; u < TOK_LOADS; ++u) {
-            const int it = it0 + u;
-            if (it >= end) break;                      // the same for the whole warp
-            if (it < nq) {
-                const int head = it * HPW + hl;
-                float x[8];
+            if (it + u < end && it + u < nq) {         // the same for the whole warp
+                float x[8], y[8];
                 pc[u].get(x);
-                norm_rotate<D>(x, a.q_weight, a.eps, lane, a.rotary, a.interleaved != 0, s_cos[warp], s_sin[warp]);
+                others(pc[u], y);
+                load(pc[u], it + u + TOK_LOADS);
+                turn.template apply<D>(x, y, a.q_weight != nullptr, a.eps);
+                const int head = (it + u) * HPW + hl;
                 if (head < a.Hq) *reinterpret_cast<uint4*>(a.q_out + (row * a.Hq + head) * D + 8 * cl) = pack_bf16(x);
-                continue;
             }
-            const bool is_k = it < nq + nkv;
-            const int head = (is_k ? it - nq : it - nq - nkv) * HPW + hl;
-            const bool on = head < a.Hkv;
-            if constexpr (KV4) {
-                double x[8];
+        }
+    }
+    // ---- keys and values
+    Turn<F> turn_k;
+    const int first = max(begin, nq);                  // pieces of these items are in the slots that follow the queries'
+    if (first < end && first < nq + nkv) turn_k.template set<D>(a.k_weight, cl, a.rotary, a.interleaved != 0, s_cos[warp], s_sin[warp]);
+    for (it = first - (first - begin) % TOK_LOADS; it < end; it += TOK_LOADS) {
+#pragma unroll
+        for (int u = 0; u < TOK_LOADS; ++u) {
+            if (it + u >= first && it + u < end) {
+                const bool is_k = it + u < nq + nkv;
+                const int head = (is_k ? it + u - nq : it + u - nq - nkv) * HPW + hl;
+                const bool on = head < a.Hkv;
+                F x[8], y[8];
                 pc[u].get(x);
-                if (is_k) norm_rotate<D>(x, a.k_weight, a.eps, lane, a.rotary, a.interleaved != 0, s_cos[warp], s_sin[warp]);
-                unsigned char* blk = a.pool + page * a.ks_b + head * a.ks_h + (int64_t)(off / a.b) * a.ks_t;
-                const int t = off % a.b;
-                store_kv4(x, is_k ? a.k_scale : a.v_scale, blk + (is_k ? 0 : at.v_codes) + t * (D / 2),
-                          blk + (is_k ? at.k_scales : at.v_scales) + t * (D / KV4_GROUP), cl, on);
-            } else {
-                float x[8];
-                pc[u].get(x);
-                if (is_k) norm_rotate<D>(x, a.k_weight, a.eps, lane, a.rotary, a.interleaved != 0, s_cos[warp], s_sin[warp]);
-                __nv_bfloat16* to = is_k ? a.K + page * a.ks_b + head * a.ks_h + off * a.ks_t : a.V + page * a.vs_b + head * a.vs_h + off * a.vs_t;
-                if (on) *reinterpret_cast<uint4*>(to + 8 * cl) = pack_bf16(x);
+                if (is_k) others(pc[u], y);
+                load(pc[u], it + u + TOK_LOADS);
+                if (is_k) turn_k.template apply<D>(x, y, a.k_weight != nullptr, a.eps);
+                if constexpr (KV4) {
+                    const Kv4Block at(a.b, D);
+                    unsigned char* blk = a.pool + page * a.ks_b + head * a.ks_h + (int64_t)(off / a.b) * a.ks_t + (is_k ? 0 : at.v_codes);
+                    const int t = off % a.b;
+                    store_kv4(x, is_k ? a.k_scale : a.v_scale, blk + t * (D / 2), blk + a.b * (D / 2) + t * (D / KV4_GROUP), cl, on);
+                } else {
+                    __nv_bfloat16* to = is_k ? a.K + page * a.ks_b + head * a.ks_h + off * a.ks_t : a.V + page * a.vs_b + head * a.vs_h + off * a.vs_t;
+                    if (on) *reinterpret_cast<uint4*>(to + 8 * cl) = pack_bf16(x);
+                }
             }
         }
     }
