@@ -6,9 +6,11 @@
 // A warp takes one row's heads two (d = 128) or four (64) at a time, a piece of eight channels per lane: a head's sum and a channel's
 // partner are shuffles away, and everything is read once and written once.
 #include <math.h>
+#include <string.h>
 
 #include <type_traits>
 
+#include "eta_attend.cuh"
 #include "eta_kv4.cuh"
 
 namespace eta {
@@ -26,7 +28,8 @@ struct TokensArgs {
     int64_t ks_b, ks_h, ks_t, vs_b, vs_h, vs_t;       // bf16 cache: elements; 4-bit: ks_* in bytes (page or sequence, head, block)
     int64_t limit;                                    // slots of the cache
     int rows, Hq, Hkv, per_page, b, parts, rotary, interleaved;
-    double k_scale, v_scale;
+    float k_scale, v_scale;
+    int fast;              // bit 0: the keys' scale is of a size that leaves fp32 its range; bit 1: the values' too, and its product with a group's is exact
     float eps;
 };
 
@@ -70,6 +73,12 @@ __device__ __forceinline__ uint4 pack_bf16(const float (&x)[8]) {
     return o;
 }
 
+// The angle of a row's pair, reduced by whole turns with a two-part 2 pi (Cody and Waite): any 32-bit position keeps its 64-bit angle
+__device__ __forceinline__ double reduced_angle(const TokensArgs& a, int64_t row, int pair) {
+    const double x = (double)__ldcg(a.positions + row) * __ldcg(a.inv_freq + pair), n = rint(x * 0.15915494309189535);
+    return fma(-n, 2.4492935982947064e-16, fma(-n, 6.283185307179586, x));
+}
+
 // What a lane's eight channels are multiplied with, norm weight and rotation in one: y = (x C + x_partner S) r, where x_partner are the pairs'
 // other channels as they came, C = w cos, S = -+ w_partner sin, and r = 1 / sqrt(mean x^2 + eps) (1 without a norm).
 template <typename F>
@@ -90,9 +99,9 @@ struct Turn {
             S[k] = turns ? (minus ? -wp : wp) * sn[pair] : (F)0;
         }
     }
-    // x: the lane's channels, y: their partners
-    template <int D>
-    __device__ __forceinline__ void apply(F (&x)[8], const F (&y)[8], bool norm, float eps) const {
+    // x: the lane's channels, y: their partners.  With m: also the sizes |x C| + |x_partner S| times r, which bound what rounding did.
+    template <int D, bool SIZES = false>
+    __device__ __forceinline__ void apply(F (&x)[8], const F (&y)[8], bool norm, float eps, F* m = nullptr) const {
         F r = 1;
         if (norm) {
             F ss = 0;
@@ -103,44 +112,128 @@ struct Turn {
             r = rsqrt(ss * (F)(1.0 / D) + (F)eps);
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = fma(x[k], C[k], y[k] * S[k]) * r;
+        for (int k = 0; k < 8; ++k) {
+            if constexpr (SIZES) {
+                const F a = x[k] * C[k], b = y[k] * S[k];
+                m[k] = (fabsf(a) + fabsf(b)) * r;
+                x[k] = (a + b) * r;
+            } else {
+                x[k] = fma(x[k], C[k], y[k] * S[k]) * r;
+            }
+        }
     }
 };
 
-// Eight channels of a row into a 4-bit block: the two lanes that hold a group agree on its scale.
-__device__ __forceinline__ void store_kv4(const double (&x)[8], double g, unsigned char* codes, unsigned char* scales, int cl, bool on) {
+// ---- Eight channels of a row as codes, and their group's scale, which the lane's neighbour agrees on: scale e4m3(max|x| / (6 g)), codes
+// e2m1(x / (scale g)), quotients rounded to fp32.
+
+struct Kv4Codes { uint32_t codes, scale; };
+
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
+    unsigned short pair;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(pair) : "f"(hi), "f"(lo));
+    return pair;
+}
+template <typename Q>
+__device__ __forceinline__ uint32_t e2m1x8(Q quotient) {
+    uint32_t bytes = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) bytes |= f32x2_to_e2m1x2(quotient(2 * k), quotient(2 * k + 1)) << (8 * k);
+    return bytes;
+}
+
+// As the definition has it, in fp64.
+__device__ __forceinline__ Kv4Codes codes_exact(const double (&x)[8], double g) {
     // (rounding is monotonic: the largest of the rounded quotients is the largest quotient rounded)
     const double sixth = 1.0 / (6.0 * g);
     float want = 0.f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) want = max_nan(want, fabsf((float)(x[k] * sixth)));
     want = max_nan(want, __shfl_xor_sync(0xffffffffu, want, 1));
-    unsigned short pair;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(pair) : "f"(0.f), "f"(want));
-    const uint32_t code = pair & 0xffu;
-    const double scale = (double)f16_lo(e4m3x2_to_f16x2(code));
-    const bool any = scale > 0;                                    // (false for a NaN too)
-    const double inv = any ? 1.0 / (scale * g) : 0.0;
-    uint32_t bytes = 0;
+    const uint32_t scale = e4m3x2(want, 0.f) & 0xffu;
+    const double s = (double)f16_lo(e4m3x2_to_f16x2(scale));
+    const bool any = s > 0;                            // (false for a NaN too)
+    const double inv = any ? 1.0 / (s * g) : 0.0;
+    return {e2m1x8([&](int k) { return any ? (float)(x[k] * inv) : 0.f; }), scale};
+}
+
+// Values as they came, where scale * g is exact in fp32 (g of at most 20 significant bits): the quotient correctly rounded from a rounded
+// reciprocal and the remainder (Markstein's division), so that ties are ties.
+__device__ __forceinline__ Kv4Codes codes_of_values(const float (&x)[8], float g) {
+    float top = 0.f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const float lo = any ? (float)(x[2 * k] * inv) : 0.f, hi = any ? (float)(x[2 * k + 1] * inv) : 0.f;
-        bytes |= f32x2_to_e2m1x2(lo, hi) << (8 * k);
+    for (int k = 0; k < 8; ++k) top = max_nan(top, fabsf(x[k]));
+    top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    const uint32_t scale = e4m3x2(__fdiv_rn(top, 6.f * g), 0.f) & 0xffu;
+    const float s = f16_lo(e4m3x2_to_f16x2(scale)), sg = s * g;
+    const bool any = s > 0.f;
+    const float inv = any ? __frcp_rn(sg) : 0.f;
+    const uint32_t codes = e2m1x8([&](int k) {
+        const float y = x[k] * inv;
+        return fabsf(y) < 8.f ? fmaf(fmaf(-y, sg, x[k]), inv, y) : y;          // (beyond 8, infinities among them, it saturates)
+    });
+    return {any ? codes : 0u, scale};
+}
+
+// Keys in fp32, each off by at most 2^-19 of its m: codes and scale where that cannot change them, else false (for the whole warp).
+__device__ __forceinline__ bool codes_of_keys(const float (&x)[8], const float (&m)[8], float g, Kv4Codes& out) {
+    constexpr float OFF = 1.f / (1 << 19), ROUND = 1.f / (1 << 22);
+    float top = 0.f, size = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { top = max_nan(top, fabsf(x[k])); size = fmaxf(size, m[k]); }
+    top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    size = fmaxf(size, __shfl_xor_sync(0xffffffffu, size, 1));
+    const float sixth = 1.f / (6.f * g), off = size * OFF + top * ROUND;
+    const uint32_t pair = e4m3x2((top - off) * sixth, (top + off) * sixth);
+    out.scale = pair & 0xffu;
+    const float s = f16_lo(e4m3x2_to_f16x2(out.scale));
+    const float inv = s > 0.f ? rcp_approx(s * g) : 0.f;
+    float e[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) e[k] = fmaf(m[k], OFF * inv, fabsf(x[k] * inv) * ROUND);
+    out.codes = e2m1x8([&](int k) { return fmaf(x[k], inv, e[k]); });
+    const uint32_t low = e2m1x8([&](int k) { return fmaf(x[k], inv, -e[k]); });
+    return __all_sync(0xffffffffu, top < 1e30f && (pair >> 8) == out.scale && low == out.codes);
+}
+
+// Token t of a tensor's codes and scales at `to`, in a block of b
+__device__ __forceinline__ void store_codes(const Kv4Codes& c, unsigned char* to, int b, int D, int t, int cl) {
+    *reinterpret_cast<uint32_t*>(to + t * (D / 2) + 4 * cl) = c.codes;
+    if ((cl & 1) == 0) to[b * (D / 2) + t * (D / KV4_GROUP) + cl / 2] = (unsigned char)c.scale;
+}
+
+// Norm and rotation of a lane's keys in fp64.  y: the channels' partners.
+template <int D>
+__device__ __forceinline__ void turn_exact(const TokensArgs& a, double (&x)[8], const double (&y)[8], int64_t row, int cl) {
+    const int reach = a.rotary / 16;
+    const bool turns = 8 * cl < a.rotary;
+    double ss = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) ss = fma(x[k], x[k], ss);
+#pragma unroll
+    for (int s = 1; s < D / 8; s <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, s);
+    const double r = a.k_weight ? rsqrt(ss * (1.0 / D) + (double)a.eps) : 1.0;
+#pragma unroll 1
+    for (int n = 0; n < 8; ++n) {
+        const int c = 8 * cl + n, pair = a.interleaved ? c / 2 : (cl < reach ? c : c - a.rotary / 2);
+        const int other = a.interleaved ? c ^ 1 : (cl < reach ? c + a.rotary / 2 : c - a.rotary / 2);
+        const bool minus = a.interleaved ? !(n & 1) : cl < reach;
+        const double w = a.k_weight ? a.k_weight[c] : 1.f, wp = a.k_weight && turns ? a.k_weight[other] : 1.f;
+        double cs = 1, sn = 0;
+        if (turns) sincos(reduced_angle(a, row, pair), &sn, &cs);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k == n) x[k] = fma(x[k], w * cs, y[k] * ((minus ? -wp : wp) * sn)) * r;
     }
-    if (!on) return;
-    *reinterpret_cast<uint32_t*>(codes + 4 * cl) = bytes;
-    if ((cl & 1) == 0) scales[cl / 2] = (unsigned char)code;
 }
 
 constexpr int TOK_WARPS = 4, TOK_LOADS = 4;       // warps of a CTA; pieces that a lane has in flight
 
 // A warp takes items (two or four heads of the row each) one after the other, four on their way at any time: queries, keys, values.
 template <typename T, int D, bool KV4>
-__global__ void __launch_bounds__(32 * TOK_WARPS, (sizeof(T) == 4 ? 4 : 5) - (KV4 ? 1 : 0)) append_tokens_kernel(const TokensArgs a) {
-    using F = typename std::conditional<KV4, double, float>::type;       // what keys are worked out in
+__global__ void __launch_bounds__(32 * TOK_WARPS, sizeof(T) == 4 ? 4 : 5) append_tokens_kernel(const __grid_constant__ TokensArgs a) {
     constexpr int LPH = D / 8, HPW = 32 / LPH;         // lanes of a head, heads of a warp
-    __shared__ F s_cos[TOK_WARPS][D / 2], s_sin[TOK_WARPS][D / 2];
-    __shared__ float s_cosf[KV4 ? TOK_WARPS : 1][D / 2], s_sinf[KV4 ? TOK_WARPS : 1][D / 2];
+    __shared__ float s_cos[TOK_WARPS][D / 2], s_sin[TOK_WARPS][D / 2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     pdl_wait();
     const int64_t wid = (int64_t)blockIdx.x * TOK_WARPS + warp;
@@ -166,25 +259,11 @@ __global__ void __launch_bounds__(32 * TOK_WARPS, (sizeof(T) == 4 ? 4 : 5) - (KV
     };
 #pragma unroll
     for (int u = 0; u < TOK_LOADS; ++u) load(pc[u], begin + u);
-    // ---- the row's angles, reduced by whole turns with a two-part 2 pi (Cody and Waite): any 32-bit position keeps its 64-bit angle
+    // ---- the row's angles
     if (a.rotary && begin < nq + nkv) {
-        const double pos = (double)__ldcg(a.positions + row);
-        for (int c = lane; c < a.rotary / 2; c += 32) {
-            const double x = pos * __ldcg(a.inv_freq + c), n = rint(x * 0.15915494309189535);
-            const double r = fma(-n, 2.4492935982947064e-16, fma(-n, 6.283185307179586, x));
-            F sn, cs;
-            if constexpr (KV4) {
-                sincos(r, &sn, &cs);
-                s_cosf[warp][c] = (float)cs; s_sinf[warp][c] = (float)sn;
-            } else {
-                sincosf((float)r, &sn, &cs);
-            }
-            s_cos[warp][c] = cs; s_sin[warp][c] = sn;
-        }
+        for (int c = lane; c < a.rotary / 2; c += 32) sincosf((float)reduced_angle(a, row, c), &s_sin[warp][c], &s_cos[warp][c]);
         __syncwarp();
     }
-    const float *const csf = KV4 ? s_cosf[KV4 ? warp : 0] : reinterpret_cast<const float*>(s_cos[warp]),
-                *const snf = KV4 ? s_sinf[KV4 ? warp : 0] : reinterpret_cast<const float*>(s_sin[warp]);
     const int64_t page = slot / a.per_page;
     const int off = (int)(slot - page * a.per_page);
     // the pairs' other halves are in lane `partner`, or in the lane's own neighbours
@@ -204,7 +283,7 @@ __global__ void __launch_bounds__(32 * TOK_WARPS, (sizeof(T) == 4 ? 4 : 5) - (KV
         }
     };
     Turn<float> turn;
-    if (begin < nq) turn.template set<D>(a.q_weight, cl, a.rotary, a.interleaved != 0, csf, snf);
+    if (begin < nq) turn.template set<D>(a.q_weight, cl, a.rotary, a.interleaved != 0, s_cos[warp], s_sin[warp]);
     // ---- queries
     int it = begin;
     for (; it < end && it < nq; it += TOK_LOADS) {
@@ -221,10 +300,14 @@ __global__ void __launch_bounds__(32 * TOK_WARPS, (sizeof(T) == 4 ? 4 : 5) - (KV
             }
         }
     }
+    // where a head's codes of this row's block are
+    auto place = [&](bool is_k, int head) {
+        return a.pool + page * a.ks_b + head * a.ks_h + (int64_t)(off / a.b) * a.ks_t + (is_k ? 0 : Kv4Block(a.b, D).v_codes);
+    };
+    uint64_t left = 0;                                 // items that fp32 did not settle (bit 63: one of those from there on)
     // ---- keys and values
-    Turn<F> turn_k;
     const int first = max(begin, nq);                  // pieces of these items are in the slots that follow the queries'
-    if (first < end && first < nq + nkv) turn_k.template set<D>(a.k_weight, cl, a.rotary, a.interleaved != 0, s_cos[warp], s_sin[warp]);
+    if (first < end && first < nq + nkv) turn.template set<D>(a.k_weight, cl, a.rotary, a.interleaved != 0, s_cos[warp], s_sin[warp]);
     for (it = first - (first - begin) % TOK_LOADS; it < end; it += TOK_LOADS) {
 #pragma unroll
         for (int u = 0; u < TOK_LOADS; ++u) {
@@ -232,21 +315,49 @@ __global__ void __launch_bounds__(32 * TOK_WARPS, (sizeof(T) == 4 ? 4 : 5) - (KV
                 const bool is_k = it + u < nq + nkv;
                 const int head = (is_k ? it + u - nq : it + u - nq - nkv) * HPW + hl;
                 const bool on = head < a.Hkv;
-                F x[8], y[8];
+                float x[8], y[8];
                 pc[u].get(x);
                 if (is_k) others(pc[u], y);
                 load(pc[u], it + u + TOK_LOADS);
-                if (is_k) turn_k.template apply<D>(x, y, a.k_weight != nullptr, a.eps);
                 if constexpr (KV4) {
-                    const Kv4Block at(a.b, D);
-                    unsigned char* blk = a.pool + page * a.ks_b + head * a.ks_h + (int64_t)(off / a.b) * a.ks_t + (is_k ? 0 : at.v_codes);
-                    const int t = off % a.b;
-                    store_kv4(x, is_k ? a.k_scale : a.v_scale, blk + t * (D / 2), blk + a.b * (D / 2) + t * (D / KV4_GROUP), cl, on);
+                    Kv4Codes c;
+                    bool settled;
+                    if (is_k) {
+                        float m[8];
+                        turn.template apply<D, true>(x, y, a.k_weight != nullptr, a.eps, m);
+                        settled = codes_of_keys(x, m, a.k_scale, c) && (a.fast & 1);
+                    } else {
+                        c = codes_of_values(x, a.v_scale);
+                        settled = (a.fast & 2) != 0;
+                    }
+                    if (settled) {
+                        if (on) store_codes(c, place(is_k, head), a.b, D, off % a.b, cl);
+                    } else {
+                        left |= 1ull << min(it + u - first, 63);
+                    }
                 } else {
+                    if (is_k) turn.template apply<D>(x, y, a.k_weight != nullptr, a.eps);
                     __nv_bfloat16* to = is_k ? a.K + page * a.ks_b + head * a.ks_h + off * a.ks_t : a.V + page * a.vs_b + head * a.vs_h + off * a.vs_t;
                     if (on) *reinterpret_cast<uint4*>(to + 8 * cl) = pack_bf16(x);
                 }
             }
+        }
+    }
+    if constexpr (KV4) {
+        // ---- what lies too near a border between two codes for fp32, about one item in a hundred, once more in fp64
+        for (it = first; left != 0 && it < end; ++it) {
+            if (((left >> min(it - first, 63)) & 1) == 0) continue;
+            const bool is_k = it < nq + nkv;
+            const int head = (is_k ? it - nq : it - nq - nkv) * HPW + hl;
+            double x[8], y[8];
+            load(pc[0], it);
+            pc[0].get(x);
+            if (is_k) {
+                others(pc[0], y);
+                turn_exact<D>(a, x, y, row, cl);
+            }
+            const Kv4Codes c = codes_exact(x, is_k ? a.k_scale : a.v_scale);
+            if (head < a.Hkv) store_codes(c, place(is_k, head), a.b, D, off % a.b, cl);
         }
     }
 }
@@ -347,6 +458,10 @@ static int append_tokens(const eta_cache_desc* desc, const eta_kv4_desc* kv4, co
     a.vs_b = desc->v_stride_b; a.vs_h = desc->v_stride_h; a.vs_t = desc->v_stride_t;
     if (kv4) { a.ks_b = kv4->stride_b; a.ks_h = kv4->stride_h; a.ks_t = n_pages > 0 ? 0 : kv4->stride_j; }
     a.k_scale = kv4 ? kv4->k_scale : 1; a.v_scale = kv4 ? kv4->v_scale : 1;
+    const auto plain_size = [](float g) { return g >= 0x1p-60f && g <= 0x1p60f; };
+    uint32_t v_bits;
+    memcpy(&v_bits, &a.v_scale, 4);
+    a.fast = (plain_size(a.k_scale) ? 1 : 0) | (plain_size(a.v_scale) && (v_bits & 0xfu) == 0 ? 2 : 0);
     a.per_page = n_pages > 0 ? desc->block_size : desc->t_cap;
     a.limit = (int64_t)a.per_page * (n_pages > 0 ? n_pages : desc->batch);
     a.rows = tok->n_rows; a.Hq = desc->n_q_heads; a.Hkv = desc->n_kv_heads; a.b = desc->block_size;
