@@ -3,8 +3,8 @@
 //
 //   y = x * w / sqrt(mean_c x_c^2 + eps);   (a, b) -> (a cos - b sin, a sin + b cos),  angle = position * inv_freq
 //
-// A warp takes one row's heads two (d = 128) or four (64) at a time, a piece of eight channels per lane: a head's sum and a channel's
-// partner are shuffles away, and everything is read once and written once.
+// A warp takes a row's heads two (d = 128) or four (64) at a time, eight channels per lane, so that a head's sum is a few shuffles away;
+// everything is read once and written once.  Bound by the instructions per element where rows are many, by latency where they are few.
 #include <math.h>
 #include <string.h>
 
@@ -27,9 +27,10 @@ struct TokensArgs {
     int64_t q_sr, q_sh, k_sr, k_sh, v_sr, v_sh;       // elements
     int64_t ks_b, ks_h, ks_t, vs_b, vs_h, vs_t;       // bf16 cache: elements; 4-bit: ks_* in bytes (page or sequence, head, block)
     int64_t limit;                                    // slots of the cache
-    int rows, Hq, Hkv, per_page, b, parts, rotary, interleaved;
+    int rows, Hq, Hkv, per_page, b, q_parts, kv_parts, rotary, interleaved;
+    FastDiv div_page;
     float k_scale, v_scale;
-    int fast;              // bit 0: the keys' scale is of a size that leaves fp32 its range; bit 1: the values' too, and its product with a group's is exact
+    int fast;              // bit 0, 1: the keys', the values' scale leaves fp32 its range, and its product with a group's is exact (20 bits)
     float eps;
 };
 
@@ -175,31 +176,31 @@ __device__ __forceinline__ Kv4Codes codes_of_values(const float (&x)[8], float g
     return {any ? codes : 0u, scale};
 }
 
-// Keys in fp32, each off by at most 2^-19 of its m: codes and scale where that cannot change them, else false (for the whole warp).
-__device__ __forceinline__ bool codes_of_keys(const float (&x)[8], const float (&m)[8], float g, Kv4Codes& out) {
+// Keys in fp32, each off by at most 2^-19 of its m: codes and scale where that cannot change them, else false (for the whole warp).  `touched`: the
+// lane's keys were normed or rotated; those that were not are as exact as they came, and divided as values are.
+__device__ __forceinline__ bool codes_of_keys(const float (&x)[8], const float (&m)[8], float g, bool touched, Kv4Codes& out) {
     constexpr float OFF = 1.f / (1 << 19), ROUND = 1.f / (1 << 22);
     float top = 0.f, size = 0.f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) { top = max_nan(top, fabsf(x[k])); size = fmaxf(size, m[k]); }
     top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    size = fmaxf(size, __shfl_xor_sync(0xffffffffu, size, 1));
-    const float sixth = 1.f / (6.f * g), off = size * OFF + top * ROUND;
-    const uint32_t pair = e4m3x2((top - off) * sixth, (top + off) * sixth);
+    size = fmaxf(touched ? size : 0.f, __shfl_xor_sync(0xffffffffu, touched ? size : 0.f, 1));
+    const float off = size > 0.f ? fmaf(size, OFF, top * ROUND) : 0.f, six = 6.f * g;
+    const uint32_t pair = e4m3x2(__fdiv_rn(top - off, six), __fdiv_rn(top + off, six));
     out.scale = pair & 0xffu;
-    const float s = f16_lo(e4m3x2_to_f16x2(out.scale));
-    const float inv = s > 0.f ? rcp_approx(s * g) : 0.f;
-    float e[8];
+    const float s = f16_lo(e4m3x2_to_f16x2(out.scale)), sg = s * g;
+    const bool any = s > 0.f;
+    const float inv = any ? __frcp_rn(sg) : 0.f, off_y = touched ? OFF * inv : 0.f, round_y = touched ? ROUND : 0.f;
+    float y[8], e[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) e[k] = fmaf(m[k], OFF * inv, fabsf(x[k] * inv) * ROUND);
-    out.codes = e2m1x8([&](int k) { return fmaf(x[k], inv, e[k]); });
-    const uint32_t low = e2m1x8([&](int k) { return fmaf(x[k], inv, -e[k]); });
+    for (int k = 0; k < 8; ++k) {
+        y[k] = x[k] * inv;
+        y[k] = fabsf(y[k]) < 8.f ? fmaf(fmaf(-y[k], sg, x[k]), inv, y[k]) : y[k];
+        e[k] = fmaf(m[k], off_y, fabsf(y[k]) * round_y);
+    }
+    out.codes = any ? e2m1x8([&](int k) { return y[k] + e[k]; }) : 0u;
+    const uint32_t low = any ? e2m1x8([&](int k) { return y[k] - e[k]; }) : 0u;
     return __all_sync(0xffffffffu, top < 1e30f && (pair >> 8) == out.scale && low == out.codes);
-}
-
-// Token t of a tensor's codes and scales at `to`, in a block of b
-__device__ __forceinline__ void store_codes(const Kv4Codes& c, unsigned char* to, int b, int D, int t, int cl) {
-    *reinterpret_cast<uint32_t*>(to + t * (D / 2) + 4 * cl) = c.codes;
-    if ((cl & 1) == 0) to[b * (D / 2) + t * (D / KV4_GROUP) + cl / 2] = (unsigned char)c.scale;
 }
 
 // Norm and rotation of a lane's keys in fp64.  y: the channels' partners.
@@ -227,18 +228,132 @@ __device__ __forceinline__ void turn_exact(const TokensArgs& a, double (&x)[8], 
     }
 }
 
-constexpr int TOK_WARPS = 4, TOK_LOADS = 4;       // warps of a CTA; pieces that a lane has in flight
+constexpr int TOK_WARPS = 4, TOK_LOADS = 4;       // warps of a CTA; items that a warp has on their way
 
-// A warp takes items (two or four heads of the row each) one after the other, four on their way at any time: queries, keys, values.
+// Four consecutive channels
+template <typename T>
+struct Quad {
+    uint32_t w[sizeof(T)];
+    __device__ __forceinline__ void load(const T* p, bool on) {
+        if constexpr (sizeof(T) == 4) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (on) v = __ldcg(reinterpret_cast<const uint4*>(p));
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else {
+            uint2 v = make_uint2(0, 0);
+            if (on) v = __ldcg(reinterpret_cast<const uint2*>(p));
+            w[0] = v.x; w[1] = v.y;
+        }
+    }
+    __device__ __forceinline__ void get(float (&x)[4]) const {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if constexpr (sizeof(T) == 4) x[k] = __uint_as_float(w[k]);
+            else if constexpr (std::is_same<T, __half>::value) x[k] = (k & 1) ? f16_hi(w[k / 2]) : f16_lo(w[k / 2]);
+            else x[k] = (k & 1) ? bf16_hi(w[k / 2]) : bf16_lo(w[k / 2]);
+        }
+    }
+};
+
+// A row's queries.  A lane takes four pairs of a head: channels ca .. ca + 3 and their partners cb .. cb + 3 (interleaved: two times two pairs of
+// neighbours), so that no channel travels between lanes; y = (x C + x_partner S) r, two channels an instruction.
+template <typename T, int D, bool INTER>
+__device__ __forceinline__ void queries(const TokensArgs& a, int64_t row, int begin, int end, int lane, float* cs, float* sn) {
+    constexpr int LPH = D / 8, HPW = 32 / LPH;
+    const int hl = lane / LPH, p = 4 * (lane % LPH), half = a.rotary / 2, nq = (a.Hq + HPW - 1) / HPW;
+    const bool turns = INTER ? 2 * p < a.rotary : p < half;
+    const int ca = INTER ? 2 * p : (turns ? p : half + p), cb = ca + (INTER ? 4 : (turns ? half : D / 2 - half));
+    const bool in_last = (nq - 1) * HPW + hl < a.Hq;       // the last item may have fewer heads
+    const int64_t step = HPW * a.q_sh;
+    const T* from = static_cast<const T*>(a.q) + row * a.q_sr + hl * a.q_sh + begin * step + ca;
+    __nv_bfloat16* to = a.q_out + (row * a.Hq + begin * HPW + hl) * D + ca;
+    Quad<T> qa[TOK_LOADS], qb[TOK_LOADS];
+    auto load = [&](int u, int it) {
+        if (it >= end) return;
+        const bool on = it < nq - 1 || in_last;
+        qa[u].load(from, on);
+        qb[u].load(from + (cb - ca), on);
+        from += step;
+    };
+#pragma unroll
+    for (int u = 0; u < TOK_LOADS; ++u) load(u, begin + u);
+    if (a.rotary) {
+        for (int c = lane; c < half; c += 32) sincosf((float)reduced_angle(a, row, c), sn + c, cs + c);
+        __syncwarp();
+    }
+    float C[8], S[8];
+    {
+        const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
+        const float4 wa = a.q_weight ? *reinterpret_cast<const float4*>(a.q_weight + ca) : one, wb = a.q_weight ? *reinterpret_cast<const float4*>(a.q_weight + cb) : one;
+        const float4 c4 = *reinterpret_cast<const float4*>(cs + p), s4 = *reinterpret_cast<const float4*>(sn + p);
+        const float w[8] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w}, cv[4] = {c4.x, c4.y, c4.z, c4.w}, sv[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int pair = INTER ? k / 2 : k % 4;
+            const bool minus = INTER ? !(k & 1) : k < 4;
+            const float wp = w[INTER ? k ^ 1 : k ^ 4];
+            C[k] = turns ? w[k] * cv[pair] : w[k];
+            S[k] = turns ? (minus ? -wp : wp) * sv[pair] : 0.f;
+        }
+    }
+    const bool some_stay = a.rotary < D;
+#pragma unroll 1
+    for (int it = begin; it < end; it += TOK_LOADS) {
+#pragma unroll
+        for (int u = 0; u < TOK_LOADS; ++u) {
+            if (it + u >= end) break;                  // the same for the whole warp
+            float x[8], y[8], r = 1.f;
+            {
+                float x0[4], x1[4];
+                qa[u].get(x0);
+                qb[u].get(x1);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) { x[k] = x0[k]; x[4 + k] = x1[k]; }
+            }
+            load(u, it + u + TOK_LOADS);
+            if (a.q_weight) {
+                float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; k += 2) fma2(s0, s1, x[k], x[k + 1], x[k], x[k + 1]);
+                float ss = s0 + s1;
+#pragma unroll
+                for (int n = 1; n < LPH; n <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, n);
+                r = rsqrtf(ss * (1.f / D) + a.eps);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) y[k] = x[INTER ? k ^ 1 : k ^ 4];
+            if (some_stay && !turns) {                 // channels that do not turn have no part in anything: not even an infinity times 0
+#pragma unroll
+                for (int k = 0; k < 8; ++k) y[k] = 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+                float t0, t1;
+                mul2(t0, t1, y[k], y[k + 1], S[k], S[k + 1]);
+                fma2(t0, t1, x[k], x[k + 1], C[k], C[k + 1]);
+                mul2(x[k], x[k + 1], t0, t1, r, r);
+            }
+            if (it + u < nq - 1 || in_last) {
+                const uint4 o = pack_bf16(x);
+                *reinterpret_cast<uint2*>(to) = make_uint2(o.x, o.y);
+                *reinterpret_cast<uint2*>(to + (cb - ca)) = make_uint2(o.z, o.w);
+            }
+            to += HPW * D;
+        }
+    }
+}
+
+// A warp takes a part of a row's queries, or of its keys and values, an item (two or four heads) after the other, four on their way at any time.
 template <typename T, int D, bool KV4>
 __global__ void __launch_bounds__(32 * TOK_WARPS, sizeof(T) == 4 ? 4 : 5) append_tokens_kernel(const __grid_constant__ TokensArgs a) {
     constexpr int LPH = D / 8, HPW = 32 / LPH;         // lanes of a head, heads of a warp
-    __shared__ float s_cos[TOK_WARPS][D / 2], s_sin[TOK_WARPS][D / 2];
+    __shared__ __align__(16) float s_cos[TOK_WARPS][D / 2], s_sin[TOK_WARPS][D / 2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     pdl_wait();
     const int64_t wid = (int64_t)blockIdx.x * TOK_WARPS + warp;
-    const int64_t row = wid / a.parts;
-    const int part = (int)(wid % a.parts);
+    const int parts = a.q_parts + a.kv_parts;
+    const int64_t row = wid / parts;
+    const int part = (int)(wid - row * parts);
     if (row >= a.rows) return;
     const int64_t slot = __ldcg(reinterpret_cast<const long long*>(a.slot_map) + row);
     if (slot < 0) return;
@@ -246,29 +361,47 @@ __global__ void __launch_bounds__(32 * TOK_WARPS, sizeof(T) == 4 ? 4 : 5) append
         if (lane == 0 && part == 0 && a.status) atomicOr(a.status, ETA_DEV_BAD_SLOT);
         return;
     }
-    const int nq = (a.Hq + HPW - 1) / HPW, nkv = (a.Hkv + HPW - 1) / HPW, all = nq + 2 * nkv;
-    const int begin = part * all / a.parts, end = (part + 1) * all / a.parts;
-    const int hl = lane / LPH, cl = lane % LPH;
-    const T *const q = static_cast<const T*>(a.q) + row * a.q_sr + 8 * cl, *const k = static_cast<const T*>(a.k) + row * a.k_sr + 8 * cl,
-            *const v = static_cast<const T*>(a.v) + row * a.v_sr + 8 * cl;
-    Piece<T> pc[TOK_LOADS];
-    auto load = [&](Piece<T>& p, int it) {
-        const bool is_q = it < nq, is_k = it < nq + nkv;
-        const int head = (is_q ? it : (is_k ? it - nq : it - nq - nkv)) * HPW + hl;
-        p.load(is_q ? q + head * a.q_sh : (is_k ? k + head * a.k_sh : v + head * a.v_sh), it < end && head < (is_q ? a.Hq : a.Hkv));
-    };
-#pragma unroll
-    for (int u = 0; u < TOK_LOADS; ++u) load(pc[u], begin + u);
-    // ---- the row's angles
-    if (a.rotary && begin < nq + nkv) {
-        for (int c = lane; c < a.rotary / 2; c += 32) sincosf((float)reduced_angle(a, row, c), &s_sin[warp][c], &s_cos[warp][c]);
-        __syncwarp();
+    if (part < a.q_parts) {
+        const int nq = (a.Hq + HPW - 1) / HPW, begin = part * nq / a.q_parts, end = (part + 1) * nq / a.q_parts;
+        if (a.interleaved) queries<T, D, true>(a, row, begin, end, lane, s_cos[warp], s_sin[warp]);
+        else queries<T, D, false>(a, row, begin, end, lane, s_cos[warp], s_sin[warp]);
+        return;
     }
-    const int64_t page = slot / a.per_page;
-    const int off = (int)(slot - page * a.per_page);
+    // ---- keys, then values: a lane holds eight consecutive channels, so that two lanes hold a group of the 4-bit cache
+    const int nkv = (a.Hkv + HPW - 1) / HPW, begin = (part - a.q_parts) * 2 * nkv / a.kv_parts, end = (part - a.q_parts + 1) * 2 * nkv / a.kv_parts;
+    const int hl = lane / LPH, cl = lane % LPH;
+    const bool in_last = (nkv - 1) * HPW + hl < a.Hkv;     // the last item may have fewer heads
+    int64_t page;
+    int off;
+    if (a.limit <= INT32_MAX) { int p32; a.div_page.divmod((int)slot, p32, off); page = p32; }
+    else { page = slot / a.per_page; off = (int)(slot - page * a.per_page); }
+    // items first .. last - 1 of a tensor, four on their way: use(piece, item, whether the lane has a head of it)
+    auto stream = [&](const void* tensor, int64_t sr, int64_t sh, int first, int last, auto&& use) {
+        const T* from = static_cast<const T*>(tensor) + row * sr + (first * HPW + hl) * sh + 8 * cl;
+        const int64_t step = HPW * sh;
+        Piece<T> pc[TOK_LOADS];
+        auto load = [&](int u, int it) {
+            if (it >= last) return;
+            pc[u].load(from, it < nkv - 1 || in_last);
+            from += step;
+        };
+#pragma unroll
+        for (int u = 0; u < TOK_LOADS; ++u) load(u, first + u);
+#pragma unroll 1
+        for (int it = first; it < last; it += TOK_LOADS) {
+#pragma unroll
+            for (int u = 0; u < TOK_LOADS; ++u) {
+                if (it + u >= last) break;                 // the same for the whole warp
+                const Piece<T> now = pc[u];
+                load(u, it + u + TOK_LOADS);
+                use(now, it + u, it + u < nkv - 1 || in_last);
+            }
+        }
+    };
     // the pairs' other halves are in lane `partner`, or in the lane's own neighbours
     const int reach = a.rotary / 16;
-    const int partner = a.interleaved || 8 * cl >= a.rotary ? lane : (cl < reach ? lane + reach : lane - reach);
+    const bool turns = 8 * cl < a.rotary;
+    const int partner = a.interleaved || !turns ? lane : (cl < reach ? lane + reach : lane - reach);
     auto others = [&](const Piece<T>& p, auto& y) {
         Piece<T> o = p;
         if (a.rotary && !a.interleaved) o.exchange(partner);
@@ -277,87 +410,85 @@ __global__ void __launch_bounds__(32 * TOK_WARPS, sizeof(T) == 4 ? 4 : 5) append
 #pragma unroll
             for (int c = 0; c < 8; c += 2) { const auto t = y[c]; y[c] = y[c + 1]; y[c + 1] = t; }
         }
-        if (a.rotary < D && 8 * cl >= a.rotary) {      // channels that do not turn have no part in anything: not even an infinity times 0
+        if (a.rotary < D && !turns) {
 #pragma unroll
             for (int c = 0; c < 8; ++c) y[c] = 0;
         }
     };
+    const int k0 = min(begin, nkv), k1 = min(end, nkv), v0 = max(begin, nkv) - nkv, v1 = max(end, nkv) - nkv;
     Turn<float> turn;
-    if (begin < nq) turn.template set<D>(a.q_weight, cl, a.rotary, a.interleaved != 0, s_cos[warp], s_sin[warp]);
-    // ---- queries
-    int it = begin;
-    for (; it < end && it < nq; it += TOK_LOADS) {
-#pragma unroll
-        for (int u = 0; u < TOK_LOADS; ++u) {
-            if (it + u < end && it + u < nq) {         // the same for the whole warp
-                float x[8], y[8];
-                pc[u].get(x);
-                others(pc[u], y);
-                load(pc[u], it + u + TOK_LOADS);
-                turn.template apply<D>(x, y, a.q_weight != nullptr, a.eps);
-                const int head = (it + u) * HPW + hl;
-                if (head < a.Hq) *reinterpret_cast<uint4*>(a.q_out + (row * a.Hq + head) * D + 8 * cl) = pack_bf16(x);
-            }
+    if (k0 < k1) {
+        if (a.rotary) {
+            for (int c = lane; c < a.rotary / 2; c += 32) sincosf((float)reduced_angle(a, row, c), &s_sin[warp][c], &s_cos[warp][c]);
+            __syncwarp();
         }
+        turn.template set<D>(a.k_weight, cl, a.rotary, a.interleaved != 0, s_cos[warp], s_sin[warp]);
     }
-    // where a head's codes of this row's block are
-    auto place = [&](bool is_k, int head) {
-        return a.pool + page * a.ks_b + head * a.ks_h + (int64_t)(off / a.b) * a.ks_t + (is_k ? 0 : Kv4Block(a.b, D).v_codes);
-    };
-    uint64_t left = 0;                                 // items that fp32 did not settle (bit 63: one of those from there on)
-    // ---- keys and values
-    const int first = max(begin, nq);                  // pieces of these items are in the slots that follow the queries'
-    if (first < end && first < nq + nkv) turn.template set<D>(a.k_weight, cl, a.rotary, a.interleaved != 0, s_cos[warp], s_sin[warp]);
-    for (it = first - (first - begin) % TOK_LOADS; it < end; it += TOK_LOADS) {
-#pragma unroll
-        for (int u = 0; u < TOK_LOADS; ++u) {
-            if (it + u >= first && it + u < end) {
-                const bool is_k = it + u < nq + nkv;
-                const int head = (is_k ? it + u - nq : it + u - nq - nkv) * HPW + hl;
-                const bool on = head < a.Hkv;
-                float x[8], y[8];
-                pc[u].get(x);
-                if (is_k) others(pc[u], y);
-                load(pc[u], it + u + TOK_LOADS);
-                if constexpr (KV4) {
-                    Kv4Codes c;
-                    bool settled;
-                    if (is_k) {
-                        float m[8];
-                        turn.template apply<D, true>(x, y, a.k_weight != nullptr, a.eps, m);
-                        settled = codes_of_keys(x, m, a.k_scale, c) && (a.fast & 1);
-                    } else {
-                        c = codes_of_values(x, a.v_scale);
-                        settled = (a.fast & 2) != 0;
-                    }
-                    if (settled) {
-                        if (on) store_codes(c, place(is_k, head), a.b, D, off % a.b, cl);
-                    } else {
-                        left |= 1ull << min(it + u - first, 63);
-                    }
-                } else {
-                    if (is_k) turn.template apply<D>(x, y, a.k_weight != nullptr, a.eps);
-                    __nv_bfloat16* to = is_k ? a.K + page * a.ks_b + head * a.ks_h + off * a.ks_t : a.V + page * a.vs_b + head * a.vs_h + off * a.vs_t;
-                    if (on) *reinterpret_cast<uint4*>(to + 8 * cl) = pack_bf16(x);
-                }
+    if constexpr (!KV4) {
+        const int64_t kb = page * a.ks_b + (int64_t)off * a.ks_t + 8 * cl, vb = page * a.vs_b + (int64_t)off * a.vs_t + 8 * cl;
+        stream(a.k, a.k_sr, a.k_sh, k0, k1, [&](const Piece<T>& p, int it, bool on) {
+            float x[8], y[8];
+            p.get(x);
+            others(p, y);
+            turn.template apply<D>(x, y, a.k_weight != nullptr, a.eps);
+            if (on) *reinterpret_cast<uint4*>(a.K + kb + (it * HPW + hl) * a.ks_h) = pack_bf16(x);
+        });
+        stream(a.v, a.v_sr, a.v_sh, v0, v1, [&](const Piece<T>& p, int it, bool on) {
+            float x[8];
+            p.get(x);
+            if (on) *reinterpret_cast<uint4*>(a.V + vb + (it * HPW + hl) * a.vs_h) = pack_bf16(x);
+        });
+    } else {
+        // this row's codes in a head's block: byte of the codes, and of the scale that the pair of lanes holds
+        const int b_shift = a.b == 32 ? 5 : (a.b == 64 ? 6 : 7), t = off & (a.b - 1);
+        unsigned char* const base = a.pool + page * a.ks_b + (int64_t)(off >> b_shift) * a.ks_t;
+        const int c_at = t * (D / 2) + 4 * cl, s_at = a.b * (D / 2) + t * (D / KV4_GROUP) + cl / 2;
+        auto store = [&](const Kv4Codes& c, int tensor_at, int it) {
+            unsigned char* const to = base + (it * HPW + hl) * a.ks_h + tensor_at;
+            *reinterpret_cast<uint32_t*>(to + c_at) = c.codes;
+            if ((cl & 1) == 0) to[s_at] = (unsigned char)c.scale;
+        };
+        const int v_at = Kv4Block(a.b, D).v_codes;
+        uint64_t left = 0;                                 // keys that fp32 did not settle (bit 63: one of those from there on)
+        stream(a.k, a.k_sr, a.k_sh, k0, k1, [&](const Piece<T>& p, int it, bool on) {
+            float x[8], y[8], m[8];
+            p.get(x);
+            others(p, y);
+            turn.template apply<D, true>(x, y, a.k_weight != nullptr, a.eps, m);
+            Kv4Codes c;
+            if (codes_of_keys(x, m, a.k_scale, turns || a.k_weight, c) && (a.fast & 1)) {
+                if (on) store(c, 0, it);
+            } else {
+                left |= 1ull << min(it - k0, 63);
             }
+        });
+        if (a.fast & 2) {
+            stream(a.v, a.v_sr, a.v_sh, v0, v1, [&](const Piece<T>& p, int it, bool on) {
+                float x[8];
+                p.get(x);
+                const Kv4Codes c = codes_of_values(x, a.v_scale);
+                if (on) store(c, v_at, it);
+            });
+        } else {
+            stream(a.v, a.v_sr, a.v_sh, v0, v1, [&](const Piece<T>& p, int it, bool on) {
+                double x[8];
+                p.get(x);
+                const Kv4Codes c = codes_exact(x, a.v_scale);
+                if (on) store(c, v_at, it);
+            });
         }
-    }
-    if constexpr (KV4) {
-        // ---- what lies too near a border between two codes for fp32, about one item in a hundred, once more in fp64
-        for (it = first; left != 0 && it < end; ++it) {
-            if (((left >> min(it - first, 63)) & 1) == 0) continue;
-            const bool is_k = it < nq + nkv;
-            const int head = (is_k ? it - nq : it - nq - nkv) * HPW + hl;
+        // what lies too near a border between two codes for fp32, about one item in a hundred, once more in fp64
+        for (int it = k0; left != 0 && it < k1; ++it) {
+            if (((left >> min(it - k0, 63)) & 1) == 0) continue;
+            const bool on = it < nkv - 1 || in_last;
+            Piece<T> p;
+            p.load(static_cast<const T*>(a.k) + row * a.k_sr + (it * HPW + hl) * a.k_sh + 8 * cl, on);
             double x[8], y[8];
-            load(pc[0], it);
-            pc[0].get(x);
-            if (is_k) {
-                others(pc[0], y);
-                turn_exact<D>(a, x, y, row, cl);
-            }
-            const Kv4Codes c = codes_exact(x, is_k ? a.k_scale : a.v_scale);
-            if (head < a.Hkv) store_codes(c, place(is_k, head), a.b, D, off % a.b, cl);
+            p.get(x);
+            others(p, y);
+            turn_exact<D>(a, x, y, row, cl);
+            const Kv4Codes c = codes_exact(x, a.k_scale);
+            if (on) store(c, 0, it);
         }
     }
 }
@@ -458,21 +589,27 @@ static int append_tokens(const eta_cache_desc* desc, const eta_kv4_desc* kv4, co
     a.vs_b = desc->v_stride_b; a.vs_h = desc->v_stride_h; a.vs_t = desc->v_stride_t;
     if (kv4) { a.ks_b = kv4->stride_b; a.ks_h = kv4->stride_h; a.ks_t = n_pages > 0 ? 0 : kv4->stride_j; }
     a.k_scale = kv4 ? kv4->k_scale : 1; a.v_scale = kv4 ? kv4->v_scale : 1;
-    const auto plain_size = [](float g) { return g >= 0x1p-60f && g <= 0x1p60f; };
-    uint32_t v_bits;
-    memcpy(&v_bits, &a.v_scale, 4);
-    a.fast = (plain_size(a.k_scale) ? 1 : 0) | (plain_size(a.v_scale) && (v_bits & 0xfu) == 0 ? 2 : 0);
+    const auto plain = [](float g) {
+        uint32_t bits;
+        memcpy(&bits, &g, 4);
+        return g >= 0x1p-60f && g <= 0x1p60f && (bits & 0xfu) == 0;
+    };
+    a.fast = (plain(a.k_scale) ? 1 : 0) | (plain(a.v_scale) ? 2 : 0);
     a.per_page = n_pages > 0 ? desc->block_size : desc->t_cap;
     a.limit = (int64_t)a.per_page * (n_pages > 0 ? n_pages : desc->batch);
     a.rows = tok->n_rows; a.Hq = desc->n_q_heads; a.Hkv = desc->n_kv_heads; a.b = desc->block_size;
     a.rotary = tok->rotary_dim; a.interleaved = (tok->flags & ETA_TOKENS_INTERLEAVED) != 0;
     a.eps = tok->eps;
-    // A row is one warp's work where there are rows enough to fill the GPU, and split as far as it goes where there are not.
+    a.div_page = FastDiv(a.per_page);
+    // Two warps to a row, one for its queries, one for its keys and values, where there are rows enough to fill the GPU; as many as
+    // there are items where there are not.
     const int per_warp = 32 / (desc->head_dim / 8);
-    const int items = (a.Hq + per_warp - 1) / per_warp + 2 * ((a.Hkv + per_warp - 1) / per_warp);
+    const int q_items = (a.Hq + per_warp - 1) / per_warp, kv_items = 2 * ((a.Hkv + per_warp - 1) / per_warp);
     const int64_t want = ((int64_t)148 * 16 + a.rows - 1) / a.rows;
-    a.parts = (int)(want > items ? items : want);
-    const int64_t ctas = ((int64_t)a.rows * a.parts + TOK_WARPS - 1) / TOK_WARPS;
+    a.q_parts = (int)(want / 2 < 1 ? 1 : (want / 2 > q_items ? q_items : want / 2));
+    a.kv_parts = (int)(want / 2 < 1 ? 1 : (want / 2 > kv_items ? kv_items : want / 2));
+    const int64_t ctas = ((int64_t)a.rows * (a.q_parts + a.kv_parts) + TOK_WARPS - 1) / TOK_WARPS;
+    if (ctas > INT32_MAX) return ETA_ERR_UNSUPPORTED;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const char* what = kv4 ? "eta_append_tokens_kv4" : "eta_append_tokens";
 #define ETA_TOK(T, DD, Q4) launch_pdl(what, append_tokens_kernel<T, DD, Q4>, dim3((unsigned)ctas), dim3(32 * TOK_WARPS), 0, s, a)
