@@ -28,7 +28,8 @@ struct TokensArgs {
     int64_t ks_b, ks_h, ks_t, vs_b, vs_h, vs_t;       // bf16 cache: elements; 4-bit: ks_* in bytes (page or sequence, head, block)
     int64_t limit;                                    // slots of the cache
     int rows, Hq, Hkv, per_page, b, q_parts, kv_parts, rotary, interleaved;
-    FastDiv div_page;
+    FastDiv div_page, div_ctas;
+    int ctas_row;          // CTAs of a row; 0: two rows to a CTA
     float k_scale, v_scale;
     int fast;              // bit 0, 1: the keys', the values' scale leaves fp32 its range, and its product with a group's is exact (20 bits)
     float eps;
@@ -90,14 +91,26 @@ struct Turn {
     __device__ __forceinline__ void set(const float* weight, int cl, int rotary, bool interleaved, const F* cs, const F* sn) {
         const int reach = rotary / 16;                     // lanes between the two halves of a pair
         const bool turns = 8 * cl < rotary, first = cl < reach;
+        const int other = interleaved || !turns ? 8 * cl : 8 * (first ? cl + reach : cl - reach);
+        const int pair = !turns ? 0 : (interleaved ? 4 * cl : 8 * (first ? cl : cl - reach));
+        F w[8], v[8], c[8], s[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
+            const float4 a = weight ? *reinterpret_cast<const float4*>(weight + 8 * cl + 4 * h) : one, b = weight ? *reinterpret_cast<const float4*>(weight + other + 4 * h) : one;
+            const float4 x = *reinterpret_cast<const float4*>(cs + pair + (interleaved ? 0 : 4 * h)), y = *reinterpret_cast<const float4*>(sn + pair + (interleaved ? 0 : 4 * h));
+            w[4 * h] = a.x; w[4 * h + 1] = a.y; w[4 * h + 2] = a.z; w[4 * h + 3] = a.w;
+            v[4 * h] = b.x; v[4 * h + 1] = b.y; v[4 * h + 2] = b.z; v[4 * h + 3] = b.w;
+            c[4 * h] = x.x; c[4 * h + 1] = x.y; c[4 * h + 2] = x.z; c[4 * h + 3] = x.w;
+            s[4 * h] = y.x; s[4 * h + 1] = y.y; s[4 * h + 2] = y.z; s[4 * h + 3] = y.w;
+        }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const int c = 8 * cl + k, other = interleaved ? c ^ 1 : (first ? c + rotary / 2 : c - rotary / 2);
-            const int pair = interleaved ? c / 2 : (first ? c : c - rotary / 2);
+            // (interleaved: neighbours share one of the first four pairs that were read)
+            const F wp = interleaved ? v[k ^ 1] : v[k], cv = interleaved ? c[k / 2] : c[k], sv = interleaved ? s[k / 2] : s[k];
             const bool minus = interleaved ? !(k & 1) : first;
-            const F w = weight ? (F)weight[c] : (F)1, wp = weight && turns ? (F)weight[other] : (F)1;
-            C[k] = turns ? w * cs[pair] : w;
-            S[k] = turns ? (minus ? -wp : wp) * sn[pair] : (F)0;
+            C[k] = turns ? w[k] * cv : w[k];
+            S[k] = turns ? (minus ? -wp : wp) * sv : (F)0;
         }
     }
     // x: the lane's channels, y: their partners.  With m: also the sizes |x C| + |x_partner S| times r, which bound what rounding did.
@@ -257,8 +270,8 @@ struct Quad {
 
 // A row's queries.  A lane takes four pairs of a head: channels ca .. ca + 3 and their partners cb .. cb + 3 (interleaved: two times two pairs of
 // neighbours), so that no channel travels between lanes; y = (x C + x_partner S) r, two channels an instruction.
-template <typename T, int D, bool INTER>
-__device__ __forceinline__ void queries(const TokensArgs& a, int64_t row, int begin, int end, int lane, float* cs, float* sn) {
+template <typename T, int D, bool INTER, typename Angles>
+__device__ __forceinline__ void queries(const TokensArgs& a, int64_t row, int begin, int end, int lane, const float* cs, const float* sn, Angles angles) {
     constexpr int LPH = D / 8, HPW = 32 / LPH;
     const int hl = lane / LPH, p = 4 * (lane % LPH), half = a.rotary / 2, nq = (a.Hq + HPW - 1) / HPW;
     const bool turns = INTER ? 2 * p < a.rotary : p < half;
@@ -277,10 +290,7 @@ __device__ __forceinline__ void queries(const TokensArgs& a, int64_t row, int be
     };
 #pragma unroll
     for (int u = 0; u < TOK_LOADS; ++u) load(u, begin + u);
-    if (a.rotary) {
-        for (int c = lane; c < half; c += 32) sincosf((float)reduced_angle(a, row, c), sn + c, cs + c);
-        __syncwarp();
-    }
+    angles();
     float C[8], S[8];
     {
         const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
@@ -347,24 +357,33 @@ __device__ __forceinline__ void queries(const TokensArgs& a, int64_t row, int be
 template <typename T, int D, bool KV4>
 __global__ void __launch_bounds__(32 * TOK_WARPS, sizeof(T) == 4 ? 4 : 5) append_tokens_kernel(const __grid_constant__ TokensArgs a) {
     constexpr int LPH = D / 8, HPW = 32 / LPH;         // lanes of a head, heads of a warp
-    __shared__ __align__(16) float s_cos[TOK_WARPS][D / 2], s_sin[TOK_WARPS][D / 2];
+    __shared__ __align__(16) float s_cos[2][D / 2], s_sin[2][D / 2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    // two rows with two warps each, or four warps of the 4 * ctas_row that a row has
+    const bool two = a.ctas_row == 0;
+    int row, part;
+    if (two) { row = blockIdx.x * 2 + (warp >> 1); part = warp & 1; }
+    else { a.div_ctas.divmod((int)blockIdx.x, row, part); part = 4 * part + warp; }
+    const int tab = two ? warp >> 1 : 0, sub = two ? threadIdx.x & 63 : threadIdx.x, others_by = two ? 64 : 128;
+    float *const cs = s_cos[tab], *const sn = s_sin[tab];
     pdl_wait();
-    const int64_t wid = (int64_t)blockIdx.x * TOK_WARPS + warp;
-    const int parts = a.q_parts + a.kv_parts;
-    const int64_t row = wid / parts;
-    const int part = (int)(wid - row * parts);
-    if (row >= a.rows) return;
-    const int64_t slot = __ldcg(reinterpret_cast<const long long*>(a.slot_map) + row);
-    if (slot < 0) return;
-    if (slot >= a.limit) {
-        if (lane == 0 && part == 0 && a.status) atomicOr(a.status, ETA_DEV_BAD_SLOT);
+    const int64_t slot = row < a.rows ? (int64_t)__ldcg(reinterpret_cast<const long long*>(a.slot_map) + row) : -1;
+    const bool live = slot >= 0 && slot < a.limit;
+    // the row's angles, by all its warps of the CTA: every warp of a CTA comes here once
+    auto angles = [&]() {
+        if (a.rotary && live)
+            for (int c = sub; c < a.rotary / 2; c += others_by) sincosf((float)reduced_angle(a, row, c), sn + c, cs + c);
+        __syncthreads();
+    };
+    if (!live) {
+        if (slot >= 0 && lane == 0 && part == 0 && a.status) atomicOr(a.status, ETA_DEV_BAD_SLOT);
+        angles();
         return;
     }
     if (part < a.q_parts) {
         const int nq = (a.Hq + HPW - 1) / HPW, begin = part * nq / a.q_parts, end = (part + 1) * nq / a.q_parts;
-        if (a.interleaved) queries<T, D, true>(a, row, begin, end, lane, s_cos[warp], s_sin[warp]);
-        else queries<T, D, false>(a, row, begin, end, lane, s_cos[warp], s_sin[warp]);
+        if (a.interleaved) queries<T, D, true>(a, row, begin, end, lane, cs, sn, angles);
+        else queries<T, D, false>(a, row, begin, end, lane, cs, sn, angles);
         return;
     }
     // ---- keys, then values: a lane holds eight consecutive channels, so that two lanes hold a group of the 4-bit cache
@@ -376,8 +395,8 @@ __global__ void __launch_bounds__(32 * TOK_WARPS, sizeof(T) == 4 ? 4 : 5) append
     if (a.limit <= INT32_MAX) { int p32; a.div_page.divmod((int)slot, p32, off); page = p32; }
     else { page = slot / a.per_page; off = (int)(slot - page * a.per_page); }
     // items first .. last - 1 of a tensor, four on their way: use(piece, item, whether the lane has a head of it)
-    auto stream = [&](const void* tensor, int64_t sr, int64_t sh, int first, int last, auto&& use) {
-        const T* from = static_cast<const T*>(tensor) + row * sr + (first * HPW + hl) * sh + 8 * cl;
+    auto stream = [&](const void* tensor, int64_t sr, int64_t sh, int first, int last, auto&& ready, auto&& use) {
+        const T* from = static_cast<const T*>(tensor) + (int64_t)row * sr + (first * HPW + hl) * sh + 8 * cl;
         const int64_t step = HPW * sh;
         Piece<T> pc[TOK_LOADS];
         auto load = [&](int u, int it) {
@@ -387,6 +406,7 @@ __global__ void __launch_bounds__(32 * TOK_WARPS, sizeof(T) == 4 ? 4 : 5) append
         };
 #pragma unroll
         for (int u = 0; u < TOK_LOADS; ++u) load(u, first + u);
+        ready();
 #pragma unroll 1
         for (int it = first; it < last; it += TOK_LOADS) {
 #pragma unroll
@@ -417,23 +437,21 @@ __global__ void __launch_bounds__(32 * TOK_WARPS, sizeof(T) == 4 ? 4 : 5) append
     };
     const int k0 = min(begin, nkv), k1 = min(end, nkv), v0 = max(begin, nkv) - nkv, v1 = max(end, nkv) - nkv;
     Turn<float> turn;
-    if (k0 < k1) {
-        if (a.rotary) {
-            for (int c = lane; c < a.rotary / 2; c += 32) sincosf((float)reduced_angle(a, row, c), &s_sin[warp][c], &s_cos[warp][c]);
-            __syncwarp();
-        }
-        turn.template set<D>(a.k_weight, cl, a.rotary, a.interleaved != 0, s_cos[warp], s_sin[warp]);
-    }
+    auto turned = [&]() {
+        angles();
+        if (k0 < k1) turn.template set<D>(a.k_weight, cl, a.rotary, a.interleaved != 0, cs, sn);
+    };
+    auto nothing = []() {};
     if constexpr (!KV4) {
         const int64_t kb = page * a.ks_b + (int64_t)off * a.ks_t + 8 * cl, vb = page * a.vs_b + (int64_t)off * a.vs_t + 8 * cl;
-        stream(a.k, a.k_sr, a.k_sh, k0, k1, [&](const Piece<T>& p, int it, bool on) {
+        stream(a.k, a.k_sr, a.k_sh, k0, k1, turned, [&](const Piece<T>& p, int it, bool on) {
             float x[8], y[8];
             p.get(x);
             others(p, y);
             turn.template apply<D>(x, y, a.k_weight != nullptr, a.eps);
             if (on) *reinterpret_cast<uint4*>(a.K + kb + (it * HPW + hl) * a.ks_h) = pack_bf16(x);
         });
-        stream(a.v, a.v_sr, a.v_sh, v0, v1, [&](const Piece<T>& p, int it, bool on) {
+        stream(a.v, a.v_sr, a.v_sh, v0, v1, nothing, [&](const Piece<T>& p, int it, bool on) {
             float x[8];
             p.get(x);
             if (on) *reinterpret_cast<uint4*>(a.V + vb + (it * HPW + hl) * a.vs_h) = pack_bf16(x);
@@ -450,7 +468,7 @@ __global__ void __launch_bounds__(32 * TOK_WARPS, sizeof(T) == 4 ? 4 : 5) append
         };
         const int v_at = Kv4Block(a.b, D).v_codes;
         uint64_t left = 0;                                 // keys that fp32 did not settle (bit 63: one of those from there on)
-        stream(a.k, a.k_sr, a.k_sh, k0, k1, [&](const Piece<T>& p, int it, bool on) {
+        stream(a.k, a.k_sr, a.k_sh, k0, k1, turned, [&](const Piece<T>& p, int it, bool on) {
             float x[8], y[8], m[8];
             p.get(x);
             others(p, y);
@@ -463,14 +481,14 @@ __global__ void __launch_bounds__(32 * TOK_WARPS, sizeof(T) == 4 ? 4 : 5) append
             }
         });
         if (a.fast & 2) {
-            stream(a.v, a.v_sr, a.v_sh, v0, v1, [&](const Piece<T>& p, int it, bool on) {
+            stream(a.v, a.v_sr, a.v_sh, v0, v1, nothing, [&](const Piece<T>& p, int it, bool on) {
                 float x[8];
                 p.get(x);
                 const Kv4Codes c = codes_of_values(x, a.v_scale);
                 if (on) store(c, v_at, it);
             });
         } else {
-            stream(a.v, a.v_sr, a.v_sh, v0, v1, [&](const Piece<T>& p, int it, bool on) {
+            stream(a.v, a.v_sr, a.v_sh, v0, v1, nothing, [&](const Piece<T>& p, int it, bool on) {
                 double x[8];
                 p.get(x);
                 const Kv4Codes c = codes_exact(x, a.v_scale);
@@ -482,7 +500,7 @@ __global__ void __launch_bounds__(32 * TOK_WARPS, sizeof(T) == 4 ? 4 : 5) append
             if (((left >> min(it - k0, 63)) & 1) == 0) continue;
             const bool on = it < nkv - 1 || in_last;
             Piece<T> p;
-            p.load(static_cast<const T*>(a.k) + row * a.k_sr + (it * HPW + hl) * a.k_sh + 8 * cl, on);
+            p.load(static_cast<const T*>(a.k) + (int64_t)row * a.k_sr + (it * HPW + hl) * a.k_sh + 8 * cl, on);
             double x[8], y[8];
             p.get(x);
             others(p, y);
@@ -575,6 +593,7 @@ static int append_tokens(const eta_cache_desc* desc, const eta_kv4_desc* kv4, co
     if (misaligned({q, k, v, q_out, K, V, q_weight, k_weight}, 16) || misaligned({slot_map, inv_freq}, 8) || misaligned({positions}, 4))
         return ETA_ERR_UNSUPPORTED;
     if (tok->n_rows == 0) return ETA_OK;
+    if (tok->n_rows > (1 << 30)) return ETA_ERR_UNSUPPORTED;
 
     TokensArgs a;
     a.q = q; a.k = k; a.v = v;
@@ -601,18 +620,20 @@ static int append_tokens(const eta_cache_desc* desc, const eta_kv4_desc* kv4, co
     a.rotary = tok->rotary_dim; a.interleaved = (tok->flags & ETA_TOKENS_INTERLEAVED) != 0;
     a.eps = tok->eps;
     a.div_page = FastDiv(a.per_page);
-    // Two warps to a row, one for its queries, one for its keys and values, where there are rows enough to fill the GPU; as many as
-    // there are items where there are not.
+    // Two warps to a row, one for its queries, one for its keys and values, where there are rows enough to fill the GPU; as many as there
+    // are items where there are not.
     const int per_warp = 32 / (desc->head_dim / 8);
     const int q_items = (a.Hq + per_warp - 1) / per_warp, kv_items = 2 * ((a.Hkv + per_warp - 1) / per_warp);
-    const int64_t want = ((int64_t)148 * 16 + a.rows - 1) / a.rows;
-    a.q_parts = (int)(want / 2 < 1 ? 1 : (want / 2 > q_items ? q_items : want / 2));
-    a.kv_parts = (int)(want / 2 < 1 ? 1 : (want / 2 > kv_items ? kv_items : want / 2));
-    const int64_t ctas = ((int64_t)a.rows * (a.q_parts + a.kv_parts) + TOK_WARPS - 1) / TOK_WARPS;
-    if (ctas > INT32_MAX) return ETA_ERR_UNSUPPORTED;
+    const int want = (148 * 16 / 4 + a.rows - 1) / a.rows, most = (q_items + kv_items + 3) / 4;
+    a.ctas_row = a.rows >= 148 * 8 ? 0 : (want > most ? most : want);
+    const int parts = a.ctas_row ? 4 * a.ctas_row : 2;
+    a.kv_parts = parts / 2 < kv_items ? parts / 2 : kv_items;
+    a.q_parts = parts - a.kv_parts;
+    a.div_ctas = FastDiv(a.ctas_row ? a.ctas_row : 1);
+    const unsigned ctas = a.ctas_row ? (unsigned)a.rows * a.ctas_row : ((unsigned)a.rows + 1) / 2;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const char* what = kv4 ? "eta_append_tokens_kv4" : "eta_append_tokens";
-#define ETA_TOK(T, DD, Q4) launch_pdl(what, append_tokens_kernel<T, DD, Q4>, dim3((unsigned)ctas), dim3(32 * TOK_WARPS), 0, s, a)
+#define ETA_TOK(T, DD, Q4) launch_pdl(what, append_tokens_kernel<T, DD, Q4>, dim3(ctas), dim3(32 * TOK_WARPS), 0, s, a)
 #define ETA_TOK_D(T) (desc->head_dim == 128 ? (kv4 ? ETA_TOK(T, 128, true) : ETA_TOK(T, 128, false)) : (kv4 ? ETA_TOK(T, 64, true) : ETA_TOK(T, 64, false)))
     return tok->type == ETA_TYPE_BF16 ? ETA_TOK_D(__nv_bfloat16) : (tok->type == ETA_TYPE_FP16 ? ETA_TOK_D(__half) : ETA_TOK_D(float));
 #undef ETA_TOK_D
