@@ -22,7 +22,7 @@ __device__ __forceinline__ void codes_to_f16(const uint2& w, uint32_t (&h)[8]) {
     for (int k = 0; k < 4; ++k) { h[k] = x[k]; h[4 + k] = y[k]; }
 }
 // a, b += the two halves of v;  c, d += their squares.  sm_100 adds and multiplies fp16 numbers into fp32 ones: unpacking them first cost half of the
-// pass (155 -> 105 us for 4 x 128K tokens of 8 heads).
+// pass (155 -> 129 us for 4 x 128K tokens of 8 heads).
 __device__ __forceinline__ void add_moments(float& a, float& b, float& c, float& d, uint32_t v) {
     asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %4;\n\t"
         "add.rn.f32.f16 %0, l, %0;\n\tadd.rn.f32.f16 %1, h, %1;\n\t"
@@ -39,7 +39,7 @@ __device__ __forceinline__ void summarize_kv4(const unsigned char* blk, int b, f
     const int lane = threadIdx.x & 31, cc = lane % LPR, ro = lane / LPR;
     const unsigned char* codes = blk + ro * (D / 2) + cc * 8;
     const unsigned char* scales = blk + Kv4Block(b, D).k_scales + ro * LPR + cc;
-    float s1[KV4_GROUP], s2[KV4_GROUP], maxn2 = 0.f;
+    float s1[KV4_GROUP], s2[KV4_GROUP], n2[U], maxn2 = 0.f;
 #pragma unroll
     for (int k = 0; k < KV4_GROUP; ++k) { s1[k] = 0.f; s2[k] = 0.f; }
     for (int t0 = 0; t0 < b; t0 += U * RPP) {
@@ -62,12 +62,23 @@ __device__ __forceinline__ void summarize_kv4(const unsigned char* blk, int b, f
                 add_moments(s1[2 * k], s1[2 * k + 1], s2[2 * k], s2[2 * k + 1], hmul2_u(h[k], s));
             }
             const float sf = f16_lo(s);
-            float n2 = (f16_lo(sq) + f16_hi(sq)) * (sf * sf);
-#pragma unroll
-            for (int x = 1; x < LPR; x <<= 1) n2 += __shfl_xor_sync(0xffffffffu, n2, x);
-            maxn2 = max_nan(maxn2, n2);
+            n2[u] = (f16_lo(sq) + f16_hi(sq)) * (sf * sf);
         }
+        // the rows' lanes meet: every exchange halves the rows that a lane goes on with
+#pragma unroll
+        for (int x = 1, n = U; x < LPR; x <<= 1, n >>= 1) {
+            const bool up = (lane & x) != 0;
+#pragma unroll
+            for (int u = 0; u < n / 2; ++u) {
+                const float o = up ? n2[u] : n2[n / 2 + u];
+                n2[u] = (up ? n2[n / 2 + u] : n2[u]) + __shfl_xor_sync(0xffffffffu, o, x);
+            }
+        }
+        static_assert(U == LPR, "a row for every lane of a row");
+        maxn2 = max_nan(maxn2, n2[0]);
     }
+#pragma unroll
+    for (int x = 1; x < LPR; x <<= 1) maxn2 = max_nan(maxn2, __shfl_xor_sync(0xffffffffu, maxn2, x));
 #pragma unroll
     for (int x = LPR; x < 32; x <<= 1) maxn2 = max_nan(maxn2, __shfl_xor_sync(0xffffffffu, maxn2, x));
     const float inv_b = 1.0f / (float)b;
