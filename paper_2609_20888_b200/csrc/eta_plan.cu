@@ -23,31 +23,34 @@ struct PlanArgs {
 
 constexpr int PLAN_THREADS = 1024, PLAN_WARPS = PLAN_THREADS / 32;
 
-// The sum of x over the threads before this one; `all`: over all of them.  Every thread of the CTA calls it; s_warp may be used again at once
-// (its first half is read before the second barrier only, its second half is written after the next call's first).
-__device__ __forceinline__ int64_t scan(int64_t x, int64_t& all, int64_t* s_warp) {
+// The sums of x and y over the threads before this one; all: over all of them.  Every thread of the CTA calls it; s_warp may be used again at
+// once (its first half is read before the second barrier only, its second half is written after the next call's first).
+__device__ __forceinline__ longlong2 scan(int64_t x, int64_t y, longlong2& all, longlong2* s_warp) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int64_t upto = x;
+    int64_t ux = x, uy = y;
 #pragma unroll
     for (int s = 1; s < 32; s <<= 1) {
-        const int64_t o = __shfl_up_sync(0xffffffffu, upto, s);
-        if (lane >= s) upto += o;
+        const int64_t ox = __shfl_up_sync(0xffffffffu, ux, s), oy = __shfl_up_sync(0xffffffffu, uy, s);
+        if (lane >= s) { ux += ox; uy += oy; }
     }
-    if (lane == 31) s_warp[warp] = upto;
+    if (lane == 31) s_warp[warp] = make_longlong2(ux, uy);
     __syncthreads();
     if (warp == 0) {
-        int64_t w = s_warp[lane];
+        const longlong2 w = s_warp[lane];
+        int64_t wx = w.x, wy = w.y;
 #pragma unroll
         for (int s = 1; s < 32; s <<= 1) {
-            const int64_t o = __shfl_up_sync(0xffffffffu, w, s);
-            if (lane >= s) w += o;
+            const int64_t ox = __shfl_up_sync(0xffffffffu, wx, s), oy = __shfl_up_sync(0xffffffffu, wy, s);
+            if (lane >= s) { wx += ox; wy += oy; }
         }
-        s_warp[PLAN_WARPS + lane] = w;
+        s_warp[PLAN_WARPS + lane] = make_longlong2(wx, wy);
     }
     __syncthreads();
     all = s_warp[2 * PLAN_WARPS - 1];
-    return (warp ? s_warp[PLAN_WARPS + warp - 1] : 0) + upto - x;
+    const longlong2 before = warp ? s_warp[PLAN_WARPS + warp - 1] : make_longlong2(0, 0);
+    return make_longlong2(before.x + ux - x, before.y + uy - y);
 }
+__device__ __forceinline__ int32_t saturated(int64_t x) { return (int32_t)(x > INT32_MAX ? INT32_MAX : x); }
 
 // the last of n ascending numbers, the first of which is not above x, that is not above x
 __device__ __forceinline__ int last_not_above(const int32_t* v, int n, int32_t x) {
@@ -59,25 +62,26 @@ __device__ __forceinline__ int last_not_above(const int32_t* v, int n, int32_t x
     return lo;
 }
 
-// Slot and position of row r, whose sequence is i (or none: i >= batch).
-__device__ __forceinline__ void store_row(const PlanArgs& a, int r, int i) {
+// What a row of a sequence needs: position = row + shift; NO_PLACE where the sequence got nothing
+constexpr int32_t NO_PLACE = INT32_MIN;
+__device__ __forceinline__ int32_t shift_of(int len_after, int got, int row0) { return got > 0 ? len_after - got - row0 : NO_PLACE; }
+
+__device__ __forceinline__ void store_row(const PlanArgs& a, int r, int i, int32_t shift) {
     int64_t slot = -1;
     int pos = 0;
-    if (i < a.batch) {
-        const int got = __ldcg(a.granted + i);
-        if (got > 0) {
-            pos = __ldcg(a.seq_lens_out + i) - got + (r - __ldcg(a.row_start + i));
-            const int page = __ldcg(a.block_table + (int64_t)i * a.table_stride + (pos >> a.b_shift));
-            slot = ((int64_t)page << a.b_shift) + (pos & ((1 << a.b_shift) - 1));
-        }
+    if (shift != NO_PLACE) {
+        pos = r + shift;
+        const int page = __ldcg(a.block_table + (int64_t)i * a.table_stride + (pos >> a.b_shift));
+        slot = ((int64_t)page << a.b_shift) + (pos & ((1 << a.b_shift) - 1));
     }
     a.slot_map[r] = slot;
     a.positions[r] = pos;
 }
 
 __global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const PlanArgs a, const int rows_here) {
-    __shared__ int64_t s_warp[2 * PLAN_WARPS];
-    __shared__ int32_t s_before[PLAN_THREADS];
+    __shared__ longlong2 s_warp[2 * PLAN_WARPS];
+    __shared__ int32_t s_before[PLAN_THREADS], s_held[PLAN_THREADS], s_row0[PLAN_THREADS + 1], s_shift[PLAN_THREADS];
+    __shared__ int s_taken;
     const int tid = threadIdx.x, b = 1 << a.b_shift;
     pdl_wait();
     if (!rows_here) pdl_trigger();          // the rows' kernel, which waits for this one
@@ -95,24 +99,26 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const PlanArgs a, co
                 gone = len <= 0 ? 0 : (int)(((int64_t)len + b - 1) >> a.b_shift);
                 if (gone > a.table_stride) { gone = a.table_stride; refused = true; }
             }
-            int64_t all;
-            const int64_t before = scan(gone, all, s_warp);
-            s_before[tid] = (int32_t)(before > INT32_MAX ? INT32_MAX : before);
+            longlong2 all;
+            s_before[tid] = saturated(scan(gone, 0, all, s_warp).x);
             __syncthreads();
-            if (all > a.n_pages - n_free) { all = a.n_pages - n_free; refused = true; }      // more than were ever handed out
-            const int n_seq = min(PLAN_THREADS, a.batch - c);
-            for (int p = tid; p < (int)all; p += PLAN_THREADS) {
+            if (all.x > a.n_pages - n_free) { all.x = a.n_pages - n_free; refused = true; }      // more than were ever handed out
+            const int n_seq = min(PLAN_THREADS, a.batch - c), n = (int)all.x;
+#pragma unroll 4
+            for (int p = tid; p < n; p += PLAN_THREADS) {
                 const int s = last_not_above(s_before, n_seq, p);
                 a.free_pages[n_free + p] = __ldcg(a.block_table + (int64_t)(c + s) * a.table_stride + (p - s_before[s]));
             }
-            n_free += (int)all;
+            n_free += n;
             __syncthreads();
         }
     }
 
-    // ---- new tokens
+    // ---- new tokens.  One scan serves rows and pages: the rows of a sequence lie within n_rows only if those of all before it do, so
+    // among those that can be served the pages asked for before them are those of sequences that fit.
     int64_t rows_done = 0, pages_done = 0;       // rows and pages asked for so far, those that could not be had included
     int taken = 0;
+    const bool one_chunk = a.batch <= PLAN_THREADS;
     for (int c = 0; c < a.batch; c += PLAN_THREADS) {
         const int i = c + tid, n_seq = min(PLAN_THREADS, a.batch - c);
         int len = 0, fresh = 0, held = 0, need = 0;
@@ -120,51 +126,68 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const PlanArgs a, co
             fresh = max(0, __ldcg(a.new_lens + i));
             len = a.release && __ldcg(a.release + i) != 0 ? 0 : max(0, __ldcg(a.seq_lens + i));
         }
-        int64_t all_rows, all_need;
-        const int64_t row0 = rows_done + scan(fresh, all_rows, s_warp);
-        const bool fits = (int64_t)len + fresh <= a.t_cap && row0 + fresh <= a.n_rows;
+        bool fits = (int64_t)len + fresh <= a.t_cap;
         if (fits) {
             held = (int)(((int64_t)len + b - 1) >> a.b_shift);
             need = (int)(((int64_t)len + fresh + b - 1) >> a.b_shift) - held;
         }
-        const int64_t first = pages_done + scan(need, all_need, s_warp);
+        longlong2 all;
+        if (tid == 0) s_taken = INT32_MAX;
+        const longlong2 before = scan(fresh, need, all, s_warp);
+        const int64_t row0 = rows_done + before.x, first = pages_done + before.y;
+        fits = fits && row0 + fresh <= a.n_rows;
         const bool ok = fits && (need == 0 || first + need <= n_free);
+        // Once a sequence that needs pages gets none, so do all later ones that need any: the pages taken are those asked for before the first such.
+        if (!ok && need > 0) atomicMin(&s_taken, saturated(before.y));
+        const int got = ok ? fresh : 0;
+        s_before[tid] = saturated(before.y);
+        s_held[tid] = held;
+        s_row0[tid] = saturated(row0);
+        s_shift[tid] = shift_of(len + got, got, saturated(row0));
         if (i < a.batch) {
-            const int got = ok ? fresh : 0;
             refused = refused || got != fresh;
             a.granted[i] = got;
             a.seq_lens_out[i] = len + got;
-            a.row_start[i] = (int32_t)(row0 > INT32_MAX ? INT32_MAX : row0);
-            if (i == a.batch - 1) a.row_start[a.batch] = (int32_t)(row0 + fresh > INT32_MAX ? INT32_MAX : row0 + fresh);
+            a.row_start[i] = saturated(row0);
+            if (i == a.batch - 1) a.row_start[a.batch] = s_row0[n_seq] = saturated(row0 + fresh);
         }
-        // Once a sequence that needs pages gets none, `first` is past the stack for all later ones: those that get pages come
-        // first, and the pages asked for before them are the pages taken before them.
-        int64_t taken_here;
-        s_before[tid] = (int32_t)scan(ok ? need : 0, taken_here, s_warp);
         __syncthreads();
-        for (int p = tid; p < (int)taken_here; p += PLAN_THREADS) {
+        const int n = (int)(s_taken < all.y ? s_taken : all.y);
+#pragma unroll 4
+        for (int p = tid; p < n; p += PLAN_THREADS) {
             const int s = last_not_above(s_before, n_seq, p);
-            const int l = __ldcg(a.seq_lens_out + c + s) - __ldcg(a.granted + c + s);
-            const int at = (int)(((int64_t)l + b - 1) >> a.b_shift) + (p - s_before[s]);
-            a.block_table[(int64_t)(c + s) * a.table_stride + at] = a.free_pages[n_free - 1 - taken - p];
+            a.block_table[(int64_t)(c + s) * a.table_stride + s_held[s] + (p - s_before[s])] = a.free_pages[n_free - 1 - taken - p];
         }
-        taken += (int)taken_here;
-        rows_done += all_rows;
-        pages_done += all_need;
+        taken += n;
+        rows_done += all.x;
+        pages_done += all.y;
         __syncthreads();
     }
     if (tid == 0) *a.n_free_out = n_free - taken;
     if (refused && a.status) atomicOr(a.status, ETA_DEV_REFUSED);
     if (!rows_here) return;
-    for (int r = tid; r < a.n_rows; r += PLAN_THREADS)
-        store_row(a, r, r < __ldcg(a.row_start + a.batch) ? last_not_above(a.row_start, a.batch + 1, r) : a.batch);
+    for (int r = tid; r < a.n_rows; r += PLAN_THREADS) {
+        int i = 0;
+        int32_t shift = NO_PLACE;
+        if (one_chunk) {
+            if (r < s_row0[a.batch]) {
+                i = last_not_above(s_row0, a.batch, r);
+                shift = s_shift[i];
+            }
+        } else if (r < __ldcg(a.row_start + a.batch)) {
+            i = last_not_above(a.row_start, a.batch, r);
+            shift = shift_of(__ldcg(a.seq_lens_out + i), __ldcg(a.granted + i), __ldcg(a.row_start + i));
+        }
+        store_row(a, r, i, shift);
+    }
 }
 
-// The rows of a large step, ROWS_PER_CTA to a CTA: which sequences they can belong to is one sweep over the row starts, then
-// every row bisects among those.
-constexpr int ROWS_THREADS = 256, ROWS_PER_CTA = 1024;
+// The rows of a large step, ROWS_PER_CTA to a CTA: which sequences they can belong to is one sweep over the row starts; what the rows need
+// of those is put into shared memory where there is room, so that a row waits for its page's number only.
+constexpr int ROWS_THREADS = 256, ROWS_PER_CTA = 1024, ROWS_SEQS = 1024;
 __global__ void __launch_bounds__(ROWS_THREADS) plan_rows_kernel(const PlanArgs a) {
     __shared__ int s_first, s_last;
+    __shared__ int32_t s_row0[ROWS_SEQS], s_shift[ROWS_SEQS];
     const int tid = threadIdx.x, r0 = blockIdx.x * ROWS_PER_CTA, r1 = min(a.n_rows, r0 + ROWS_PER_CTA);
     if (tid == 0) { s_first = 0; s_last = 0; }
     pdl_wait();
@@ -180,7 +203,24 @@ __global__ void __launch_bounds__(ROWS_THREADS) plan_rows_kernel(const PlanArgs 
     if ((tid & 31) == 0) { atomicAdd(&s_first, first); atomicAdd(&s_last, last); }
     __syncthreads();
     const int lo = s_first - 1, n = s_last - lo;         // row_start[0] = 0: at least one is not above r0
-    for (int r = r0 + tid; r < r1; r += ROWS_THREADS) store_row(a, r, lo + last_not_above(a.row_start + lo, n, r));
+    const bool near = n <= ROWS_SEQS;
+    auto shift_at = [&](int i) {
+        return i < a.batch ? shift_of(__ldcg(a.seq_lens_out + i), __ldcg(a.granted + i), __ldcg(a.row_start + i)) : NO_PLACE;
+    };
+    if (near) {
+        for (int k = tid; k < n; k += ROWS_THREADS) {
+            s_row0[k] = __ldcg(a.row_start + lo + k);
+            s_shift[k] = shift_at(lo + k);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int u = 0; u < ROWS_PER_CTA / ROWS_THREADS; ++u) {
+        const int r = r0 + tid + u * ROWS_THREADS;
+        if (r >= r1) break;
+        const int k = last_not_above(near ? s_row0 : a.row_start + lo, n, r);
+        store_row(a, r, lo + k, near ? s_shift[k] : shift_at(lo + k));
+    }
 }
 
 }  // namespace eta
