@@ -120,7 +120,7 @@ struct AttendKv4 {
         reset();
     }
     __device__ __forceinline__ void reset() {
-        m0 = m1 = NONE;
+        m0 = m1 = k0 = k1 = NONE;
         l0 = l1 = 0.f;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
@@ -170,13 +170,17 @@ struct AttendKv4 {
             l[c0] = nx ? 1.f : x; l[c0 + 1] = ny ? 1.f : y;
         }
     }
-    // The accumulators of heads h0 .. h0 + n - 1 to sm [n][O_STRIDE], channel (D / 8) g + 2 mt + c at 16 mt + 2 g + c: the sixteen lanes of a
-    // phase write to all banks once (by channel they met four and eight at a time: 2 us of a flush's 4).
-    static constexpr int O_STRIDE = D + 4;
+    // The warp's accumulators are folded into sm [heads][O_STRIDE] every FOLD stages and at the end of a piece: an MMA cuts its sum off where
+    // fp32 would round it, and after two hundred of them in a row (64K tokens, dense) an output was off by 1.9e-6 of itself, by 7e-7 this way.
+    // Channel (D / 8) g + 2 mt + c is at 16 mt + 2 g + c: the sixteen lanes of a phase meet every bank once.
+    static constexpr int O_STRIDE = D + 4, FOLD = 10;
     // where four consecutive channels 4 k .. are: two pairs, 16 floats apart
     __device__ __forceinline__ static int o_at(int k) { return 16 * (2 * k % MT) + 2 * (2 * k / MT); }
-    __device__ __forceinline__ void store_o(float* sm, int h0, int n) const {
-        const int ha = c0 - h0, hb = ha + 1;
+    float k0, k1;                                          // the maxima that sm's sums go with
+    template <bool FIRST>
+    __device__ __forceinline__ void fold(float* sm) {
+        constexpr float LOG2E = 1.4426950408889634f;
+        const float f0 = FIRST ? 0.f : ex2_approx((k0 - m0) * LOG2E), f1 = FIRST ? 0.f : ex2_approx((k1 - m1) * LOG2E);   // (from NONE: 0)
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             float x[4];
@@ -184,12 +188,21 @@ struct AttendKv4 {
             for (int c = 0; c < 4; ++c) {
                 x[c] = o[mt][c];
                 if (!WIDE) x[c] = __shfl_xor_sync(0xffffffffu, x[c], 2) - x[c];       // remainders' columns less the (negated) values'
+                o[mt][c] = 0.f;
             }
-            const int at = 16 * mt + 2 * g;
             if (!WIDE && t >= 2) continue;
-            if (ha >= 0 && ha < n) *reinterpret_cast<float2*>(sm + ha * O_STRIDE + at) = make_float2(x[0], x[2]);
-            if (hb >= 0 && hb < n) *reinterpret_cast<float2*>(sm + hb * O_STRIDE + at) = make_float2(x[1], x[3]);
+            float2* const pa = reinterpret_cast<float2*>(sm + c0 * O_STRIDE + 16 * mt + 2 * g);
+            float2* const pb = pa + O_STRIDE / 2;
+            if (has0) {
+                if (FIRST) *pa = make_float2(x[0], x[2]);
+                else *pa = make_float2(fmaf(pa->x, f0, x[0]), fmaf(pa->y, f0, x[2]));
+            }
+            if (has1) {
+                if (FIRST) *pb = make_float2(x[1], x[3]);
+                else *pb = make_float2(fmaf(pb->x, f1, x[1]), fmaf(pb->y, f1, x[3]));
+            }
         }
+        k0 = m0; k1 = m1;
     }
     __device__ __forceinline__ float gated(float S, float te, float beta) const {
         constexpr float LOG2E = 1.4426950408889634f;

@@ -120,7 +120,7 @@ struct DecodeSmem {
     static_assert(16 * CHUNK >= 8 * MAX_SUPER, "sums of the super-chunks share the granules' place");
     static constexpr int MO_OFF = ML_OFF + 4 * 2 * NGROUPS * WARPS_PER_GROUP * 8;
     // heads whose accumulators a flush parks at a time: eight heads of 128 columns would cost the ring a stage
-    static constexpr int FLUSH_HEADS = 512 / D;
+    static constexpr int FLUSH_HEADS = Tile::KV4 ? 8 : 512 / D;       // (a 4-bit cache's are there all the time)
     static size_t bytes(int G) { return 1024 + MO_OFF + sizeof(float) * NGROUPS * WARPS_PER_GROUP * (G < FLUSH_HEADS ? G : FLUSH_HEADS) * Tile::Math::O_STRIDE; }
 };
 
@@ -738,7 +738,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         at.store_ml(sm_m + wq * 8, sm_l + wq * 8);
         const int64_t slot = ((int64_t)blockIdx.x + row) * NGROUPS + group;
         for (int h0 = 0; h0 < a.G && ok; h0 += fheads) {
-            at.store_o(sm_o + wq * fheads * OS, h0, fheads);
+            if constexpr (!Tile::KV4) at.store_o(sm_o + wq * fheads * OS, h0, fheads);
 #ifdef ETA_TEST_SKIP_FLUSH_ARRIVE
             // test build only: one warp of the first CTA never arrives, so that the group's bounded wait runs out and
             // the give-up path (status flag, orderly exit of the whole CTA) executes
@@ -781,8 +781,9 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         }
     };
     if constexpr (Tile::KV4) {
-        // Piece after piece, the stages of a piece in a loop of their own: with the flush inside that loop the accumulators were moved
-        // between registers once a slab, 53 of 396 instructions.
+        // Piece after piece, the stages of a piece in a loop of their own, with neither the fold nor the flush in it: with the flush inside
+        // the accumulators were moved between registers once a slab, 53 of 396 instructions (16 x 64K dense: 178K cycles with the fold inside,
+        // 170K this way).
         constexpr int SPU = TS / 16;                       // slabs of a unit
         // a group's stages are group, group + NGROUPS, .. round by round
         int stage = group;
@@ -795,30 +796,41 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             row = ds.x;
             if (row != q_row) load_q(row);
             at.reset();
-            do {
-                const uint32_t base = smem_u32(smem + stage * STAGE_BYTES);
-                const int2* const units = udesc + stage * Tile::UNITS;
-                // the stage's slabs in equal shares
-                const int end_slab = (wq + 1) * ds.z / WARPS_PER_GROUP;
+            bool folded = false, more;                     // more: the piece goes on
+            do {                                           // (up to FOLD stages between two folds)
+                int n = 0;
+                do {
+                    const uint32_t base = smem_u32(smem + stage * STAGE_BYTES);
+                    const int2* const units = udesc + stage * Tile::UNITS;
+                    // the stage's slabs in equal shares
+                    const int end_slab = (wq + 1) * ds.z / WARPS_PER_GROUP;
 #pragma unroll 1
-                for (int sl = wq * ds.z / WARPS_PER_GROUP; sl < end_slab; ++sl) {
-                    const int unit = sl / SPU, r0 = (sl % SPU) * 16;
-                    const int2 ud = units[unit];
-                    at.slab(base + unit * Tile::UNIT_BYTES, r0, ud.x & 0xff, (ud.x >> 8) & 0xff, ud.y, a.scale, a.beta);
-                }
-                // the arrive (release) orders the warp's reads of the stage before the producer's next copy into it
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&empty[stage]);
-                stage += NGROUPS;
-                if (stage >= NSTAGE) { stage -= NSTAGE; parity ^= 1; }
-                ok = mbar_wait(&full[stage], parity);
+                    for (int sl = wq * ds.z / WARPS_PER_GROUP; sl < end_slab; ++sl) {
+                        const int unit = sl / SPU, r0 = (sl % SPU) * 16;
+                        const int2 ud = units[unit];
+                        at.slab(base + unit * Tile::UNIT_BYTES, r0, ud.x & 0xff, (ud.x >> 8) & 0xff, ud.y, a.scale, a.beta);
+                    }
+                    // the arrive (release) orders the warp's reads of the stage before the producer's next copy into it
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&empty[stage]);
+                    stage += NGROUPS;
+                    if (stage >= NSTAGE) { stage -= NSTAGE; parity ^= 1; }
+                    ok = mbar_wait(&full[stage], parity);
+                    if (!ok) break;
+                    ds = desc[stage];
+                    more = !(ds.y & (int)UF_END) && (ds.y >> 1) == piece;
+                } while (more && ++n < Tile::Math::FOLD);
                 if (!ok) break;
-                ds = desc[stage];
-            } while (!(ds.y & (int)UF_END) && (ds.y >> 1) == piece);
+                // the next piece's query is on its way during the fold and the flush, which do not read the query registers
+                if (!more) {
+                    if (ds.y & (int)UF_END) pdl_trigger();
+                    else if (ds.x != q_row) load_q(ds.x);
+                }
+                if (folded) at.template fold<false>(sm_o + wq * fheads * OS);
+                else at.template fold<true>(sm_o + wq * fheads * OS);
+                folded = true;
+            } while (more);
             if (!ok) break;
-            // the next piece's query is on its way during the flush, which does not read the query registers
-            if (ds.y & (int)UF_END) pdl_trigger();
-            else if (ds.x != q_row) load_q(ds.x);
             flush_piece();
         }
         if (!ok && lane == 0 && a.status) atomicOr(a.status, ETA_DEV_TIMEOUT);

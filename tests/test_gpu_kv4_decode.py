@@ -197,6 +197,37 @@ def test_packed_summaries_and_many_rows():
     check(s, gpu(s, m8, mnorm, tau, flags=4), want, tau.astype(np.float64), 5.0)
 
 
+@pytest.mark.parametrize("d,b,G,longest", [(128, 64, 4, 9000), (128, 32, 8, 9000), (64, 64, 8, 18000), (64, 128, 2, 18000)])
+def test_long_pieces_with_growing_scores(d, b, G, longest):
+    """160 rows, one or two to a CTA, whose running sums are put together many times over while their maxima still grow."""
+    from paper_2609_20888_b200 import binding as eb
+    B, Hkv, nb = 20, 8, -(-longest // b)
+    g = torch.Generator(device="cuda").manual_seed(d + b)
+    pool = torch.randint(0, 256, (B, Hkv, nb, eb.kv4_block_bytes(b, d)), dtype=torch.uint8, device="cuda", generator=g)
+    k0, v0, sc = b * d // 2, b * d // 2 + b * d // 16, b * d // 16
+    step = (torch.arange(nb * b, device="cuda") * 3 // (nb * b)).to(torch.uint8).reshape(nb, b, 1).expand(nb, b, d // 16).reshape(nb, sc)
+    pool[..., k0:k0 + sc] = 0x20 + 8 * step                # 2^-3, 2^-2 and 2^-1
+    pool[..., v0 + b * d // 2:] = 0x30
+    lens = torch.randint(longest // 2, longest + 1, (B,), dtype=torch.int32, device="cuda", generator=g)
+    q = torch.randn((B, Hkv * G, d), device="cuda", generator=g).to(torch.bfloat16)
+    desc, kv4 = eb.kv4_cache_desc(pool, Hkv * G, d, b, batch=B, t_cap=nb * b)
+    out, st = torch.empty((B, Hkv * G, d), device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    sel = torch.empty((B, Hkv, nb), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(eb.eta_kv4_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    eb.eta_decode_kv4(desc, kv4, eb.DecodeParams(flags=eb.ETA_FLAG_DENSE), q, pool, lens, None, None, torch.zeros((B, Hkv * G), device="cuda"), None,
+                      out, sel, ws, status=st)
+    K, V = (torch.empty((B, Hkv, nb * b, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    eb.eta_unpack_kv4(desc, kv4, pool, K, V)
+    assert st.item() == 0
+    for i in range(B):
+        n = int(lens[i])
+        x, y = K[i, :, :n].double(), V[i, :, :n].double()
+        want = torch.softmax(q[i].double().reshape(Hkv, G, d) @ x.mT / d ** 0.5, -1) @ y
+        # fp32 arithmetic, and an MMA's sum that is cut off 2^-22 below its own size, at most 80 times before it is put away
+        tol = ref.output_bound(q[i].double().cpu().numpy(), x.cpu().numpy(), y.cpu().numpy(), 0.0, d ** -0.5) + 80 * 2.0 ** -22 * float(y.abs().max())
+        assert float((out[i].reshape(Hkv, G, d).double() - want).abs().max()) <= tol
+
+
 def test_offsets_past_32_bits():
     """Pages more than 2^31 bytes apart: written by the token call, indexed, attended."""
     from paper_2609_20888_b200 import binding as eb
