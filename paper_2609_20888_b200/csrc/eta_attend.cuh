@@ -87,25 +87,7 @@ struct Attend {
                 qa[hf][m][0] = v.x; qa[hf][m][1] = v.y; qa[hf][m][2] = v.z; qa[hf][m][3] = v.w;
             }
     }
-    // The warp's maxima and sums, for a flush: m, l [8]
-    __device__ __forceinline__ void store_ml(float* m, float* l) const {
-        float lsum = l_run + __shfl_xor_sync(0xffffffffu, l_run, 1);
-        lsum += __shfl_xor_sync(0xffffffffu, lsum, 2);
-        if (t == 0) { m[g] = m_run; l[g] = lsum; }
-    }
-    // the accumulators of heads h0 .. h0 + n - 1 to sm [n][O_STRIDE]
-    static constexpr int O_STRIDE = D;
-    __device__ __forceinline__ void store_o(float* sm, int h0, int n) const {
-        const int ha = 2 * t - h0, hb = ha + 1;         // this lane's two heads within the round
-#pragma unroll
-        for (int hf = 0; hf < HALVES; ++hf)
-#pragma unroll
-            for (int mt = 0; mt < 4; ++mt) {
-                const int dcol = 64 * hf + 8 * vchunk + 2 * mt;
-                if (ha >= 0 && ha < n) *reinterpret_cast<float2*>(sm + ha * D + dcol) = make_float2(o[hf][mt][0], o[hf][mt][2]);
-                if (hb >= 0 && hb < n) *reinterpret_cast<float2*>(sm + hb * D + dcol) = make_float2(o[hf][mt][1], o[hf][mt][3]);
-            }
-    }
+    static constexpr int O_STRIDE = D;             // of a head's accumulators in a flush
     // tau: the thresholds of the group's heads
     __device__ __forceinline__ void load_te(const float* tau) { te = head ? __ldcg(tau + g) : 0.f; }
     // The tile at kbase: nvalid tokens of it are in the sequence, the heads of hmask attend it, token urow (0xff: none) keeps its

@@ -585,7 +585,8 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             const int in_run = Tile::UNITS > 1 ? lane - (31 - __clz((starts | 1u) & (0xffffffffu >> (31 - lane)))) : 0;
             const bool first_of_stage = valid && in_run % Tile::UNITS == 0;
             const unsigned vmask = __ballot_sync(0xffffffffu, first_of_stage);
-            const uint32_t my_fill = fill + (uint32_t)__popc(vmask & (0xffffffffu >> (31 - lane))) - (valid ? 1u : 0u);
+            // (a stage's later units: the number of the fill before theirs)
+            const uint32_t my_fill = fill + (uint32_t)__popc(vmask & ((1u << lane) - 1u)) - (Tile::UNITS > 1 && valid && !first_of_stage ? 1u : 0u);
             const unsigned later = lane < 31 ? vmask >> (lane + 1) : 0u;
             const int n_units = Tile::UNITS > 1 ? min(later ? __ffs(later) : 32, nb - lane) : 1;       // of the stage that starts here
             const int my_piece = piece + __popc(starts & (0xffffffffu >> (31 - lane)));
@@ -711,19 +712,19 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
     constexpr int OS = Tile::Math::O_STRIDE;
     float* sm_o = reinterpret_cast<float*>(smem + L::MO_OFF) + group * WARPS_PER_GROUP * fheads * OS;
     const int gtid = tid - group * 32 * WARPS_PER_GROUP;    // thread index inside the group
-    const float LOG2E = 1.4426950408889634f;
     typename Tile::Math at(lane, wq, a.G);
     int row = -1, piece = -1, q_row = -1;
     uint32_t flush_phase = 0;
     bool ok = true;
+    const float LOG2E = 1.4426950408889634f;
 
     // query fragments and threshold of a row: head g's slice in the permuted head_dim order of the MMA
     auto load_q = [&](int r) {
         int i, hk;
         a.div_hkv.divmod(r, i, hk);
-        const int64_t h = (int64_t)i * a.Hq + hk * a.G;
-        at.load_q(a.q + (h + (at.head ? at.qh : 0)) * D);
-        at.load_te(a.tau_eff + h);
+        const int h = hk * a.G + (at.head ? at.qh : 0);
+        at.load_q(a.q + ((int64_t)i * a.Hq + h) * D);
+        at.load_te(a.tau_eff + (int64_t)i * a.Hq + hk * a.G);
         q_row = r;
     };
     if (!mbar_wait(laybar, 0)) {
@@ -733,53 +734,6 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
     if (s_row0 < 0) return;
     load_q(s_row0);       // the row of the CTA's first unit: fetched while its first tiles are on their way
 
-    // A group's part of a piece is complete: combine its four warps and store (m, l, O) per head.
-    auto flush_piece = [&]() {
-        at.store_ml(sm_m + wq * 8, sm_l + wq * 8);
-        const int64_t slot = ((int64_t)blockIdx.x + row) * NGROUPS + group;
-        for (int h0 = 0; h0 < a.G && ok; h0 += fheads) {
-            if constexpr (!Tile::KV4) at.store_o(sm_o + wq * fheads * OS, h0, fheads);
-#ifdef ETA_TEST_SKIP_FLUSH_ARRIVE
-            // test build only: one warp of the first CTA never arrives, so that the group's bounded wait runs out and
-            // the give-up path (status flag, orderly exit of the whole CTA) executes
-            if (!(blockIdx.x == 0 && group == 0 && wq == 1))
-#endif
-            mbar_arrive(&flushbar[group]);
-            if (!mbar_wait(&flushbar[group], flush_phase)) { ok = false; break; }
-            flush_phase ^= 1;
-            for (int idx = gtid; idx < fheads * D / 4; idx += 32 * WARPS_PER_GROUP) {
-                const int hr = idx / (D / 4), dq = idx % (D / 4), hh = h0 + hr;
-                float mw[WARPS_PER_GROUP], M = -INFINITY;
-#pragma unroll
-                for (int w = 0; w < WARPS_PER_GROUP; ++w) { mw[w] = sm_m[w * 8 + hh]; M = fmaxf(M, mw[w]); }
-                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-                float lacc = 0.f;
-                if (M != -INFINITY) {
-#pragma unroll
-                    for (int w = 0; w < WARPS_PER_GROUP; ++w) {
-                        const float sc = exp2f((mw[w] - M) * LOG2E);
-                        float4 x;
-                        const float* const from = sm_o + (w * fheads + hr) * OS;
-                        if constexpr (Tile::KV4) {
-                            const float2 lo = *reinterpret_cast<const float2*>(from + Tile::Math::o_at(dq)), hi = *reinterpret_cast<const float2*>(from + Tile::Math::o_at(dq) + 16);
-                            x = make_float4(lo.x, lo.y, hi.x, hi.y);
-                        } else {
-                            x = *reinterpret_cast<const float4*>(from + 4 * dq);
-                        }
-                        acc.x = fmaf(x.x, sc, acc.x); acc.y = fmaf(x.y, sc, acc.y);
-                        acc.z = fmaf(x.z, sc, acc.z); acc.w = fmaf(x.w, sc, acc.w);
-                        lacc = fmaf(sm_l[w * 8 + hh], sc, lacc);
-                    }
-                }
-                if constexpr (Tile::KV4) { acc.x *= a.out_scale; acc.y *= a.out_scale; acc.z *= a.out_scale; acc.w *= a.out_scale; }
-                *reinterpret_cast<float4*>(a.part_o + (slot * a.G + hh) * D + 4 * dq) = acc;
-                if (dq == 0) a.part_ml[slot * a.G + hh] = make_float2(M, lacc);
-            }
-            mbar_arrive(&flushbar[group]);
-            if (!mbar_wait(&flushbar[group], flush_phase)) { ok = false; break; }
-            flush_phase ^= 1;
-        }
-    };
     if constexpr (Tile::KV4) {
         // Piece after piece, the stages of a piece in a loop of their own, with neither the fold nor the flush in it: with the flush inside
         // the accumulators were moved between registers once a slab, 53 of 396 instructions (16 x 64K dense: 178K cycles with the fold inside,
@@ -831,7 +785,35 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
                 folded = true;
             } while (more);
             if (!ok) break;
-            flush_piece();
+            // ---- this group's part of a piece is complete: as below, all heads at once
+            at.store_ml(sm_m + wq * 8, sm_l + wq * 8);
+            const int64_t slot = ((int64_t)blockIdx.x + row) * NGROUPS + group;
+            mbar_arrive(&flushbar[group]);
+            if (!mbar_wait(&flushbar[group], 0)) { ok = false; break; }
+            for (int idx = gtid; idx < a.G * D / 4; idx += 32 * WARPS_PER_GROUP) {
+                const int h = idx / (D / 4), dq = idx % (D / 4);
+                float mw[WARPS_PER_GROUP], M = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < WARPS_PER_GROUP; ++w) { mw[w] = sm_m[w * 8 + h]; M = fmaxf(M, mw[w]); }
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                float lacc = 0.f;
+                if (M != -INFINITY) {
+#pragma unroll
+                    for (int w = 0; w < WARPS_PER_GROUP; ++w) {
+                        const float sc = exp2f((mw[w] - M) * LOG2E);
+                        const float* const from = sm_o + (w * fheads + h) * OS + Tile::Math::o_at(dq);
+                        const float2 lo = *reinterpret_cast<const float2*>(from), hi = *reinterpret_cast<const float2*>(from + 16);
+                        acc.x = fmaf(lo.x, sc, acc.x); acc.y = fmaf(lo.y, sc, acc.y);
+                        acc.z = fmaf(hi.x, sc, acc.z); acc.w = fmaf(hi.y, sc, acc.w);
+                        lacc = fmaf(sm_l[w * 8 + h], sc, lacc);
+                    }
+                }
+                acc.x *= a.out_scale; acc.y *= a.out_scale; acc.z *= a.out_scale; acc.w *= a.out_scale;
+                *reinterpret_cast<float4*>(a.part_o + (slot * a.G + h) * D + 4 * dq) = acc;
+                if (dq == 0) a.part_ml[slot * a.G + h] = make_float2(M, lacc);
+            }
+            mbar_arrive(&flushbar[group]);
+            if (!mbar_wait(&flushbar[group], 1)) { ok = false; break; }
         }
         if (!ok && lane == 0 && a.status) atomicOr(a.status, ETA_DEV_TIMEOUT);
         return;
@@ -852,7 +834,55 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         // query registers, and its barriers and stores hide the load's latency
         if (!end && new_piece != piece && ds.x != q_row) load_q(ds.x);
         if ((end || new_piece != piece) && piece >= 0) {
-            flush_piece();
+            // ---- this group's part of a piece is complete: combine its four warps and store (m, l, O) per head
+            float lsum = at.l_run + __shfl_xor_sync(0xffffffffu, at.l_run, 1);
+            lsum += __shfl_xor_sync(0xffffffffu, lsum, 2);
+            if (at.t == 0) { sm_m[wq * 8 + at.g] = at.m_run; sm_l[wq * 8 + at.g] = lsum; }
+            const int64_t slot = ((int64_t)blockIdx.x + row) * NGROUPS + group;
+            for (int h0 = 0; h0 < a.G && ok; h0 += fheads) {
+                const int ha = 2 * at.t - h0, hb = ha + 1;         // this lane's two heads within the round
+#pragma unroll
+                for (int hf = 0; hf < Tile::HALVES; ++hf)
+#pragma unroll
+                    for (int mt = 0; mt < 4; ++mt) {
+                        const int dcol = 64 * hf + 8 * at.vchunk + 2 * mt;
+                        if (ha >= 0 && ha < fheads)
+                            *reinterpret_cast<float2*>(sm_o + ((wq * fheads + ha) * D + dcol)) = make_float2(at.o[hf][mt][0], at.o[hf][mt][2]);
+                        if (hb >= 0 && hb < fheads)
+                            *reinterpret_cast<float2*>(sm_o + ((wq * fheads + hb) * D + dcol)) = make_float2(at.o[hf][mt][1], at.o[hf][mt][3]);
+                    }
+#ifdef ETA_TEST_SKIP_FLUSH_ARRIVE
+                // test build only: one warp of the first CTA never arrives, so that the group's bounded wait runs out and
+                // the give-up path (status flag, orderly exit of the whole CTA) executes
+                if (!(blockIdx.x == 0 && group == 0 && wq == 1))
+#endif
+                mbar_arrive(&flushbar[group]);
+                if (!mbar_wait(&flushbar[group], flush_phase)) { ok = false; break; }
+                flush_phase ^= 1;
+                for (int idx = gtid; idx < fheads * D / 4; idx += 32 * WARPS_PER_GROUP) {
+                    const int hr = idx / (D / 4), dq = idx % (D / 4), hh = h0 + hr;
+                    float mw[WARPS_PER_GROUP], M = -INFINITY;
+#pragma unroll
+                    for (int w = 0; w < WARPS_PER_GROUP; ++w) { mw[w] = sm_m[w * 8 + hh]; M = fmaxf(M, mw[w]); }
+                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                    float lacc = 0.f;
+                    if (M != -INFINITY) {
+#pragma unroll
+                        for (int w = 0; w < WARPS_PER_GROUP; ++w) {
+                            const float sc = exp2f((mw[w] - M) * LOG2E);
+                            const float4 x = *reinterpret_cast<const float4*>(sm_o + (w * fheads + hr) * D + 4 * dq);
+                            acc.x = fmaf(x.x, sc, acc.x); acc.y = fmaf(x.y, sc, acc.y);
+                            acc.z = fmaf(x.z, sc, acc.z); acc.w = fmaf(x.w, sc, acc.w);
+                            lacc = fmaf(sm_l[w * 8 + hh], sc, lacc);
+                        }
+                    }
+                    *reinterpret_cast<float4*>(a.part_o + (slot * a.G + hh) * D + 4 * dq) = acc;
+                    if (dq == 0) a.part_ml[slot * a.G + hh] = make_float2(M, lacc);
+                }
+                mbar_arrive(&flushbar[group]);
+                if (!mbar_wait(&flushbar[group], flush_phase)) { ok = false; break; }
+                flush_phase ^= 1;
+            }
             if (!ok) break;
         }
         if (end) {
@@ -860,6 +890,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             break;
         }
 
+        const int hmask = ds.z & 0xff, urow = (ds.z >> 8) & 0xff, nvalid = ds.w;
         const uint32_t kbase = smem_u32(smem + stage * STAGE_BYTES);
 
         if (new_piece != piece) {
@@ -870,7 +901,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         }
 
         // the arrive (release) orders the warp's reads of the stage before the producer's next copy into it
-        at.tile(kbase, ds.z & 0xff, (ds.z >> 8) & 0xff, ds.w, a.scale, a.beta, [&]() { if (lane == 0) mbar_arrive(&empty[stage]); });
+        at.tile(kbase, hmask, urow, nvalid, a.scale, a.beta, [&]() { if (lane == 0) mbar_arrive(&empty[stage]); });
     }
     if (!ok && lane == 0 && a.status) atomicOr(a.status, ETA_DEV_TIMEOUT);
     }
