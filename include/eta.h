@@ -358,7 +358,7 @@ int eta_plan_pages(int32_t batch, int32_t block_size, int32_t t_cap, const int32
  * q, k, v are [n_rows, heads, head_dim] of one type, unit stride along head_dim, the other strides multiples of 16 bytes; they may be
  * parts of one projection.  Pointers 16-byte aligned (slot_map and inv_freq 8, positions 4).  Of the cache descriptor n_q_heads, n_kv_heads,
  * head_dim, block_size, batch, t_cap and strides are used; unlike a step's, batch * n_kv_heads is not limited.  rotary_dim: a
- * multiple of 16 up to head_dim; 0: no rotation, inv_freq and positions may be NULL.
+ * multiple of 16 up to head_dim; 0: no rotation, inv_freq and positions may be NULL.  n_rows <= 2^30.
  * Launched with programmatic dependent launch: the kernel waits for everything before it in the stream before it reads or
  * writes, and releases its successors only as it ends.
  */
