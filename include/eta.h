@@ -352,7 +352,8 @@ int eta_plan_pages(int32_t batch, int32_t block_size, int32_t t_cap, const int32
  * A row with a negative slot is skipped: nothing of it is read or written, its row of q_out included.  A slot past the cache is
  * skipped too and sets ETA_DEV_BAD_SLOT.  The rows of a call have different slots (of two rows with one slot the cache would hold
  * either, or a mixture).  Places that no row names keep their bytes.
- * Arithmetic is fp32 with one rounding, to bf16, at the end.  For the 4-bit cache keys are worked out in fp64 up to the quotient that
+ * Arithmetic is fp32 with one rounding, to bf16, at the end (a head whose squares leave fp32's range is not normalised for what it
+ * is: its sum counts as infinite, or as zero).  For the 4-bit cache keys are worked out in fp64 up to the quotient that
  * is rounded to a code, so that a key next to a border between two codes gets the same one whatever the order of the sums: the
  * same tokens give the same bytes.
  * q, k, v are [n_rows, heads, head_dim] of one type, unit stride along head_dim, the other strides multiples of 16 bytes; they may be

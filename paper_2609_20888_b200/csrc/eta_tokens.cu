@@ -113,17 +113,21 @@ struct Turn {
             S[k] = turns ? (minus ? -wp : wp) * sv : (F)0;
         }
     }
-    // x: the lane's channels, y: their partners.  With m: also the sizes |x C| + |x_partner S| times r, which bound what rounding did.
+    // x: the lane's channels, y: their partners.  With m: also the sizes |x C| + |x_partner S| times r, which bound what rounding did;
+    // the first infinite where the squares have left fp32's range.
     template <int D, bool SIZES = false>
     __device__ __forceinline__ void apply(F (&x)[8], const F (&y)[8], bool norm, float eps, F* m = nullptr) const {
         F r = 1;
+        bool lost = false;
         if (norm) {
             F ss = 0;
 #pragma unroll
             for (int k = 0; k < 8; ++k) ss = fma(x[k], x[k], ss);
 #pragma unroll
             for (int s = 1; s < D / 8; s <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, s);
-            r = rsqrt(ss * (F)(1.0 / D) + (F)eps);
+            const F mean = ss * (F)(1.0 / D) + (F)eps;
+            lost = !(mean > (F)1e-30 && mean < (F)1e30);
+            r = rsqrt(mean);
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -135,6 +139,7 @@ struct Turn {
                 x[k] = fma(x[k], C[k], y[k] * S[k]) * r;
             }
         }
+        if constexpr (SIZES) m[0] = lost ? (F)INFINITY : m[0];
     }
 };
 

@@ -194,6 +194,26 @@ def test_kv4_ties_zeros_infinities_and_nans(dtype):
     assert np.array_equal(K[0].double().cpu().numpy(), ref.decode(c, s, 1.0).transpose(1, 0, 2), equal_nan=True)
 
 
+@pytest.mark.parametrize("size,eps", [(1e22, 1e-6), (1e-22, 0.0), (1e-19, 0.0), (1e-25, 1e-6)])
+def test_kv4_keys_whose_squares_leave_fp32(size, eps):
+    """Keys are those of the 64-bit norm, bytes and all, where fp32 could not hold the sum of their squares."""
+    from paper_2609_20888_b200 import binding as eb
+    rows, d, block = 32, 128, 32
+    q, k, v = inputs(rows, 2, 2, d, "fp32", 9)
+    k = k * size
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda") * 1000
+    w = torch.rand(d, device="cuda") + 0.5
+    inv = (10000.0 ** -(torch.arange(64, dtype=torch.float64) / 64)).cuda()
+    pool = torch.zeros((1, 2, eb.kv4_block_bytes(block, d)), dtype=torch.uint8, device="cuda")
+    desc, kv4 = eb.kv4_cache_desc(pool, 2, d, block, batch=1, t_cap=block)
+    q_out = torch.empty((rows, 2, d), dtype=torch.bfloat16, device="cuda")
+    eb.eta_append_tokens_kv4(desc, kv4, q, k, v, torch.arange(rows, device="cuda"), pos, q_out, pool, inv_freq=inv, k_weight=w, eps=eps)
+    _, _, yk, _, _ = expected(q, k, v, pos, None, w, inv, False, eps)
+    c, s = ref.encode(yk, 1.0)
+    kc, ks, _, _ = ref.split(pool.cpu().numpy(), block, d)
+    assert np.array_equal(kc[0], c.transpose(1, 0, 2)) and np.array_equal(ks[0], s.transpose(1, 0, 2))
+
+
 @pytest.mark.parametrize("four", [False, True])
 def test_far_positions_keep_their_angle(four):
     """Positions up to the last 32-bit one, frequencies from 1 down: bytes, or bf16 values, of the 64-bit angle."""
