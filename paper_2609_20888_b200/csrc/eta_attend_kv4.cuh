@@ -324,7 +324,7 @@ struct AttendKv4 {
         l0 += p[0] + p[2];
         l1 += p[1] + p[3];
         // ---- P as the B operand: the value cut off after eleven bits, and what that leaves.  Up to four heads, columns 0 .. 3 get the value (with
-        // its sign turned, which store_o undoes) and 4 .. 7 the remainder, by one fma: p * 0 - value, p * 1 - value.
+        // its sign turned, which fold undoes) and 4 .. 7 the remainder, by one fma: p * 0 - value, p * 1 - value.
         uint32_t bh[2], bl[2] = {0u, 0u};
 #pragma unroll
         for (int h = 0; h < 2; ++h) {

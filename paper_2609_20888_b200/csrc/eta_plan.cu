@@ -6,8 +6,8 @@
 //   row r of sequence i: position p = len_i + (r - row_start_i), slot = table[i][p / b] * b + p % b
 //
 // Everything that depends on an order hangs on three prefix sums over the sequences (rows, pages back, pages needed): plan_kernel
-// is one CTA that scans them 1024 sequences at a time, and moves the pages with a thread per page (found in the scan by
-// bisection), so that a few long prompts do not leave it to a few threads.  The rows are its work too while they are few; beyond
+// is one CTA that scans them 1024 sequences at a time, and moves the pages in equal shares of a warp (whose sequences are found in the
+// scan by bisection), so that a few long prompts do not leave it to a few threads.  The rows are its work too while they are few; beyond
 // that a kernel over all rows follows.
 #include "eta_common.cuh"
 
@@ -62,6 +62,34 @@ __device__ __forceinline__ int last_not_above(const int32_t* v, int n, int32_t x
     return lo;
 }
 
+// Pages 0 .. n - 1; s is the last of n_seq ascending numbers that is not above p.  A warp takes consecutive pages, so that it looks for its first
+// sequence once and a lane looks again only where its page is past the sequence it is at: with a bisection per page it was the instructions of
+// one SM that 200 requests with prompts waited for (21.5 -> 17.5 us).  MOVE loads before the first store, which the compiler would not do, since tables and stack could be the same memory.
+constexpr int MOVE = 8;
+template <typename Load, typename Store>
+__device__ __forceinline__ void move_pages(const int32_t* before, int n_seq, int n, Load load, Store store) {
+    const int per_warp = (n + PLAN_THREADS - 1) / PLAN_THREADS * 32, begin = (threadIdx.x >> 5) * per_warp, end = min(n, begin + per_warp);
+    if (begin >= end) return;
+    int s = last_not_above(before, n_seq, begin), next = s + 1 < n_seq ? before[s + 1] : INT32_MAX;
+    for (int p0 = begin + (threadIdx.x & 31); p0 < end; p0 += 32 * MOVE) {
+        int of[MOVE], page[MOVE];
+#pragma unroll
+        for (int u = 0; u < MOVE; ++u) {
+            const int p = p0 + 32 * u;
+            if (p >= end) continue;
+            if (p >= next) {
+                s += last_not_above(before + s, n_seq - s, p);
+                next = s + 1 < n_seq ? before[s + 1] : INT32_MAX;
+            }
+            of[u] = s;
+            page[u] = load(s, p);
+        }
+#pragma unroll
+        for (int u = 0; u < MOVE; ++u)
+            if (p0 + 32 * u < end) store(of[u], p0 + 32 * u, page[u]);
+    }
+}
+
 // What a row of a sequence needs: position = row + shift; NO_PLACE where the sequence got nothing
 constexpr int32_t NO_PLACE = INT32_MIN;
 __device__ __forceinline__ int32_t shift_of(int len_after, int got, int row0) { return got > 0 ? len_after - got - row0 : NO_PLACE; }
@@ -86,16 +114,25 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const PlanArgs a, co
     pdl_wait();
     if (!rows_here) pdl_trigger();          // the rows' kernel, which waits for this one
     int n_free = __ldcg(a.n_free);
+    // the first 1024 sequences' numbers at once, before anything is waited for (cold, every one of them is a microsecond)
+    int32_t fresh0 = 0, gone0 = 0, len0 = 0;
+    auto fetch = [&](int i, int32_t& fresh, int32_t& gone, int32_t& len) {
+        fresh = gone = len = 0;
+        if (i >= a.batch) return;
+        if (a.release) gone = __ldcg(a.release + i);
+        len = __ldcg(a.seq_lens + i);
+        fresh = __ldcg(a.new_lens + i);
+    };
+    fetch(tid, fresh0, gone0, len0);
     n_free = n_free < 0 ? 0 : (n_free > a.n_pages ? a.n_pages : n_free);
     bool refused = false;
 
     // ---- pages of released sequences go back
     if (a.release) {
         for (int c = 0; c < a.batch; c += PLAN_THREADS) {
-            const int i = c + tid;
-            int gone = 0;
-            if (i < a.batch && __ldcg(a.release + i) != 0) {
-                const int len = __ldcg(a.seq_lens + i);
+            int32_t fresh = fresh0, gone = gone0, len = len0;
+            if (c) fetch(c + tid, fresh, gone, len);
+            if (gone != 0) {
                 gone = len <= 0 ? 0 : (int)(((int64_t)len + b - 1) >> a.b_shift);
                 if (gone > a.table_stride) { gone = a.table_stride; refused = true; }
             }
@@ -104,11 +141,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const PlanArgs a, co
             __syncthreads();
             if (all.x > a.n_pages - n_free) { all.x = a.n_pages - n_free; refused = true; }      // more than were ever handed out
             const int n_seq = min(PLAN_THREADS, a.batch - c), n = (int)all.x;
-#pragma unroll 4
-            for (int p = tid; p < n; p += PLAN_THREADS) {
-                const int s = last_not_above(s_before, n_seq, p);
-                a.free_pages[n_free + p] = __ldcg(a.block_table + (int64_t)(c + s) * a.table_stride + (p - s_before[s]));
-            }
+            move_pages(s_before, n_seq, n, [&](int s, int p) { return __ldcg(a.block_table + (int64_t)(c + s) * a.table_stride + (p - s_before[s])); },
+                       [&](int, int p, int page) { a.free_pages[n_free + p] = page; });
             n_free += n;
             __syncthreads();
         }
@@ -121,11 +155,11 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const PlanArgs a, co
     const bool one_chunk = a.batch <= PLAN_THREADS;
     for (int c = 0; c < a.batch; c += PLAN_THREADS) {
         const int i = c + tid, n_seq = min(PLAN_THREADS, a.batch - c);
-        int len = 0, fresh = 0, held = 0, need = 0;
-        if (i < a.batch) {
-            fresh = max(0, __ldcg(a.new_lens + i));
-            len = a.release && __ldcg(a.release + i) != 0 ? 0 : max(0, __ldcg(a.seq_lens + i));
-        }
+        int32_t fresh = fresh0, gone = gone0, len = len0;
+        if (c) fetch(i, fresh, gone, len);
+        fresh = max(0, fresh);
+        len = gone != 0 ? 0 : max(0, len);
+        int held = 0, need = 0;
         bool fits = (int64_t)len + fresh <= a.t_cap;
         if (fits) {
             held = (int)(((int64_t)len + b - 1) >> a.b_shift);
@@ -153,11 +187,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const PlanArgs a, co
         }
         __syncthreads();
         const int n = (int)(s_taken < all.y ? s_taken : all.y);
-#pragma unroll 4
-        for (int p = tid; p < n; p += PLAN_THREADS) {
-            const int s = last_not_above(s_before, n_seq, p);
-            a.block_table[(int64_t)(c + s) * a.table_stride + s_held[s] + (p - s_before[s])] = a.free_pages[n_free - 1 - taken - p];
-        }
+        move_pages(s_before, n_seq, n, [&](int, int p) { return __ldcg(a.free_pages + n_free - 1 - taken - p); },
+                   [&](int s, int p, int page) { a.block_table[(int64_t)(c + s) * a.table_stride + s_held[s] + (p - s_before[s])] = page; });
         taken += n;
         rows_done += all.x;
         pages_done += all.y;
