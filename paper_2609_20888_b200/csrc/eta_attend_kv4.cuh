@@ -11,6 +11,8 @@
 //     repeat the heads of 0 to 3, whose lanes compute the same scores again and feed the remainder.
 //   - the running maximum follows the scores only when one is more than SLACK above it: exp(s - m) is then at most 2^6, and with
 //     the factor 2^BASE, which every part carries and the final division drops, inside fp16's range at both ends.
+// Bound by instructions: a conversion makes two numbers in two cycles of a scheduler, an MMA takes eight that add to them.  16 x 8K to 64K tokens
+// of 4 heads, all attended: 92 to 102 us a step (340 MB: 3.3 to 3.7 TB/s, half a copy's rate); 4 x 128K of 8 heads, a tenth of the blocks: 35 us.
 #pragma once
 
 #include "eta_attend.cuh"
