@@ -112,7 +112,7 @@ struct Turn {
             const F wp = interleaved ? v[k ^ 1] : v[k], cv = interleaved ? c[k / 2] : c[k], sv = interleaved ? s[k / 2] : s[k];
             const bool minus = interleaved ? !(k & 1) : first;
             C[k] = turns ? w[k] * cv : w[k];
-            S[k] = turns ? (minus ? -wp : wp) * sv : (F)0;
+            S[k] = turns ? (minus ? -wp : wp) * sv : (F)-0.0;      // (adds -0 to channels that stay: a zero keeps its sign)
         }
     }
     // x: the lane's channels, y: their partners.  With m: also the sizes |x C| + |x_partner S| times r, which bound what rounding did;
@@ -179,7 +179,8 @@ __device__ __forceinline__ Kv4Codes codes_exact(const double (&x)[8], double g) 
 }
 
 // Values as they came, where scale * g is exact in fp32 (g of at most 20 significant bits): the quotient correctly rounded from a rounded
-// reciprocal and the remainder (Markstein's division), so that ties are ties.
+// reciprocal and the remainder (Markstein's division), so that ties are ties.  The remainder is taken with its sign turned: that way a zero
+// keeps its own.
 __device__ __forceinline__ Kv4Codes codes_of_values(const float (&x)[8], float g) {
     float top = 0.f;
 #pragma unroll
@@ -191,7 +192,7 @@ __device__ __forceinline__ Kv4Codes codes_of_values(const float (&x)[8], float g
     const float inv = any ? __frcp_rn(sg) : 0.f;
     const uint32_t codes = e2m1x8([&](int k) {
         const float y = x[k] * inv;
-        return fabsf(y) < 8.f ? fmaf(fmaf(-y, sg, x[k]), inv, y) : y;          // (beyond 8, infinities among them, it saturates)
+        return fabsf(y) < 8.f ? fmaf(-fmaf(y, sg, -x[k]), inv, y) : y;          // (beyond 8, infinities among them, it saturates)
     });
     return {any ? codes : 0u, scale};
 }
@@ -215,10 +216,11 @@ __device__ __forceinline__ bool codes_of_keys(const float (&x)[8], const float (
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         y[k] = x[k] * inv;
-        y[k] = fabsf(y[k]) < 8.f ? fmaf(fmaf(-y[k], sg, x[k]), inv, y[k]) : y[k];
+        y[k] = fabsf(y[k]) < 8.f ? fmaf(-fmaf(y[k], sg, -x[k]), inv, y[k]) : y[k];
         e[k] = fmaf(m[k], off_y, fabsf(y[k]) * round_y);
     }
-    out.codes = any ? e2m1x8([&](int k) { return y[k] + e[k]; }) : 0u;
+    // (y + e as the negative of -y - e, whose codes differ in the sign bit: with e = 0 a zero keeps its sign in both)
+    out.codes = any ? e2m1x8([&](int k) { return -y[k] - e[k]; }) ^ 0x88888888u : 0u;
     const uint32_t low = any ? e2m1x8([&](int k) { return y[k] - e[k]; }) : 0u;
     return __all_sync(0xffffffffu, top < 1e30f && (pair >> 8) == out.scale && low == out.codes);
 }
@@ -244,7 +246,7 @@ __device__ __forceinline__ void turn_exact(const TokensArgs& a, double (&x)[8], 
         if (turns) sincos(reduced_angle(a, row, pair), &sn, &cs);
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            if (k == n) x[k] = fma(x[k], w * cs, y[k] * ((minus ? -wp : wp) * sn)) * r;
+            if (k == n) x[k] = fma(x[k], w * cs, y[k] * (turns ? (minus ? -wp : wp) * sn : -0.0)) * r;
     }
 }
 
@@ -310,7 +312,7 @@ __device__ __forceinline__ void queries(const TokensArgs& a, int64_t row, int be
             const bool minus = INTER ? !(k & 1) : k < 4;
             const float wp = w[INTER ? k ^ 1 : k ^ 4];
             C[k] = turns ? w[k] * cv[pair] : w[k];
-            S[k] = turns ? (minus ? -wp : wp) * sv[pair] : 0.f;
+            S[k] = turns ? (minus ? -wp : wp) * sv[pair] : -0.f;
         }
     }
     const bool some_stay = a.rotary < D;
