@@ -77,10 +77,21 @@ __device__ __forceinline__ uint4 pack_bf16(const float (&x)[8]) {
     return o;
 }
 
-// The angle of a row's pair, reduced by whole turns with a two-part 2 pi (Cody and Waite): any 32-bit position keeps its 64-bit angle
-__device__ __forceinline__ double reduced_angle(const TokensArgs& a, int64_t row, int pair) {
-    const double x = (double)__ldcg(a.positions + row) * __ldcg(a.inv_freq + pair), n = rint(x * 0.15915494309189535);
-    return fma(-n, 2.4492935982947064e-16, fma(-n, 6.283185307179586, x));
+// Sine and cosine of a row's pair.  The 64-bit angle is reduced by whole quarter turns with a two-part pi / 2 (Cody and Waite; the first difference
+// is exact, so that what is left is as good as 64 bits however little that is): any 32-bit position keeps its angle, and next to a multiple of pi / 2
+// the small one of the two is the sine of a small number, whose relative error F's rounding keeps small.  Rounding the angle itself to fp32
+// moved a small factor by up to 2^-23 whatever its size.
+__device__ __forceinline__ void sincos_of(float x, float* s, float* c) { sincosf(x, s, c); }
+__device__ __forceinline__ void sincos_of(double x, double* s, double* c) { sincos(x, s, c); }
+template <typename F>
+__device__ __forceinline__ void turn_of(const TokensArgs& a, int64_t row, int pair, F& sn, F& cs) {
+    const double x = (double)__ldcg(a.positions + row) * __ldcg(a.inv_freq + pair), n = rint(x * 0.6366197723675814);
+    const int quarters = (int)__double2ll_rn(n);
+    F s, c;
+    sincos_of((F)fma(-n, 6.123233995736766e-17, fma(-n, 1.5707963267948966, x)), &s, &c);
+    sn = (quarters & 1) ? c : s;
+    cs = (quarters & 1) ? -s : c;
+    if (quarters & 2) { sn = -sn; cs = -cs; }
 }
 
 // What a lane's eight channels are multiplied with, norm weight and rotation in one: y = (x C + x_partner S) r, where x_partner are the pairs'
@@ -116,7 +127,9 @@ struct Turn {
         }
     }
     // x: the lane's channels, y: their partners.  With m: also the sizes |x C| + |x_partner S| times r, which bound what rounding did;
-    // the first infinite where the squares have left fp32's range.
+    // the first infinite where the squares have left fp32's range.  In units of 2^-24 of m, what comes before C, S or r is good to: an angle 1, its sine or
+    // cosine 4 (two places), the product with w 1; the products with x and their sum 2; r 10.5 (thirteen roundings in the mean, half of which a
+    // root passes on, and two places of its own) and its product 1: less than 20, where codes_of_keys allows 32.
     template <int D, bool SIZES = false>
     __device__ __forceinline__ void apply(F (&x)[8], const F (&y)[8], bool norm, float eps, F* m = nullptr) const {
         F r = 1;
@@ -243,7 +256,7 @@ __device__ __forceinline__ void turn_exact(const TokensArgs& a, double (&x)[8], 
         const bool minus = a.interleaved ? !(n & 1) : cl < reach;
         const double w = a.k_weight ? a.k_weight[c] : 1.f, wp = a.k_weight && turns ? a.k_weight[other] : 1.f;
         double cs = 1, sn = 0;
-        if (turns) sincos(reduced_angle(a, row, pair), &sn, &cs);
+        if (turns) turn_of(a, row, pair, sn, cs);
 #pragma unroll
         for (int k = 0; k < 8; ++k)
             if (k == n) x[k] = fma(x[k], w * cs, y[k] * (turns ? (minus ? -wp : wp) * sn : -0.0)) * r;
@@ -381,7 +394,7 @@ __global__ void __launch_bounds__(32 * TOK_WARPS, sizeof(T) == 4 ? 4 : 5) append
     // the row's angles, by all its warps of the CTA: every warp of a CTA comes here once
     auto angles = [&]() {
         if (a.rotary && live)
-            for (int c = sub; c < a.rotary / 2; c += others_by) sincosf((float)reduced_angle(a, row, c), sn + c, cs + c);
+            for (int c = sub; c < a.rotary / 2; c += others_by) turn_of(a, row, c, sn[c], cs[c]);
         __syncthreads();
     };
     if (!live) {
