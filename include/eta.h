@@ -327,7 +327,8 @@ int eta_decode_paged(const eta_cache_desc* desc, const eta_page_table* pages, co
  *      tokens or not (row_start int32 [batch + 1], saturating).  For every row r < n_rows: positions[r] (int32) the token's position
  *      in its sequence and slot_map[r] (int64) = page * block_size + token of the page, as eta_append_tokens takes it; 0 and
  *      -1 for rows without a place (a sequence that got none, and what is left behind the last sequence).
- * Anything that could not be served sets ETA_DEV_REFUSED.  A release of more pages than are missing from the stack is cut off there.
+ * Anything that could not be served sets ETA_DEV_REFUSED.  A release of more pages than are missing from the stack is cut off there, and
+ * one of a length past t_cap at the ceil(t_cap / block_size) pages that a sequence can have.
  * Page numbers are handed on as they are.  block_size 32, 64 or 128; table_stride * block_size >= t_cap; n_rows <= 2^30.  n_rows = 0:
  * slot_map and positions may be NULL.
  * Launched with programmatic dependent launch: waits for everything before it in the stream before it reads or writes, and the rows'

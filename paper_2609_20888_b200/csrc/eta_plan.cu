@@ -112,6 +112,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const PlanArgs a, co
     __shared__ int32_t s_before[PLAN_THREADS], s_held[PLAN_THREADS], s_row0[PLAN_THREADS + 1], s_shift[PLAN_THREADS];
     __shared__ int s_taken;
     const int tid = threadIdx.x, b = 1 << a.b_shift;
+    // pages that a sequence can hold: what a table's row has beyond them (up to its stride) is nobody's
+    const int most = (int)(((int64_t)a.t_cap + b - 1) >> a.b_shift);
     pdl_wait();
     if (!rows_here) pdl_trigger();          // the rows' kernel, which waits for this one
     int n_free = __ldcg(a.n_free);
@@ -135,7 +137,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const PlanArgs a, co
             if (c) fetch(c + tid, fresh, gone, len);
             if (gone != 0) {
                 gone = len <= 0 ? 0 : (int)(((int64_t)len + b - 1) >> a.b_shift);
-                if (gone > a.table_stride) { gone = a.table_stride; refused = true; }
+                if (gone > most) { gone = most; refused = true; }
             }
             longlong2 all;
             s_before[tid] = saturated(scan(gone, 0, all, s_warp).x);
