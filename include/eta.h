@@ -433,7 +433,8 @@ int eta_append_summary_kv4(const eta_cache_desc* desc, const eta_kv4_desc* kv4, 
 /*
  * eta_decode over a 4-bit cache, contiguous or, with `pages` not NULL, paged: the same screening, rescue, gate, masks, tail, statistics
  * and status, on the keys and values as the cache holds them.  musig and mnorm come from the calls above.  A code times its scale is
- * exact in fp16, products are exact and sums fp32; probabilities are held to 22 bits for the second product.  Always the general path
+ * exact in fp16, products are exact and sums fp32; a token's weight enters the second product to 2^-24 of itself, or to 2^-45 of the
+ * largest weight where that is more.  Always the general path
  * (three kernels, four with a long rescue window).  A NaN in a block reaches the heads that attend the block and no others.
  * Launch order, determinism, errors: as eta_decode.  workspace: eta_kv4_workspace_bytes() bytes, 256-byte aligned.
  */

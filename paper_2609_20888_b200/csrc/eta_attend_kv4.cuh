@@ -7,8 +7,10 @@
 //   - a code is converted by the hardware, two at a time, and scaled as an fp16 pair: code * scale is exact in fp16, so both products are
 //     exact and their sums fp32.  Queries are scaled by a power of two per head to use fp16's range (their bf16 values stay exact
 //     down to 2^-38 of the head's largest).
-//   - probabilities are fed as an fp16 value and an fp16 remainder (22 bits).  Up to four heads, both are columns of one MMA: columns 4 to 7
-//     repeat the heads of 0 to 3, whose lanes compute the same scores again and feed the remainder.
+//   - probabilities are fed as the nearest fp16 value and 2^11 times what that leaves, in fp16 (24 bits; remainders as they are would be subnormal from
+//     2^-12 of the largest weight on, and all that an output is made of is smaller where one token has the weight and next to no value).  Up
+//     to four heads, both are columns of one MMA: columns 4 to 7 repeat the heads of 0 to 3, whose lanes compute the same scores again and feed
+//     the remainder.  With eight heads the remainders' MMA starts from zero and its sums are added 2^-11 fold.
 //   - the running maximum follows the scores only when one is more than SLACK above it: exp(s - m) is then at most 2^6, and with
 //     the factor 2^BASE, which every part carries and the final division drops, inside fp16's range at both ends.
 // Bound by instructions: a conversion makes two numbers in two cycles of a scheduler, an MMA takes eight that add to them.  16 x 8K to 64K tokens
@@ -68,6 +70,13 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// a, b -= 2048 times the halves of v: exact
+__device__ __forceinline__ void sub_rest(float& a, float& b, uint32_t v) {
+    asm("{\n\t.reg .b16 l, h, m;\n\tmov.b32 {l, h}, %2;\n\tmov.b16 m, 0xe800;\n\t"
+        "fma.rn.f32.f16 %0, l, m, %0;\n\tfma.rn.f32.f16 %1, h, m, %1;\n\t}"
+        : "+f"(a), "+f"(b) : "r"(v));
+}
+
 __device__ __forceinline__ bool has_nan(uint32_t p) {
     const __half2 h = *reinterpret_cast<const __half2*>(&p);
     return !__hbeq2(h, h);
@@ -89,13 +98,14 @@ struct AttendKv4 {
     static constexpr int CR = D / 2, SR = D / 16;          // bytes of a row's codes and scales
     static constexpr Kv4Block AT = Kv4Block(b, D);
     static constexpr float BASE = 9.f, SLACK = 4.f;        // 2^9, e^4 < 2^6
+    static constexpr float REST = 2048.f;                  // what remainders are multiplied with
     static constexpr float NONE = -1e30f;                  // the maximum of no score: every score is more than SLACK above it
     int g, t, qh;
     bool head;                                             // the lane's query column is a head
     int c0;                                                // head of column 2 t (of 2 t + 1: c0 + 1)
     bool has0, has1;
     uint32_t all;                                          // bits of the group's heads
-    float own;                                             // 1 in the lanes that feed a weight's remainder, 0 in those that feed the value
+    bool rest;                                             // up to four heads: the lane feeds a weight's remainder, not the value
     uint32_t qb[2 * MT];
     float back0, back1;                                    // undo the queries' powers of two
     float te0, te1;
@@ -111,7 +121,7 @@ struct AttendKv4 {
         c0 = WIDE ? 2 * t : (2 * t) & 3;
         has0 = c0 < G; has1 = c0 + 1 < G;
         all = (1u << G) - 1;
-        own = t < 2 ? 0.f : 1.f;
+        rest = t >= 2;
         te0 = te1 = 0.f;
         gate_on = true;
         back0 = back1 = 1.f;
@@ -189,7 +199,7 @@ struct AttendKv4 {
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 x[c] = o[mt][c];
-                if (!WIDE) x[c] = __shfl_xor_sync(0xffffffffu, x[c], 2) - x[c];       // remainders' columns less the (negated) values'
+                if (!WIDE) x[c] = fmaf(__shfl_xor_sync(0xffffffffu, x[c], 2), 1.f / REST, x[c]);       // values' columns and remainders'
                 o[mt][c] = 0.f;
             }
             if (!WIDE && t >= 2) continue;
@@ -325,18 +335,18 @@ struct AttendKv4 {
         for (int k = 0; k < 4; ++k) p[k] = ex2_approx(fmaf(x[k] - ((k & 1) ? m1 : m0), LOG2E, BASE));      // -inf gives 0
         l0 += p[0] + p[2];
         l1 += p[1] + p[3];
-        // ---- P as the B operand: the value cut off after eleven bits, and what that leaves.  Up to four heads, columns 0 .. 3 get the value (with
-        // its sign turned, which fold undoes) and 4 .. 7 the remainder, by one fma: p * 0 - value, p * 1 - value.
+        // ---- P as the B operand: the nearest fp16 value, and REST times what that leaves.  A weight is held to 2^-24 of itself, or to 2^-36 in p, that is
+        // 2^-45 of the warp's largest, where that is more.
         uint32_t bh[2], bl[2] = {0u, 0u};
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const float v0 = __uint_as_float(__float_as_uint(p[2 * h]) & 0xffffe000u), v1 = __uint_as_float(__float_as_uint(p[2 * h + 1]) & 0xffffe000u);
-            if (WIDE) {
-                bh[h] = transpose8(pack_f16(v0, v1));
-                bl[h] = transpose8(pack_f16(p[2 * h] - v0, p[2 * h + 1] - v1));
-            } else {
-                bh[h] = transpose8(pack_f16(fmaf(p[2 * h], own, -v0), fmaf(p[2 * h + 1], own, -v1)));
-            }
+            const uint32_t v = pack_f16(p[2 * h], p[2 * h + 1]);
+            float r0, r1;
+            mul2(r0, r1, p[2 * h], p[2 * h + 1], REST, REST);
+            sub_rest(r0, r1, v);
+            const uint32_t r = pack_f16(r0, r1);
+            bh[h] = transpose8(WIDE ? v : (rest ? r : v));
+            if (WIDE) bl[h] = transpose8(r);
         }
         // ---- O^T += V^T P
 #pragma unroll
@@ -354,7 +364,12 @@ struct AttendKv4 {
             }
             if (WIDE) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) mma_f16_16816(o[4 * w + k], e01[k], d01[k], e23[k], d23[k], bl[0], bl[1]);
+                for (int k = 0; k < 4; ++k) {
+                    float x[4];
+                    mma_f16_16816_first(x, e01[k], d01[k], e23[k], d23[k], bl[0], bl[1]);
+                    fma2(o[4 * w + k][0], o[4 * w + k][1], x[0], x[1], 1.f / REST, 1.f / REST);
+                    fma2(o[4 * w + k][2], o[4 * w + k][3], x[2], x[3], 1.f / REST, 1.f / REST);
+                }
             }
         }
     }
