@@ -54,13 +54,22 @@ __device__ __forceinline__ longlong2 scan(int64_t x, int64_t y, longlong2& all, 
 __device__ __forceinline__ int32_t saturated(int64_t x) { return (int32_t)(x > INT32_MAX ? INT32_MAX : x); }
 
 // the last of n ascending numbers, the first of which is not above x, that is not above x
-__device__ __forceinline__ int last_not_above(const int32_t* v, int n, int32_t x) {
+template <typename At>
+__device__ __forceinline__ int last_where_not_above(At at, int n, int32_t x) {
     int lo = 0, hi = n;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (v[mid] <= x) lo = mid; else hi = mid;
+        if (at(mid) <= x) lo = mid; else hi = mid;
     }
     return lo;
+}
+// of numbers in shared memory
+__device__ __forceinline__ int last_not_above(const int32_t* v, int n, int32_t x) {
+    return last_where_not_above([&](int k) { return v[k]; }, n, x);
+}
+// of numbers in global memory, which this launch or the one before it wrote
+__device__ __forceinline__ int last_not_above_in_memory(const int32_t* v, int n, int32_t x) {
+    return last_where_not_above([&](int k) { return __ldcg(v + k); }, n, x);
 }
 
 // Pages 0 .. n - 1; s is the last of n_seq ascending numbers that is not above p.  A warp takes consecutive pages, so that it looks for its first
@@ -209,7 +218,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const PlanArgs a, co
                 shift = s_shift[i];
             }
         } else if (r < __ldcg(a.row_start + a.batch)) {
-            i = last_not_above(a.row_start, a.batch, r);
+            i = last_not_above_in_memory(a.row_start, a.batch, r);
             shift = shift_of(__ldcg(a.seq_lens_out + i), __ldcg(a.granted + i), __ldcg(a.row_start + i));
         }
         store_row(a, r, i, shift);
@@ -252,7 +261,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) plan_rows_kernel(const PlanArgs 
     for (int u = 0; u < ROWS_PER_CTA / ROWS_THREADS; ++u) {
         const int r = r0 + tid + u * ROWS_THREADS;
         if (r >= r1) break;
-        const int k = last_not_above(near ? s_row0 : a.row_start + lo, n, r);
+        const int k = near ? last_not_above(s_row0, n, r) : last_not_above_in_memory(a.row_start + lo, n, r);
         store_row(a, r, lo + k, near ? s_shift[k] : shift_at(lo + k));
     }
 }
