@@ -17,6 +17,8 @@
 // of 4 heads, all attended: 92 to 102 us a step (340 MB: 3.3 to 3.7 TB/s, half a copy's rate); 4 x 128K of 8 heads, a tenth of the blocks: 35 us.
 #pragma once
 
+#include <float.h>
+
 #include "eta_attend.cuh"
 #include "eta_kv4.cuh"
 
@@ -99,7 +101,7 @@ struct AttendKv4 {
     static constexpr Kv4Block AT = Kv4Block(b, D);
     static constexpr float BASE = 9.f, SLACK = 4.f;        // 2^9, e^4 < 2^6
     static constexpr float REST = 2048.f;                  // what remainders are multiplied with
-    static constexpr float NONE = -1e30f;                  // the maximum of no score: every score is more than SLACK above it
+    static constexpr float NONE = -FLT_MAX;                // the maximum of no score: every other number is above it, SLACK lost in its rounding
     int g, t, qh;
     bool head;                                             // the lane's query column is a head
     int c0;                                                // head of column 2 t (of 2 t + 1: c0 + 1)
