@@ -101,7 +101,7 @@ struct AttendKv4 {
     static constexpr Kv4Block AT = Kv4Block(b, D);
     static constexpr float BASE = 9.f, SLACK = 4.f;        // 2^9, e^4 < 2^6
     static constexpr float REST = 2048.f;                  // what remainders are multiplied with
-    static constexpr float NONE = -FLT_MAX;                // the maximum of no score: every other number is above it, SLACK lost in its rounding
+    static constexpr float NONE = -FLT_MAX;                // the maximum of no score: every other number is more than SLACK above it
     int g, t, qh;
     bool head;                                             // the lane's query column is a head
     int c0;                                                // head of column 2 t (of 2 t + 1: c0 + 1)
@@ -319,7 +319,7 @@ struct AttendKv4 {
             }
         }
         float b0 = fmaxf(x[0], x[2]), b1 = fmaxf(x[1], x[3]);
-        if (__any_sync(0xffffffffu, b0 > m0 + SLACK || b1 > m1 + SLACK)) {
+        if (__any_sync(0xffffffffu, b0 - m0 > SLACK || b1 - m1 > SLACK)) {       // (the differences are exact where it matters)
 #pragma unroll
             for (int k = 4; k < 32; k <<= 1) {
                 b0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, b0, k));
