@@ -356,7 +356,9 @@ int eta_plan_pages(int32_t batch, int32_t block_size, int32_t t_cap, const int32
  * Arithmetic is fp32 with one rounding, to bf16, at the end (a head whose squares leave fp32's range is not normalised for what it
  * is: its sum counts as infinite, or as zero).  For the 4-bit cache keys are worked out in fp64 up to the quotient that
  * is rounded to a code, so that a key next to a border between two codes gets the same one whatever the order of the sums: the
- * same tokens give the same bytes.
+ * same tokens give the same bytes.  Most of them fp32 settles, with a bound on its error, if k_scale (for values v_scale) lies between
+ * 2^-60 and 2^60 and has at most 20 significant bits, that is, zeros in the last four of its fraction.  Other scales give their bytes in fp64 throughout,
+ * three times as long where rows are many: a calibrated scale is best rounded to 20 bits before anything is written with it.
  * q, k, v are [n_rows, heads, head_dim] of one type, unit stride along head_dim, the other strides multiples of 16 bytes; they may be
  * parts of one projection.  Pointers 16-byte aligned (slot_map and inv_freq 8, positions 4).  Of the cache descriptor n_q_heads, n_kv_heads,
  * head_dim, block_size, batch, t_cap and strides are used; unlike a step's, batch * n_kv_heads is not limited.  rotary_dim: a

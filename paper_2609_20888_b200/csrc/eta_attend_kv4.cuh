@@ -5,16 +5,18 @@
 //   - tokens are the rows of the first product (S = K q^T: sixteen tokens an MMA, query heads its eight columns), channels the rows of the second
 //     (O^T = V^T P), so that no row of an MMA is padding; the probabilities get from one's layout to the other's by a transpose of 8x8.
 //   - a code is converted by the hardware, two at a time, and scaled as an fp16 pair: code * scale is exact in fp16, so both products are
-//     exact and their sums fp32.  Queries are scaled by a power of two per head to use fp16's range (their bf16 values stay exact
-//     down to 2^-38 of the head's largest).
+//     exact and their sums fp32.  Queries are scaled by a power of two per head to use fp16's range: bf16's eight bits stay whole down to
+//     2^-30 of the head's largest channel, below that fewer of them, and nothing under 2^-38.
 //   - probabilities are fed as the nearest fp16 value and 2^11 times what that leaves, in fp16 (24 bits; remainders as they are would be subnormal from
 //     2^-12 of the largest weight on, and all that an output is made of is smaller where one token has the weight and next to no value).  Up
 //     to four heads, both are columns of one MMA: columns 4 to 7 repeat the heads of 0 to 3, whose lanes compute the same scores again and feed
 //     the remainder.  With eight heads the remainders' MMA starts from zero and its sums are added 2^-11 fold.
 //   - the running maximum follows the scores only when one is more than SLACK above it: exp(s - m) is then at most 2^6, and with
 //     the factor 2^BASE, which every part carries and the final division drops, inside fp16's range at both ends.
-// Bound by instructions: a conversion makes two numbers in two cycles of a scheduler, an MMA takes eight that add to them.  16 x 8K to 64K tokens
-// of 4 heads, all attended: 92 to 102 us a step (340 MB: 3.3 to 3.7 TB/s, half a copy's rate); 4 x 128K of 8 heads, a tenth of the blocks: 35 us.
+// Where every block is attended, what bounds it is the scheduler: a conversion makes two numbers in two cycles of one, an MMA takes eight that add to
+// them.  16 x 8K to 64K tokens, 4 KV heads of eight: 97 to 99 us a step (340 MB: 3.4 TB/s, half a copy's rate; 57 M warp instructions in 56 % of the
+// streaming kernel's issue slots, 22 M of them on the ALU pipe).  4 x 128K of 8 KV heads, a tenth of the blocks: 35 us, where
+// the streaming kernel's instructions fill 44 % of its issue slots and its warps wait for memory most; neither bytes nor instructions bound it.
 #pragma once
 
 #include <float.h>

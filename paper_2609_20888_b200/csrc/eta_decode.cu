@@ -1221,6 +1221,7 @@ static int decode_impl(const eta_cache_desc* desc, const eta_kv4_desc* kv4, cons
     // where most gain, it is not sharp.  It goes by the capacity, which the host knows; of a cache of 128K x 4 that holds little,
     // a step takes without and with both, 4K x 4 21.3, 21.4; 16K x 4 26.2, 27.1; 32K x 4 34.9, 32.7.  Lengths added up on the device
     // win the second and cost 0.5 to 2 us on the large steps, 8 where 183 MB are held in 419 (76.6 against 71.3 with both).
+    // The prefetch goes through the cache's tensor maps, which a 4-bit cache does not have.
     const int64_t unit_bytes = kv4 ? (int64_t)Kv4Block(b, D).bytes : (int64_t)4 * b * D, segs = (int64_t)L.rows * L.nseg;
     const bool large = (int64_t)L.rows * desc->nb_cap * unit_bytes > LARGE_CACHE_BYTES;
     const int64_t share = (PREFETCH_BYTES + segs * unit_bytes - 1) / (segs * unit_bytes);

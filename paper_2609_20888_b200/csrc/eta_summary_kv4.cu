@@ -9,7 +9,8 @@
 // without the shift that bf16 keys need, and is exactly 0 for identical keys.  A row's squared norm is summed group by group from
 // the codes' squares (quarters, up to 288 in either half of an fp16 pair: exact) times the scale's square.
 // Build and append run the same routine: appending a block gives the bytes rebuilding it would.
-// Bound by the adds and fused multiply-adds of the two moments: 4 x 128K tokens of 8 heads take 127 us (336 MB: 2.6 TB/s, 40 % of a copy's rate).
+// 4 x 128K tokens of 8 heads take 127 to 129 us (336 MB: 2.6 TB/s, 40 % of a copy's rate): 104 M warp instructions, 65 M of them the moments' on the FMA
+// pipe, fill 72 % of the issue slots.  The rest is the wait for the next eight rows, which are asked for only when the last eight are summed.
 #include "eta_kv4.cuh"
 
 namespace eta {

@@ -4,9 +4,10 @@
 //   y = x * w / sqrt(mean_c x_c^2 + eps);   (a, b) -> (a cos - b sin, a sin + b cos),  angle = position * inv_freq
 //
 // A warp takes a row's heads two (d = 128) or four (64) at a time, eight channels per lane, so that a head's sum is a few shuffles away;
-// everything is read once and written once.  Bound by the instructions per element where rows are many, by latency where they are few: 8229 rows
-// of 32 + 8 + 8 heads of 128, bf16, take 48.7 us (202 MB: 4.2 TB/s, 63 % of a copy's rate), 8 rows 4.4 us; 32768 rows into the 4-bit cache
-// and back 248 us (883 MB: 3.6 TB/s), 38 us of it the way back.
+// everything is read once and written once.  Few rows take latency: 8 rows 4.5 us.  Many are bound by no single thing: 8229 rows of 32 + 8 + 8 heads of
+// 128, bf16, take 49 us (202 MB: 4.1 TB/s, 62 % of a copy's rate), in which 24 M warp instructions fill 48 % of the issue slots, at sixteen
+// warps an SM that wait for their loads most.  32768 rows into the 4-bit cache and back take 248 us (883 MB: 3.6 TB/s): 210 for the write (137 M
+// instructions, 59 % of the slots), 38 for the way back (31 M, 77 %: the index arithmetic, 64-bit divisions among it, is what a group's 41 bytes cost).
 #include <math.h>
 #include <string.h>
 
@@ -33,7 +34,9 @@ struct TokensArgs {
     FastDiv div_page, div_ctas;
     int ctas_row;          // CTAs of a row; 0: two rows to a CTA
     float k_scale, v_scale;
-    int fast;              // bit 0, 1: the keys', the values' scale leaves fp32 its range, and its product with a group's is exact (20 bits)
+    // bit 0, 1: the keys', the values' scale leaves fp32 its range, and its product with a group's is exact (20 bits).  Of another scale everything is
+    // worked out in fp64: 32768 rows take 682 us instead of 217 (bf16; 755 instead of 295 in fp32).
+    int fast;
     float eps;
 };
 
@@ -642,8 +645,8 @@ static int append_tokens(const eta_cache_desc* desc, const eta_kv4_desc* kv4, co
     a.rotary = tok->rotary_dim; a.interleaved = (tok->flags & ETA_TOKENS_INTERLEAVED) != 0;
     a.eps = tok->eps;
     a.div_page = FastDiv(a.per_page);
-    // Two warps to a row, one for its queries, one for its keys and values, where there are rows enough to fill the GPU; as many as there
-    // are items where there are not.
+    // Two warps to a row, one for its queries, one for its keys and values, where there are rows enough to fill the GPU (148 SMs; a partition of it only
+    // gets more CTAs than it needs); as many as there are items where there are not.
     const int per_warp = 32 / (desc->head_dim / 8);
     const int q_items = (a.Hq + per_warp - 1) / per_warp, kv_items = 2 * ((a.Hkv + per_warp - 1) / per_warp);
     const int want = (148 * 16 / 4 + a.rows - 1) / a.rows, most = (q_items + kv_items + 3) / 4;
