@@ -187,7 +187,8 @@ struct AttendKv4 {
         }
     }
     // The warp's accumulators are folded into sm [heads][O_STRIDE] every FOLD stages and at the end of a piece: an MMA cuts its sum off where
-    // fp32 would round it, and after two hundred of them in a row (64K tokens, dense) an output was off by 1.9e-6 of itself, by 3.5e-7 this way.
+    // fp32 would round it, and after two hundred of them in a row (64K tokens, dense) an output was off by
+    // 1.9e-6 of itself, by 7e-7 with the sums folded; with remainders fed REST fold as well it is 3.5e-7.
     // Channel (D / 8) g + 2 mt + c is at 16 mt + 2 g + c: the sixteen lanes of a phase meet every bank once.
     static constexpr int O_STRIDE = D + 4, FOLD = 10;
     // where four consecutive channels 4 k .. are: two pairs, 16 floats apart
