@@ -446,6 +446,31 @@ int eta_decode_kv4(const eta_cache_desc* desc, const eta_kv4_desc* kv4, const et
                    const float* head_const, float* out, uint8_t* sel_mask, int32_t* stats, uint32_t* status_dev, void* workspace,
                    size_t workspace_bytes, void* stream);
 
+/*
+ * Attention of a step's new tokens: prompts, chunks of prompts behind what is cached, single tokens, packed as eta_plan_pages packs
+ * them.  The cache holds the new tokens already (eta_append_tokens before this call).  Sequence i has the rows row_start[i] ..
+ * row_start[i + 1] - 1 of q, of which the first granted[i] count (granted nullable: all of them); those are its newest tokens, the last at
+ * position seq_lens[i] - 1.  For every such row r, at position p, and every query head h:
+ *   out[r, h] = sum_{t <= p} w_t v_t / sum_{t <= p} w_t,  w = exp(S~), S = s <q_h, k_t>,
+ *   S~ = S sigmoid(beta (S - tau_eff)) (Eq. mult_attn over all tokens, no block is screened out), tau_eff = (tau[r, h] or head_const[h]) - a;
+ *   with ETA_FLAG_UNGATE_LAST the row's own token t = p keeps its raw score; with ETA_FLAG_DENSE S~ = S (softmax).
+ * q bf16 [n_rows, n_q_heads, head_dim]; out bf16, the same shape: what the output projection takes; tau fp32 [n_rows, n_q_heads].
+ * Exactly one of tau / head_const unless ETA_FLAG_DENSE, which looks at neither.  z, lwb and rescue_window are not looked at.
+ * Rows that do not count, and those behind the last sequence, are left as they are.  A row whose position is negative (more new tokens
+ * than seq_lens) sees nothing: zeros, and ETA_DEV_EMPTY_ROW.  A length past t_cap is clamped (ETA_DEV_LEN_CLAMPED).
+ * Cache: contiguous, or with `pages` not NULL paged, as for eta_decode; table entries behind the last token are not read.  What the cache
+ * holds behind a row's position, NaN and infinities included, does not reach the row.
+ * bf16 operands, fp32 scores and sums; weights enter the second product as bf16 (2^-8 of each, as much as rounding the output).
+ * Deterministic for a given device.  batch <= 1024, n_kv_heads <= 1024, n_rows <= 2^30; nb_cap is not looked at.
+ * Two kernels, launched with programmatic dependent launch: the first waits for everything before it in the stream before it reads or
+ * writes, the second releases its successors as it ends.  workspace: eta_prefill_workspace_bytes() bytes, 256-byte aligned, no
+ * initialisation needed; two calls that can overlap need one each.
+ */
+int eta_prefill_workspace_bytes(const eta_cache_desc* desc, size_t* out_bytes);
+int eta_prefill(const eta_cache_desc* desc, const eta_page_table* pages, const eta_params* params, int32_t n_rows, const void* q,
+                const int32_t* row_start, const int32_t* seq_lens, const int32_t* granted, const void* K, const void* V, const float* tau,
+                const float* head_const, void* out, uint32_t* status_dev, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Size of the built-in scratch of eta_decode_static, in bytes. */
 size_t eta_static_scratch_bytes(void);
 

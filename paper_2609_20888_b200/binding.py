@@ -32,7 +32,8 @@ EXPORTS = ("eta_workspace_bytes", "eta_build_block_summaries", "eta_append_summa
            "eta_score_dual", "eta_calibration_workspace_bytes", "eta_calibrate_head_const", "eta_decode", "eta_decode_static", "eta_static_scratch_bytes", "eta_decode_kernel_count", "eta_decode_launches", "eta_profile_enable", "eta_profile_read",
            "eta_profile_kernel_name", "eta_set_pdl", "eta_strerror", "eta_last_cuda_error", "eta_plan_pages",
            "eta_append_tokens", "eta_append_tokens_kv4", "eta_kv4_block_bytes", "eta_unpack_kv4",
-           "eta_build_block_summaries_kv4", "eta_append_summary_kv4", "eta_decode_kv4", "eta_kv4_workspace_bytes")
+           "eta_build_block_summaries_kv4", "eta_append_summary_kv4", "eta_decode_kv4", "eta_kv4_workspace_bytes",
+           "eta_prefill", "eta_prefill_workspace_bytes")
 
 
 class CacheDesc(ctypes.Structure):
@@ -71,7 +72,7 @@ _lib = None
 _native = None          # the compiled marshalling module, or what stands for it where it is missing
 _STEP_CALLS = ("eta_append_summary", "eta_append_summary_paged", "eta_predict_threshold", "eta_decode", "eta_decode_paged",
                "eta_decode_static", "eta_plan_pages", "eta_append_tokens", "eta_append_tokens_kv4", "eta_unpack_kv4",
-               "eta_build_block_summaries_kv4", "eta_append_summary_kv4", "eta_decode_kv4")
+               "eta_build_block_summaries_kv4", "eta_append_summary_kv4", "eta_decode_kv4", "eta_prefill")
 
 
 class _Missing:
@@ -136,6 +137,8 @@ def load(path: str | None = None) -> ctypes.CDLL:
         lib.eta_kv4_workspace_bytes.argtypes = [D, ctypes.POINTER(ctypes.c_size_t)]
         lib.eta_kv4_block_bytes.argtypes = [i32, i32]
         lib.eta_kv4_block_bytes.restype = ctypes.c_size_t
+        lib.eta_prefill_workspace_bytes.argtypes = [D, ctypes.POINTER(ctypes.c_size_t)]
+        lib.eta_prefill.argtypes = [D, PT, P, i32, vp, i32p, i32p, i32p, vp, vp, f32p, f32p, vp, vp, vp, ctypes.c_size_t, vp]
         lib.eta_decode_static.argtypes = [D, P, vp, vp, vp, i32p, vp, f32p, f32p, f32p, f32p, vp, i32p, vp, vp]
         lib.eta_static_scratch_bytes.restype = ctypes.c_size_t
         lib.eta_decode_kernel_count.restype = ctypes.c_int
@@ -461,6 +464,24 @@ def eta_decode_kv4(desc: CacheDesc, kv4: Kv4Desc, params: DecodeParams, q, pool,
                             sel_mask, stats, status, workspace)
     if rc:
         _check(rc, "eta_decode_kv4")
+
+
+def eta_prefill_workspace_bytes(desc: CacheDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().eta_prefill_workspace_bytes(ctypes.byref(desc), ctypes.byref(n)), "eta_prefill_workspace_bytes")
+    return n.value
+
+
+def eta_prefill(desc: CacheDesc, params: DecodeParams, q, K, V, row_start, seq_lens, out, workspace, tau=None, head_const=None,
+                granted=None, status=None, pages: PageTable | None = None) -> None:
+    """Attention of a step's new tokens over the cache that holds them (see include/eta.h): q and out bf16 [rows, n_q_heads, head_dim],
+    packed by row_start (int32 [batch + 1]); tau fp32 [rows, n_q_heads] or head_const fp32 [n_q_heads], neither with ETA_FLAG_DENSE;
+    paged with a page table."""
+    lib = _lib or load()
+    rc = _native.prefill(lib.addresses["eta_prefill"], desc, pages, params, q, row_start, seq_lens, granted, K, V, tau, head_const, out,
+                         status, workspace)
+    if rc:
+        _check(rc, "eta_prefill")
 
 
 def eta_static_scratch_bytes() -> int:

@@ -1,0 +1,1047 @@
+// Attention of a step's new tokens over the cache that holds them already: prompts, chunks of prompts and single tokens, packed, each
+// sequence behind its own context.
+//
+//   out[r, h] = sum_{t <= p(r)} w_t v_t / sum_{t <= p(r)} w_t,   w = exp(S~),   S = s <q_h, k_t>
+//   S~ = S (softmax), or S sigmoid(beta (S - tau_eff)) (Eq. mult_attn), raw for t = p(r) with ETA_FLAG_UNGATE_LAST
+//
+// A work item is 256 query rows of one (sequence, KV head): 256 / G tokens with the G heads of the group packed behind each other, so
+// that a tile of K and V serves them all.  The rows are two halves of 128 with a softmax warpgroup each, a row per thread, and take
+// turns on the tensor core: while one half's scores are turned into weights the other half's products run.
+//   tensor memory   S of each half (128 fp32 columns; its weights, bf16, overwrite the first 64), O of each half (head_dim columns)
+//   shared memory   the queries (two halves), a ring of K and V tiles of 128 tokens (128-byte swizzle, 64-column halves)
+//   warps           0-3, 4-7 softmax and epilogue; 8 copies (TMA, a copy per page and 64 columns); 9 issues the MMAs; 10, 11 clean tiles
+// S = Q K^T has both operands in shared memory; O += P V takes P from tensor memory and V as it lies (token-major).
+// The running maximum moves only when it would by more than 2^8: weights are then at most 2^8 and O is rescaled a few times a row
+// instead of once a tile.  Weights are rounded to bf16 (relative 2^-8, as much as the output's own rounding); their sum, O and
+// the maximum are fp32.
+//
+// V rows that some row of the item must not see (behind its position, or behind the sequence) would reach it as 0 * V, which is not 0 for
+// infinities and NaN.  In the one to three tiles of an item where that can be, two warps take them out of the shared-memory tile: rows
+// behind the last visible token whole, other non-finite values one by one; the epilogue adds the latter to the rows that see them.
+//
+// How items are shared out is decided on the device from the lengths, by every CTA for itself: whole items in rounds of one per CTA
+// where there are many, or equal shares of all tiles with a few items split along t, whose parts a second kernel joins.
+#include <cuda.h>
+
+#include <algorithm>
+#include <type_traits>
+#include <vector>
+
+#include "eta_common.cuh"
+
+namespace eta {
+
+constexpr int PF_TILE = 128;               // tokens of a K or V tile
+constexpr int PF_HALF = 128;               // query rows of a half item
+constexpr int PF_ROWS = 2 * PF_HALF;
+constexpr int PF_THREADS = 384;
+constexpr int PF_MAX_CTAS = 160;           // sizes the scratch of split items
+constexpr int PF_MAX_BATCH = 1024;         // sequences whose prefix sums a CTA keeps in shared memory
+constexpr int PF_ITEM_COST = 2;            // what an item costs beside its tiles, in tiles: queries, output, a pipeline that runs dry
+constexpr int PF_SPLIT_COST = 4;           // what joining split items costs, in tiles
+constexpr int64_t PF_L2_BYTES = 64ll << 20;     // K and V of the heads that are worked on side by side
+// registers: 384 threads start with 168; 256 of them take 208, the others 88 (together what the block was launched with)
+constexpr int PF_REGS = 168, PF_REGS_SOFTMAX = 208, PF_REGS_OTHER = 88;
+static_assert(256 * PF_REGS_SOFTMAX + 128 * PF_REGS_OTHER <= PF_REGS * PF_THREADS, "more registers than the block has");
+constexpr float PF_SLACK = 8.f;            // log2 of how far a weight may exceed 1
+
+struct PrefillArgs {
+    const int32_t *row_start, *seq_lens, *granted, *block_table;
+    const float *tau, *head_const;
+    const __nv_bfloat16* V;                // for values that were taken out of a tile
+    int64_t v_sb, v_sh, v_st;
+    __nv_bfloat16* out;
+    float* part_o;                         // [2 PF_MAX_CTAS][PF_ROWS][D]
+    float2* part_ml;                       // [2 PF_MAX_CTAS][PF_ROWS]
+    int4* desc;                            // [PF_MAX_CTAS] the split item that starts in a CTA's share: parts, first row, tokens, KV head
+    uint32_t* status;
+    float a, beta, scale;
+    int batch, Hq, Hkv, g_shift, b_shift, t_cap, n_rows, table_stride, ungate;
+};
+
+// ------------------------------------------------------------------------------------------------ work items
+
+#define PF_BOTH __host__ __device__ __forceinline__
+
+// Tiles of K that query tile t of a sequence needs, and what all before it need, for n new tokens behind ctx; m tokens per query tile.
+struct PfTiles {
+    int nq, m, n, base;
+    PF_BOTH PfTiles(int len, int n_, int m_) {
+        n = n_; m = m_;
+        nq = (n + m - 1) / m;
+        base = max(len - n, 0);
+    }
+    PF_BOTH int tiles(int t) const { return (int)(((int64_t)base + min((int64_t)(t + 1) * m, (int64_t)n) + PF_TILE - 1) / PF_TILE); }
+    // sum over the first t query tiles, t <= nq
+    PF_BOTH int64_t before(int t) const {
+        int64_t last = 0;
+        if (t == nq && t > 0) { last = tiles(--t); }
+        const int64_t b0 = (int64_t)base + m + PF_TILE - 1;
+        int64_t sum;
+        if (m >= PF_TILE) {
+            sum = t * (b0 / PF_TILE) + (int64_t)(m / PF_TILE) * t * (t - 1) / 2;
+        } else {
+            const int p = PF_TILE / m, U = t / p, R = t % p;
+            sum = (int64_t)p * U * (U - 1) / 2 + (int64_t)R * U;
+            for (int v = 0; v < p; ++v) sum += (int64_t)(U + (v < R)) * ((b0 + v * m) / PF_TILE);
+        }
+        return sum + last;
+    }
+    PF_BOTH int64_t cost_before(int t) const { return before(t) + (int64_t)t * PF_ITEM_COST; }
+};
+
+struct PfTables {                          // in shared memory
+    int64_t cost[PF_MAX_BATCH + 1];        // cost of all items of the sequences before
+    int32_t items[PF_MAX_BATCH + 1];
+    int32_t row0[PF_MAX_BATCH], n[PF_MAX_BATCH], len[PF_MAX_BATCH];
+    int32_t longest;                       // tiles of the longest item
+};
+
+struct PfItem {
+    int seq, hk, row0, n_tok;              // first row in the packed rows, tokens that count
+    int p0;                                // position of the first token
+    int kv_end;                            // tokens [0, kv_end) are seen by some row
+    int k0, n[2];                          // first tile, tiles of each half
+    int clean0;                            // first tile in which not every row sees every token
+    int slot;                              // of a part of a split item; -1: whole
+    int pieces;                            // the parts of the item that starts here and goes on; 0: none
+};
+
+// Walks the items of a CTA.  Every warp of it runs the same walk.
+struct PfWalk {
+    const PfTables& tab;
+    int batch, Hkv, m, cta, ctas;
+    int64_t head_bytes;                    // bytes of K and V per token and KV head
+    bool whole;                            // items in rounds, or shares
+    int64_t C, x, x1;                      // shares: all cost, the CTA's range
+    int P;
+    int round;
+    int total;
+
+    PF_BOTH PfWalk(const PfTables& t, int batch_, int Hkv_, int g_shift, int D, int cta_, int ctas_) : tab(t) {
+        batch = batch_; Hkv = Hkv_; m = PF_ROWS >> g_shift;
+        cta = cta_; ctas = ctas_;
+        head_bytes = 4 * D;
+        C = tab.cost[batch];
+        total = tab.items[batch];
+        round = 0;
+        const int64_t longest = tab.longest + PF_ITEM_COST, mean = C / ctas;
+        // whole items: as long as the longest, or as the mean with half an item left over at the end
+        const int64_t est_whole = total <= ctas ? longest : max(longest, mean + longest / 2);
+        whole = est_whole <= mean + PF_ITEM_COST + PF_SPLIT_COST;
+        P = (int)min((int64_t)ctas, max((int64_t)1, C / (PF_ITEM_COST + 4)));
+        x = x1 = C;
+        if (!whole && cta < P) { x = C * cta / P; x1 = C * (cta + 1) / P; }
+    }
+    template <typename T>
+    PF_BOTH int last_not_above(const T* v, T key) const {
+        int lo = 0, hi = batch;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (v[mid] <= key) lo = mid; else hi = mid;
+        }
+        return lo;
+    }
+    PF_BOTH void fill(PfItem& it, int seq, int hk, int qt) const {
+        const int n = tab.n[seq], len = tab.len[seq], tok = qt * m;
+        it.seq = seq; it.hk = hk;
+        it.row0 = tab.row0[seq] + tok;
+        it.n_tok = min(m, n - tok);
+        it.p0 = len - n + tok;
+        it.kv_end = max(0, it.p0 + it.n_tok);
+        it.clean0 = it.p0 < 0 ? 0 : (it.p0 + 1) / PF_TILE;
+    }
+    // tiles of each half within [k0, k1)
+    PF_BOTH void clip(PfItem& it, int k0, int k1) const {
+        it.k0 = k0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int tok = min(it.n_tok, (h + 1) * (m / 2));
+            const int end = tok > h * (m / 2) ? max(0, it.p0 + tok) : 0;
+            it.n[h] = max(0, min(k1, end > 0 ? (end - 1) / PF_TILE + 1 : 0) - k0);
+        }
+    }
+    PF_BOTH bool next(PfItem& it) {
+        if (whole) {
+            // rounds run back and forth, so that whoever got the longest item of one gets the shortest of the next
+            while ((int64_t)round * ctas < total) {
+                const int idx = round * ctas + ((round & 1) ? ctas - 1 - cta : cta);
+                ++round;
+                if (idx >= total) continue;
+                const int seq = last_not_above(tab.items, idx);
+                const PfTiles ti(tab.len[seq], tab.n[seq], m);
+                // heads in groups whose K and V the L2 holds, within a group the longest query tiles first
+                const int group = (int)max((int64_t)1, min((int64_t)Hkv, PF_L2_BYTES / (head_bytes * max(1, tab.len[seq]))));
+                int l = idx - tab.items[seq];
+                const int g = l / (ti.nq * group);
+                l -= g * ti.nq * group;
+                const int hs = min(group, Hkv - g * group);
+                fill(it, seq, g * group + l % hs, ti.nq - 1 - l / hs);
+                clip(it, 0, 1 << 30);
+                it.slot = -1; it.pieces = 0;
+                return true;
+            }
+            return false;
+        }
+        while (x < x1) {
+            const int seq = last_not_above(tab.cost, x);
+            const PfTiles ti(tab.len[seq], tab.n[seq], m);
+            const int64_t F = ti.cost_before(ti.nq), in_seq = x - tab.cost[seq];
+            const int hk = (int)(in_seq / F);
+            const int64_t y = in_seq - hk * F, z = F - y;
+            // the longest query tile first: tile qt lies at [F - cost_before(qt + 1), F - cost_before(qt))
+            int lo = 0, hi = ti.nq;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (ti.cost_before(mid) < z) lo = mid; else hi = mid;
+            }
+            const int qt = lo, tiles = ti.tiles(qt);
+            const int64_t start = tab.cost[seq] + hk * F + F - ti.cost_before(qt + 1), end = start + PF_ITEM_COST + tiles;
+            const int k0 = (int)max((int64_t)0, x - start - PF_ITEM_COST), k1 = (int)max((int64_t)0, min(x1, end) - start - PF_ITEM_COST);
+            x = end;
+            if (k1 <= k0) continue;            // (a share that ends in the fixed part of an item)
+            fill(it, seq, hk, qt);
+            clip(it, k0, k1);
+            it.slot = -1; it.pieces = 0;
+            if (k0 > 0) {
+                it.slot = 2 * cta;
+            } else if (k1 < tiles) {
+                it.slot = 2 * cta + 1;
+                it.pieces = (int)((end * P + C - 1) / C) - cta;          // the share that holds the item's last tile
+            }
+            return true;
+        }
+        return false;
+    }
+};
+
+// ------------------------------------------------------------------------------------------------ tensor core
+
+// Operand in shared memory as the copies leave it: rows of 128 bytes, 128-byte swizzle, eight rows (1024 bytes) to a group.
+// Queries, keys: the contraction runs along a row.  Values: it runs along the rows, and the next 64 columns are a half tile further.
+__device__ __forceinline__ uint64_t pf_operand(uint32_t addr, uint32_t next64) {
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(next64 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// fp32 accumulator, bf16 operands, 128 rows
+__host__ __device__ constexpr uint32_t pf_idesc(int n, bool b_rows) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | (b_rows ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(PF_HALF >> 4) << 24);
+}
+__device__ __forceinline__ void pf_mma_ss(uint32_t acc, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(acc), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
+}
+__device__ __forceinline__ void pf_mma_ts(uint32_t acc, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(acc), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
+}
+// arrives on the barrier when every MMA issued so far has completed
+__device__ __forceinline__ void pf_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void pf_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void pf_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+// 32 columns of this thread's lane; complete after pf_wait_ld
+__device__ __forceinline__ void pf_ld32(uint32_t addr, float* v) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+          "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
+          "=r"(r[30]), "=r"(r[31]) : "r"(addr));
+}
+__device__ __forceinline__ void pf_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void pf_st32(uint32_t addr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+          "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+          "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void pf_st16(uint32_t addr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void pf_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ float pf_ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float pf_rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pf_pack(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// (a0, a1) * (b, b) + (c, c)
+__device__ __forceinline__ void pf_fma2(float& d0, float& d1, float a0, float a1, float b, float c) {
+    asm("{\n\t.reg .b64 ra, rb, rc;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %4};\n\tmov.b64 rc, {%5, %5};\n\t"
+        "fma.rn.f32x2 rc, ra, rb, rc;\n\tmov.b64 {%0, %1}, rc;\n\t}"
+        : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b), "f"(c));
+}
+
+__device__ __forceinline__ bool pf_elect() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
+// A bounded wait that others' failures end too
+__device__ __forceinline__ bool pf_wait(uint64_t* bar, uint32_t parity, const volatile int* dead) {
+    for (uint32_t it = 0; it < WAIT_LIMIT; ++it) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((it & 255) == 255 && *dead) return false;
+    }
+    return false;
+}
+
+// ------------------------------------------------------------------------------------------------ kernel
+
+template <int D>
+struct PfSmem {
+    static constexpr int HALVES = D / 64;
+    static constexpr int Q_BYTES = PF_HALF * D * 2;
+    static constexpr int STAGE = PF_TILE * D * 2;
+    static constexpr int NSTAGE = 128 * 1024 / STAGE;
+    static constexpr int RING = 2 * Q_BYTES;
+    static constexpr int TABLES = RING + NSTAGE * STAGE;
+    static constexpr int BARS = TABLES + (int)((sizeof(PfTables) + 15) / 16 * 16);
+    static constexpr int N_BARS = 3 * NSTAGE + 2 * 5 + 1;
+    static constexpr int BYTES = 1024 + BARS + 8 * N_BARS;
+    static_assert(BYTES <= 227 * 1024, "too much shared memory");
+};
+
+template <int D, bool GATED>
+__global__ void __launch_bounds__(PF_THREADS, 1)
+prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+               const __grid_constant__ PrefillArgs a) {
+    using L = PfSmem<D>;
+    constexpr int NSTAGE = L::NSTAGE, HALVES = L::HALVES;
+    extern __shared__ unsigned char pf_raw[];
+    unsigned char* const smem = pf_raw + ((1024u - (smem_u32(pf_raw) & 1023u)) & 1023u);
+    PfTables& tab = *reinterpret_cast<PfTables*>(smem + L::TABLES);
+    uint64_t* const full = reinterpret_cast<uint64_t*>(smem + L::BARS);
+    uint64_t *const empty = full + NSTAGE, *const cleaned = empty + NSTAGE;
+    uint64_t *const q_full = cleaned + NSTAGE, *const q_empty = q_full + 2, *const s_full = q_empty + 2, *const p_full = s_full + 2,
+             *const o_full = p_full + 2, *const drained = o_full + 2;
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_dead;
+    __shared__ int s_poison[16];               // item (counted from 1) of whose tiles values were taken out
+    __shared__ int64_t s_scan[PF_THREADS / 32][2];
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int G = 1 << a.g_shift, HT = PF_HALF >> a.g_shift;       // heads of a group, tokens of a half
+
+    if (tid == 0) {
+        // (tiles of K and V take turns, so the odd stages hold V: the cleaning warps let go of those too)
+        for (int k = 0; k < NSTAGE; ++k) { mbar_init(&full[k], 1); mbar_init(&empty[k], k & 1 ? 3 : 1); mbar_init(&cleaned[k], 2); }
+        mbar_init(drained, 1);
+        for (int k = 0; k < 2; ++k) {
+            mbar_init(&q_full[k], 1); mbar_init(&q_empty[k], 1); mbar_init(&s_full[k], 1);
+            mbar_init(&p_full[k], 4); mbar_init(&o_full[k], 1);
+        }
+        fence_barrier_init();
+        prefetch_tmap(&tmQ); prefetch_tmap(&tmK); prefetch_tmap(&tmV);
+        s_dead = 0;
+        tab.longest = 0;
+    }
+    if (tid < 16) s_poison[tid] = 0;
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    pdl_wait();
+    __syncthreads();
+
+    // ---- sequences: rows, lengths, and prefix sums of items and cost
+    {
+        const int per = (a.batch + PF_THREADS - 1) / PF_THREADS, first = min(a.batch, tid * per), end = min(a.batch, first + per);
+        int64_t cost = 0;
+        int items = 0, longest = 0;
+        uint32_t flags = 0;
+        for (int i = first; i < end; ++i) {
+            const int r0 = __ldcg(a.row_start + i), r1 = __ldcg(a.row_start + i + 1);
+            int len = __ldcg(a.seq_lens + i), n = r1 > r0 ? r1 - r0 : 0;
+            if (a.granted) n = min(n, max(0, __ldcg(a.granted + i)));
+            if (r0 < 0 || r0 > a.n_rows) n = 0;
+            n = min(n, a.n_rows - min(max(r0, 0), a.n_rows));
+            if (len > a.t_cap) { len = a.t_cap; flags |= ETA_DEV_LEN_CLAMPED; }
+            len = max(len, 0);
+            if (n > len) flags |= ETA_DEV_EMPTY_ROW;
+            tab.row0[i] = r0; tab.n[i] = n; tab.len[i] = len;
+            tab.items[i] = items; tab.cost[i] = cost;
+            const PfTiles ti(len, n, PF_ROWS >> a.g_shift);
+            items += ti.nq * a.Hkv;
+            cost += a.Hkv * ti.cost_before(ti.nq);
+            if (n) longest = max(longest, ti.tiles(ti.nq - 1));
+        }
+        int64_t sc = cost, si = items;
+#pragma unroll
+        for (int s = 1; s < 32; s <<= 1) {
+            const int64_t oc = __shfl_up_sync(0xffffffffu, sc, s), oi = __shfl_up_sync(0xffffffffu, si, s);
+            if (lane >= s) { sc += oc; si += oi; }
+        }
+        if (lane == 31) { s_scan[warp][0] = sc; s_scan[warp][1] = si; }
+        longest = __reduce_max_sync(0xffffffffu, longest);
+        if (lane == 0 && longest) atomicMax(&tab.longest, longest);
+        flags = __reduce_or_sync(0xffffffffu, flags);
+        if (lane == 0 && flags && blockIdx.x == 0 && a.status) atomicOr(a.status, flags);
+        __syncthreads();
+        sc -= cost; si -= items;
+        for (int w = 0; w < warp; ++w) { sc += s_scan[w][0]; si += s_scan[w][1]; }
+        for (int i = first; i < end; ++i) { tab.cost[i] += sc; tab.items[i] += (int)si; }
+        if (end == a.batch && first < end) { tab.cost[a.batch] = sc + cost; tab.items[a.batch] = (int)si + items; }
+    }
+    pf_fence_before();
+    __syncthreads();
+    pf_fence_after();
+    const uint32_t tmem = s_tmem;
+    PfWalk walk(tab, a.batch, a.Hkv, a.g_shift, D, blockIdx.x, gridDim.x);
+    PfItem it;
+    bool ok = true;
+
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PF_REGS_OTHER));
+        if (warp == 8) {
+            // -------------------------------------------------------------- copies
+            uint32_t fill = 0, q_loads[2] = {0, 0};
+            int4 split = make_int4(0, 0, 0, 0);
+            while (ok && walk.next(it)) {
+                if (it.pieces > 1) split = make_int4(it.pieces, it.row0, it.n_tok, it.hk);
+                const int n = max(it.n[0], it.n[1]);
+                auto load_q = [&](int h) {
+                    if (!ok || !it.n[h]) return;
+                    if (q_loads[h] && !pf_wait(&q_empty[h], (q_loads[h] - 1) & 1, &s_dead)) { ok = false; return; }
+                    ++q_loads[h];
+                    if (lane == 0) {
+                        mbar_arrive_expect_tx(&q_full[h], L::Q_BYTES);
+#pragma unroll
+                        for (int c = 0; c < HALVES; ++c)
+                            asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                                         ::"r"(smem_u32(smem + h * L::Q_BYTES + c * (PF_HALF * 128))), "l"(&tmQ), "r"(smem_u32(&q_full[h])),
+                                           "r"(64 * c), "r"(it.hk * G), "r"(it.row0 + h * HT) : "memory");
+                    }
+                    __syncwarp();
+                };
+                // a tile: a copy per 64 columns, and in a paged cache per page
+                const int per_tile = a.block_table ? PF_TILE >> a.b_shift : 1;
+                auto load_tile = [&](const CUtensorMap* tm, int j, int page) {
+                    if (!ok) return;
+                    const int stage = fill % NSTAGE;
+                    if (!pf_wait(&empty[stage], ((fill / NSTAGE) & 1) ^ 1, &s_dead)) { ok = false; return; }
+                    ++fill;
+                    int copies = HALVES, bytes = L::STAGE;
+                    if (a.block_table) {
+                        const int pages = (min(PF_TILE, it.kv_end - j * PF_TILE) + (1 << a.b_shift) - 1) >> a.b_shift;
+                        copies = HALVES * pages;
+                        bytes = (pages << a.b_shift) * D * 2;
+                    }
+                    if (lane == 0) mbar_arrive_expect_tx(&full[stage], bytes);
+                    __syncwarp();
+                    const int sub = lane / HALVES, c = lane % HALVES;
+                    if (lane < copies)
+                        tma_load_4d(smem + L::RING + stage * L::STAGE + c * (PF_TILE * 128) + ((sub << a.b_shift) * 128 & (PF_TILE * 128 - 1)), tm, 64 * c,
+                                    a.block_table ? 0 : j * PF_TILE, it.hk, a.block_table ? page : it.seq, &full[stage]);
+                    __syncwarp();
+                };
+                auto page_of = [&](int j) {            // the page of this lane's copy
+                    const int sub = lane / HALVES, blk = j * per_tile + sub;
+                    return a.block_table && sub < per_tile && (blk << a.b_shift) < it.kv_end
+                               ? __ldcg(a.block_table + (int64_t)it.seq * a.table_stride + blk) : 0;
+                };
+                int page = n ? page_of(it.k0) : 0;
+                load_q(0);
+                for (int j = 0; j < n && ok; ++j) {
+                    const int next = j + 1 < n ? page_of(it.k0 + j + 1) : 0;
+                    load_tile(&tmK, it.k0 + j, page);
+                    if (j == 0) load_q(1);
+                    load_tile(&tmV, it.k0 + j, page);
+                    page = next;
+                }
+            }
+            if (lane == 0) a.desc[blockIdx.x] = split;
+            if (!ok) {
+                // give up: report, and let the copies that are on their way land before the shared memory is given back
+                if (lane == 0) {
+                    s_dead = 1;
+                    if (a.status) atomicOr(a.status, ETA_DEV_TIMEOUT);
+                }
+                for (uint32_t f = fill > NSTAGE ? fill - NSTAGE : 0; f < fill; ++f) mbar_wait(&full[f % NSTAGE], (f / NSTAGE) & 1);
+                for (int h = 0; h < 2; ++h)
+                    if (q_loads[h]) mbar_wait(&q_full[h], (q_loads[h] - 1) & 1);
+            }
+            pdl_trigger();
+        } else if (warp == 9) {
+            // -------------------------------------------------------------- MMAs; the whole warp walks along, one lane issues
+            uint32_t fill = 0, n_clean = 0, q_n[2] = {0, 0}, p_n[2] = {0, 0};
+            const uint64_t q_op[2] = {pf_operand(smem_u32(smem), 16), pf_operand(smem_u32(smem + L::Q_BYTES), 16)};
+            const uint64_t ring_k = pf_operand(smem_u32(smem + L::RING), 16), ring_v = pf_operand(smem_u32(smem + L::RING), PF_TILE * 128);
+            auto wait = [&](uint64_t* bar, uint32_t parity) {
+                ok = ok && pf_wait(bar, parity, &s_dead);
+                ok = __all_sync(0xffffffffu, ok);
+                pf_fence_after();
+                return ok;
+            };
+            // S = Q K^T of half h
+            auto scores = [&](int h, int stage, bool last) {
+                const uint64_t k_op = ring_k + (uint32_t)(stage * (L::STAGE >> 4));
+                if (pf_elect()) {
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)       // 16 columns: 32 bytes along the swizzled row of a 64-column half
+                        pf_mma_ss(tmem + h * PF_TILE, q_op[h] + (k / 4) * (PF_HALF * 128 >> 4) + (k % 4) * 2,
+                                  k_op + (k / 4) * (PF_TILE * 128 >> 4) + (k % 4) * 2, pf_idesc(PF_TILE, false), k > 0);
+                    pf_commit(&s_full[h]);
+                    if (last) pf_commit(&q_empty[h]);
+                }
+                __syncwarp();
+            };
+            // O += P V of half h
+            auto values = [&](int h, int stage, bool first, bool last) {
+                const uint64_t v_op = ring_v + (uint32_t)(stage * (L::STAGE >> 4));
+                if (pf_elect()) {
+#pragma unroll
+                    for (int k = 0; k < PF_TILE / 16; ++k)     // 16 tokens: two groups of eight rows
+                        pf_mma_ts(tmem + 2 * PF_TILE + h * D, tmem + h * PF_TILE + 8 * k, v_op + k * (16 * 128 >> 4), pf_idesc(D, true),
+                                  !first || k > 0);
+                    if (last) pf_commit(&o_full[h]);
+                }
+                __syncwarp();
+            };
+            auto release = [&](int stage) {
+                if (pf_elect()) pf_commit(&empty[stage]);
+                __syncwarp();
+            };
+            while (ok && walk.next(it)) {
+                const int n = max(it.n[0], it.n[1]);
+                if (!n) continue;
+                for (int h = 0; h < 2 && ok; ++h) {
+                    if (!it.n[h] || !wait(&q_full[h], q_n[h]++ & 1) || !wait(&full[fill % NSTAGE], (fill / NSTAGE) & 1)) continue;
+                    scores(h, fill % NSTAGE, it.n[h] == 1);
+                }
+                if (!ok) break;
+                release(fill % NSTAGE);
+                ++fill;
+                for (int j = 0; j < n; ++j) {
+                    const int vs = fill % NSTAGE;
+                    if (!wait(&full[vs], (fill / NSTAGE) & 1)) break;
+                    if (it.k0 + j >= it.clean0) {
+                        if (!wait(&cleaned[n_clean % NSTAGE], (n_clean / NSTAGE) & 1)) break;
+                        ++n_clean;
+                    }
+                    ++fill;
+                    const int ks = fill % NSTAGE;
+                    for (int h = 0; h < 2 && ok; ++h) {
+                        if (j < it.n[h]) {
+                            if (!wait(&p_full[h], p_n[h]++ & 1)) break;
+                            values(h, vs, j == 0, j + 1 == it.n[h]);
+                        }
+                        if (j + 1 < it.n[h]) {
+                            if (!wait(&full[ks], (fill / NSTAGE) & 1)) break;
+                            scores(h, ks, j + 2 == it.n[h]);
+                        }
+                    }
+                    if (!ok) break;
+                    release(vs);
+                    if (j + 1 < n) {
+                        release(ks);
+                        ++fill;
+                    }
+                }
+            }
+            // what was issued has to end before tensor and shared memory are given back
+            if (pf_elect()) pf_commit(drained);
+            __syncwarp();
+            mbar_wait(drained, 0);
+            if (!ok && lane == 0) {
+                s_dead = 1;
+                if (a.status) atomicOr(a.status, ETA_DEV_TIMEOUT);
+            }
+        } else {
+            // -------------------------------------------------------------- values that not every row may see
+            uint32_t fill = 0, n_clean = 0;
+            int item = 0;
+            const int w = warp - 10;
+            while (ok && walk.next(it)) {
+                ++item;
+                const int n = max(it.n[0], it.n[1]);
+                for (int j = 0; j < n; ++j) {
+                    ++fill;                            // K's
+                    const int stage = fill % NSTAGE;
+                    ok = __all_sync(0xffffffffu, pf_wait(&full[stage], (fill / NSTAGE) & 1, &s_dead));
+                    if (!ok) break;
+                    ++fill;
+                    if (it.k0 + j >= it.clean0) {
+                        bool found = false;
+                        unsigned char* const tile = smem + L::RING + stage * L::STAGE + w * (PF_TILE / 2 * 128) + lane * 16;
+                        const int t0 = (it.k0 + j) * PF_TILE + w * (PF_TILE / 2) + (lane >> 3);
+#pragma unroll 4
+                        for (int r = 0; r < PF_TILE / 2; r += 4)
+#pragma unroll
+                            for (int c = 0; c < HALVES; ++c) {
+                                uint4* const at = reinterpret_cast<uint4*>(tile + c * (PF_TILE * 128) + r * 128);
+                                if (t0 + r >= it.kv_end) {
+                                    *at = make_uint4(0, 0, 0, 0);
+                                } else {
+                                    uint4 v = *at;
+                                    uint32_t* const x = reinterpret_cast<uint32_t*>(&v);
+                                    uint32_t bad = 0;
+#pragma unroll
+                                    for (int u = 0; u < 4; ++u) {
+                                        const uint32_t hi = (x[u] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+                                        const uint32_t lo = (x[u] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u;
+                                        bad |= hi | lo;
+                                        x[u] &= ~(hi | lo);
+                                    }
+                                    if (bad) { *at = v; found = true; }
+                                }
+                            }
+                        if (found) s_poison[item & 15] = item;
+                        fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&cleaned[n_clean % NSTAGE]);
+                        ++n_clean;
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&empty[stage]);
+                }
+            }
+            if (!ok && lane == 0) s_dead = 1;
+        }
+    } else {
+        // ------------------------------------------------------------------ softmax and epilogue: a row per thread
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PF_REGS_SOFTMAX));
+        constexpr float LOG2E = 1.4426950408889634f;
+        const int half = warp >> 2, wrow = (warp & 3) * 32, row = wrow + lane;
+        const uint32_t lanes = (uint32_t)wrow << 16, t_s = tmem + lanes + half * PF_TILE, t_o = tmem + lanes + 2 * PF_TILE + half * D;
+        const float sl2 = a.scale * LOG2E, kb = a.scale * a.beta * LOG2E;
+        uint32_t s_n = 0, o_n = 0;
+        int item = 0;
+        while (ok && walk.next(it)) {
+            ++item;
+            const int tok0 = half * HT, toks = min(max(it.n_tok - tok0, 0), HT), rows = toks << a.g_shift;
+            if (!rows) continue;
+            const int n = it.n[half];
+            const bool live = wrow < rows;                  // a warp without rows only keeps step
+            const int r = min(row, rows - 1), tok = tok0 + (r >> a.g_shift), h = it.hk * G + (r & (G - 1));
+            const int p = it.p0 + tok;                      // the row sees tokens 0 .. p
+            float tb = 0.f;                                 // the gate is 1 / (1 + 2^(tb - kb q.k))
+            float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
+            if (GATED && live) {
+                const float tau = a.tau ? __ldcg(a.tau + (int64_t)(it.row0 + tok) * a.Hq + h) : __ldcg(a.head_const + h);
+                const float te = tau - a.a;
+                if (a.beta != 0.f) tb = te * a.beta * LOG2E;
+                if (te != te) l0 = te;                      // a threshold that is NaN: so is the row
+            }
+            float m = -INFINITY, c = -INFINITY;             // running maximum: of q.k, and in the exponents' units
+            for (int j = 0; j < n; ++j) {
+                ok = __all_sync(0xffffffffu, pf_wait(&s_full[half], s_n++ & 1, &s_dead));
+                if (!ok) break;
+                if (live) {
+                    pf_fence_after();
+                    float s[PF_TILE];
+#pragma unroll
+                    for (int k = 0; k < PF_TILE; k += 32) pf_ld32(t_s + k, s + k);
+                    pf_wait_ld();
+                    const int nvis = p - (it.k0 + j) * PF_TILE + 1;           // columns that the row sees
+                    const bool edge = __any_sync(0xffffffffu, nvis <= PF_TILE);
+                    if constexpr (GATED) {
+                        const int own = a.ungate ? nvis - 1 : -1;             // the column that stays raw
+                        auto gate = [&](auto masked) {
+#pragma unroll
+                            for (int k = 0; k < PF_TILE; k += 2) {
+                                float y0, y1;
+                                pf_fma2(y0, y1, s[k], s[k + 1], -kb, tb);
+                                const float e0 = pf_ex2(y0), e1 = pf_ex2(y1);
+                                // both reciprocals from one of the product; far below the threshold the gate is 0
+                                const float d0 = fminf(1.f + e0, 0x1p62f), d1 = fminf(1.f + e1, 0x1p62f);
+                                const float rr = pf_rcp(d0 * d1);
+                                const float g0 = e0 > 0x1p60f ? 0.f : rr * d1, g1 = e1 > 0x1p60f ? 0.f : rr * d0;
+                                float x0, x1;
+                                pf_fma2(x0, x1, s[k], s[k + 1], sl2, 0.f);
+                                if (decltype(masked)::value) {
+                                    s[k] = k < nvis ? (k == own ? x0 : x0 * g0) : -INFINITY;
+                                    s[k + 1] = k + 1 < nvis ? (k + 1 == own ? x1 : x1 * g1) : -INFINITY;
+                                } else {
+                                    s[k] = x0 * g0; s[k + 1] = x1 * g1;
+                                }
+                            }
+                        };
+                        if (edge) gate(std::true_type{});
+                        else gate(std::false_type{});
+                    } else if (edge) {
+#pragma unroll
+                        for (int k = 0; k < PF_TILE; ++k) s[k] = k < nvis ? s[k] : -INFINITY;
+                    }
+                    float x[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[k] = fmaxf(s[k], s[k + 8]);
+#pragma unroll
+                    for (int k = 16; k < PF_TILE; k += 16)
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) x[u] = fmaxf(fmaxf(x[u], s[k + u]), s[k + u + 8]);
+                    const float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+                    const float cx = GATED ? mx : mx * sl2;
+                    if (__any_sync(0xffffffffu, cx > c + PF_SLACK)) {
+                        const float c_new = fmaxf(c, cx);
+                        const float alpha = c == c_new ? 1.f : pf_ex2(c - c_new);
+                        m = fmaxf(m, mx);
+                        c = c_new;
+                        l0 *= alpha; l1 *= alpha; l2 *= alpha; l3 *= alpha;
+                        if (j) {                       // these scores are complete, so is the product before them
+#pragma unroll 1
+                            for (int k = 0; k < D; k += 32) {
+                                float o[32];
+                                pf_ld32(t_o + k, o);
+                                pf_wait_ld();
+#pragma unroll
+                                for (int u = 0; u < 32; ++u) o[u] *= alpha;
+                                pf_st32(t_o + k, reinterpret_cast<const uint32_t*>(o));
+                            }
+                        }
+                    }
+                    const float cu = c == -INFINITY ? 0.f : c;
+                    // q.k scale - maximum in one rounding, off by the rounding of the maximum's product: the same factor for the whole
+                    // row, which cancels.  Where that could be a large one the difference is formed first.
+                    const bool huge = !GATED && fabsf(cu) > 4194304.f;
+                    const float mu = m == -INFINITY ? 0.f : m;
+                    if (!GATED && __any_sync(0xffffffffu, huge)) {
+#pragma unroll
+                        for (int k = 0; k < PF_TILE; ++k) s[k] = huge ? (s[k] - mu) * sl2 : fmaf(s[k], sl2, -cu);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < PF_TILE; k += 2) pf_fma2(s[k], s[k + 1], s[k], s[k + 1], GATED ? 1.f : sl2, -cu);
+                    }
+#pragma unroll
+                    for (int k = 0; k < PF_TILE; k += 64) {
+                        uint32_t w[32];
+#pragma unroll
+                        for (int u = 0; u < 32; u += 2) {
+                            const float p0 = pf_ex2(s[k + 2 * u]), p1 = pf_ex2(s[k + 2 * u + 1]), p2 = pf_ex2(s[k + 2 * u + 2]), p3 = pf_ex2(s[k + 2 * u + 3]);
+                            add2(l0, l1, p0, p1);
+                            add2(l2, l3, p2, p3);
+                            w[u] = pf_pack(p0, p1);
+                            w[u + 1] = pf_pack(p2, p3);
+                        }
+                        pf_st32(t_s + k / 2, w);
+                    }
+                    pf_wait_st();
+                    pf_fence_before();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[half]);
+            }
+            if (!ok) break;
+            if (n) {
+                ok = __all_sync(0xffffffffu, pf_wait(&o_full[half], o_n++ & 1, &s_dead));
+                if (!ok) break;
+            }
+            if (!live) continue;
+            pf_fence_after();
+            const float l = (l0 + l1) + (l2 + l3);
+            const bool mine = row < rows, split = it.slot >= 0;
+            const bool poison = n && s_poison[item & 15] == item;
+            const int64_t part = ((int64_t)it.slot * PF_ROWS + half * PF_HALF + row);
+            if (split && mine) a.part_ml[part] = make_float2(c, l);
+            const float inv = split ? 1.f : (l == 0.f ? 0.f : 1.f / l);
+            __nv_bfloat16* const to = a.out + ((int64_t)(it.row0 + tok) * a.Hq + h) * D;
+#pragma unroll 1
+            for (int k = 0; k < D; k += 32) {
+                float o[32];
+                if (n) {
+                    pf_ld32(t_o + k, o);
+                    pf_wait_ld();
+#pragma unroll
+                    for (int u = 0; u < 32; ++u) o[u] *= inv;
+                } else {
+#pragma unroll
+                    for (int u = 0; u < 32; ++u) o[u] = 0.f;
+                }
+                if (poison) {
+                    const int end = (int)min((int64_t)p + 1, (int64_t)(it.k0 + n) * PF_TILE);
+                    for (int t = max(it.clean0, it.k0) * PF_TILE; t < end; ++t) {
+                        const int64_t base = a.block_table
+                            ? (int64_t)__ldcg(a.block_table + (int64_t)it.seq * a.table_stride + (t >> a.b_shift)) * a.v_sb + (int64_t)(t & ((1 << a.b_shift) - 1)) * a.v_st
+                            : (int64_t)it.seq * a.v_sb + (int64_t)t * a.v_st;
+                        const uint4* const from = reinterpret_cast<const uint4*>(a.V + base + it.hk * a.v_sh + k);
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            const uint4 v = __ldcg(from + u);
+                            const uint32_t x4[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                const float lo = bf16_lo(x4[q]), hi = bf16_hi(x4[q]);
+                                if (!isfinite(lo)) o[8 * u + 2 * q] += lo;
+                                if (!isfinite(hi)) o[8 * u + 2 * q + 1] += hi;
+                            }
+                        }
+                    }
+                }
+                if (!mine) continue;
+                if (split) {
+                    float4* const at = reinterpret_cast<float4*>(a.part_o + part * D + k);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) at[u] = make_float4(o[4 * u], o[4 * u + 1], o[4 * u + 2], o[4 * u + 3]);
+                } else {
+                    uint4* const at = reinterpret_cast<uint4*>(to + k);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        at[u] = make_uint4(pf_pack(o[8 * u], o[8 * u + 1]), pf_pack(o[8 * u + 2], o[8 * u + 3]), pf_pack(o[8 * u + 4], o[8 * u + 5]),
+                                           pf_pack(o[8 * u + 6], o[8 * u + 7]));
+                }
+            }
+            pf_fence_before();
+        }
+        if (!ok && lane == 0) s_dead = 1;
+        pdl_trigger();
+    }
+    pf_fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        pf_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
+// Joins the parts of split items, in the order of their tiles.  A CTA per (share in which a split item starts, 32 of its rows), a warp per row.
+constexpr int PF_JOIN_ROWS = 32, PF_JOIN_WARPS = 8;
+template <int D>
+__global__ void __launch_bounds__(32 * PF_JOIN_WARPS) prefill_join_kernel(const __grid_constant__ PrefillArgs a) {
+    const int cta = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    pdl_wait();
+    const int4 d = __ldcg(a.desc + cta);
+    const int pieces = d.x, rows = d.z << a.g_shift, G = 1 << a.g_shift;
+    if (pieces < 2) return;
+    constexpr int PER = D / 32;
+    for (int r = blockIdx.y * PF_JOIN_ROWS + warp; r < min(rows, (int)(blockIdx.y + 1) * PF_JOIN_ROWS); r += PF_JOIN_WARPS) {
+        // the first part is the second slot of its share, the others the first of theirs
+        auto slot = [&](int k) { return (int64_t)(2 * (cta + k) + (k == 0)) * PF_ROWS + r; };
+        float M = -INFINITY;
+        for (int k = lane; k < pieces; k += 32) M = fmaxf(M, __ldcg(a.part_ml + slot(k)).x);
+#pragma unroll
+        for (int s = 16; s >= 1; s >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, s));
+        float acc[PER], l = 0.f;
+#pragma unroll
+        for (int u = 0; u < PER; ++u) acc[u] = 0.f;
+#pragma unroll 4
+        for (int k = 0; k < pieces; ++k) {
+            const float2 ml = __ldcg(a.part_ml + slot(k));
+            const float* const o = a.part_o + slot(k) * D + PER * lane;
+            float v[PER];
+            if constexpr (PER == 4) {
+                const float4 t = __ldcg(reinterpret_cast<const float4*>(o));
+                v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
+            } else {
+                const float2 t = __ldcg(reinterpret_cast<const float2*>(o));
+                v[0] = t.x; v[1] = t.y;
+            }
+            if (ml.x == -INFINITY && ml.y == 0.f) continue;             // the row saw none of this part
+            const float w = ml.x == M ? 1.f : exp2f(ml.x - M);
+            l = fmaf(ml.y, w, l);
+#pragma unroll
+            for (int u = 0; u < PER; ++u) acc[u] = fmaf(v[u], w, acc[u]);
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        __nv_bfloat16* const to = a.out + ((int64_t)(d.y + (r >> a.g_shift)) * a.Hq + d.w * G + (r & (G - 1))) * D + PER * lane;
+        if constexpr (PER == 4)
+            *reinterpret_cast<uint2*>(to) = make_uint2(pf_pack(acc[0] * inv, acc[1] * inv), pf_pack(acc[2] * inv, acc[3] * inv));
+        else
+            *reinterpret_cast<uint32_t*>(to) = pf_pack(acc[0] * inv, acc[1] * inv);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+
+struct PfScratch { size_t desc, part_ml, part_o, total; };
+static PfScratch pf_scratch(int D) {
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    PfScratch s;
+    s.desc = 0;
+    s.part_ml = up(sizeof(int4) * PF_MAX_CTAS);
+    s.part_o = up(s.part_ml + sizeof(float2) * 2 * PF_MAX_CTAS * PF_ROWS);
+    s.total = up(s.part_o + sizeof(float) * 2 * PF_MAX_CTAS * PF_ROWS * D);
+    return s;
+}
+
+static int pf_validate(const eta_cache_desc* d) {
+    int rc = validate_shape(d);
+    if (rc == ETA_OK) rc = validate_strides(d);
+    if (rc != ETA_OK) return rc;
+    return d->batch > PF_MAX_BATCH || d->n_kv_heads > 1024 ? ETA_ERR_UNSUPPORTED : ETA_OK;
+}
+
+template <int D, bool GATED>
+static int pf_launch(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const PrefillArgs& a, int ctas, cudaStream_t s) {
+    // the warps' shares of the registers are drawn from what the block is launched with
+    cudaFuncAttributes attr;
+    const cudaError_t e = cudaFuncGetAttributes(&attr, prefill_kernel<D, GATED>);
+    if (e != cudaSuccess) { set_cuda_error(e, "eta_prefill"); return ETA_ERR_CUDA; }
+    if (attr.numRegs < PF_REGS) return ETA_ERR_UNSUPPORTED;
+    const int rc = launch_pdl("eta_prefill", prefill_kernel<D, GATED>, dim3(ctas), dim3(PF_THREADS), PfSmem<D>::BYTES, s, tmQ, tmK, tmV, a);
+    if (rc != ETA_OK) return rc;
+    return launch_pdl("eta_prefill", prefill_join_kernel<D>, dim3(ctas, PF_ROWS / PF_JOIN_ROWS), dim3(32 * PF_JOIN_WARPS), 0, s, a);
+}
+
+}  // namespace eta
+
+extern "C" {
+
+// Host-only check of how work is shared out: for made-up lengths every tile of every item is in exactly one share, the parts of a split
+// item have slots of their own, in order, and whoever has the first part knows their number.  Not part of the public interface; called by the
+// CPU test-suite.  n, len: [batch] new tokens and tokens cached.  -> 0, or the number of the first expectation that failed.
+int eta_selftest_prefill_shares(int batch, int n_kv_heads, int g_shift, int head_dim, int ctas, const int32_t* n, const int32_t* len,
+                                int* whole) {
+    using namespace eta;
+    static PfTables tab;
+    const int m = PF_ROWS >> g_shift;
+    tab.longest = 0;
+    tab.items[0] = 0; tab.cost[0] = 0;
+    int rows = 0;
+    for (int i = 0; i < batch; ++i) {
+        const PfTiles ti(len[i], n[i], m);
+        tab.row0[i] = rows; tab.n[i] = n[i]; tab.len[i] = len[i];
+        rows += n[i];
+        tab.items[i + 1] = tab.items[i] + ti.nq * n_kv_heads;
+        tab.cost[i + 1] = tab.cost[i] + n_kv_heads * ti.cost_before(ti.nq);
+        if (n[i] && ti.tiles(ti.nq - 1) > tab.longest) tab.longest = ti.tiles(ti.nq - 1);
+        int64_t sum = 0;
+        for (int t = 0; t < ti.nq; ++t) {
+            if (ti.before(t) != sum) return 1;
+            sum += ti.tiles(t);
+        }
+        if (ti.before(ti.nq) != sum) return 2;
+    }
+    // per item: next tile expected, parts seen, parts announced
+    struct Seen { int next = 0, parts = 0, said = 0, last = -2; };
+    std::vector<Seen> seen((size_t)rows * n_kv_heads + 1);
+    for (int c = 0; c < ctas; ++c) {
+        PfWalk w(tab, batch, n_kv_heads, g_shift, head_dim, c, ctas);
+        *whole = w.whole;
+        PfItem it;
+        int starts = 0;
+        while (w.next(it)) {
+            if (it.seq < 0 || it.seq >= batch || it.hk < 0 || it.hk >= n_kv_heads || it.n_tok < 1 || it.n_tok > m) return 3;
+            const int tok = it.row0 - tab.row0[it.seq];
+            if (tok < 0 || tok % m || tok + it.n_tok > n[it.seq] || it.p0 != len[it.seq] - n[it.seq] + tok) return 4;
+            Seen& s = seen[(size_t)it.row0 * n_kv_heads + it.hk];
+            const int all = it.p0 + it.n_tok > 0 ? (it.p0 + it.n_tok - 1) / PF_TILE + 1 : 0;
+            if (it.slot < 0) {
+                if (s.parts || it.k0 != 0 || std::max(it.n[0], it.n[1]) != all) return 5;
+                s.parts = s.said = 1; s.next = all;
+                continue;
+            }
+            if (it.slot != 2 * c && it.slot != 2 * c + 1) return 6;
+            if (it.slot == 2 * c + 1) {
+                if (it.k0 != 0 || s.parts || ++starts > 1 || it.pieces < 2 || c + it.pieces > ctas) return 7;
+                s.said = it.pieces;
+            } else if (!s.parts || it.k0 < s.next || s.last != c - 1) {
+                return 8;
+            }
+            // (a gap is allowed only behind the tiles that count: positions before the sequence's first token)
+            if (it.k0 > s.next && s.next < all) return 9;
+            if (it.n[0] || it.n[1]) s.next = it.k0 + std::max(it.n[0], it.n[1]);
+            s.last = c;
+            ++s.parts;
+        }
+    }
+    for (int i = 0; i < batch; ++i)
+        for (int t = 0; t < n[i]; t += m)
+            for (int h = 0; h < n_kv_heads; ++h) {
+                const Seen& s = seen[(size_t)(tab.row0[i] + t) * n_kv_heads + h];
+                const int end = len[i] - n[i] + std::min(t + m, n[i]), all = end > 0 ? (end - 1) / PF_TILE + 1 : 0;
+                if (!s.parts || s.parts != s.said || s.next != all) return 10;
+            }
+    return 0;
+}
+
+int eta_prefill_workspace_bytes(const eta_cache_desc* desc, size_t* out_bytes) {
+    if (!out_bytes) return ETA_ERR_INVALID_ARG;
+    const int rc = eta::pf_validate(desc);
+    if (rc != ETA_OK) return rc;
+    *out_bytes = eta::pf_scratch(desc->head_dim).total;
+    return ETA_OK;
+}
+
+int eta_prefill(const eta_cache_desc* desc, const eta_page_table* pages, const eta_params* params, int32_t n_rows, const void* q,
+                const int32_t* row_start, const int32_t* seq_lens, const int32_t* granted, const void* K, const void* V, const float* tau,
+                const float* head_const, void* out, uint32_t* status_dev, void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace eta;
+    int rc = pf_validate(desc);
+    if (rc != ETA_OK) return rc;
+    if (pages && (rc = validate_pages(desc, pages)) != ETA_OK) return rc;
+    if (!params || n_rows < 0 || !row_start || !seq_lens || !K || !V || (n_rows && (!q || !out))) return ETA_ERR_INVALID_ARG;
+    const bool dense = (params->flags & ETA_FLAG_DENSE) != 0;
+    if (!dense && (tau != nullptr) == (head_const != nullptr)) return ETA_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V) | reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15)
+        return ETA_ERR_UNSUPPORTED;
+    const int D = desc->head_dim, G = desc->n_q_heads / desc->n_kv_heads;
+    // items are counted in 32 bits
+    if (n_rows > (1 << 30) || ((int64_t)n_rows * G / PF_ROWS + desc->batch) * desc->n_kv_heads > (1 << 30)) return ETA_ERR_UNSUPPORTED;
+    const PfScratch L = pf_scratch(D);
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < L.total) return ETA_ERR_WORKSPACE;
+    if (n_rows == 0) return ETA_OK;
+
+    const int n_pages = pages ? pages->n_pages : 0;
+    CUtensorMap tmQ, tmK, tmV;
+    {
+        const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)desc->n_q_heads, (cuuint64_t)n_rows};
+        const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)desc->n_q_heads * D * 2};
+        const cuuint32_t box[3] = {64, (cuuint32_t)G, (cuuint32_t)(PF_HALF / G)};
+        if ((rc = encode_tiles(&tmQ, q, 3, dims, strides, box)) != ETA_OK) return rc;
+    }
+    auto cache_map = [&](CUtensorMap* tm, const void* base, int64_t sb, int64_t sh, int64_t st) {
+        const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)(pages ? desc->block_size : desc->t_cap), (cuuint64_t)desc->n_kv_heads,
+                                    (cuuint64_t)(pages ? n_pages : desc->batch)};
+        const cuuint64_t strides[3] = {(cuuint64_t)st * 2, (cuuint64_t)sh * 2, (cuuint64_t)sb * 2};
+        const cuuint32_t box[4] = {64, (cuuint32_t)(pages ? desc->block_size : PF_TILE), 1, 1};
+        return encode_tiles(tm, base, 4, dims, strides, box);
+    };
+    if ((rc = cache_map(&tmK, K, desc->k_stride_b, desc->k_stride_h, desc->k_stride_t)) != ETA_OK) return rc;
+    if ((rc = cache_map(&tmV, V, desc->v_stride_b, desc->v_stride_h, desc->v_stride_t)) != ETA_OK) return rc;
+
+    int dev = 0, n_sm = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) { set_cuda_error(e, "device query"); return ETA_ERR_CUDA; }
+    const int ctas = n_sm < PF_MAX_CTAS ? n_sm : PF_MAX_CTAS;
+
+    unsigned char* const ws = static_cast<unsigned char*>(workspace);
+    PrefillArgs a;
+    a.row_start = row_start; a.seq_lens = seq_lens; a.granted = granted;
+    a.block_table = pages ? pages->block_table : nullptr;
+    a.table_stride = pages ? pages->table_stride : 0;
+    a.tau = tau; a.head_const = head_const;
+    a.V = static_cast<const __nv_bfloat16*>(V);
+    a.v_sb = desc->v_stride_b; a.v_sh = desc->v_stride_h; a.v_st = desc->v_stride_t;
+    a.out = static_cast<__nv_bfloat16*>(out);
+    a.desc = reinterpret_cast<int4*>(ws + L.desc);
+    a.part_ml = reinterpret_cast<float2*>(ws + L.part_ml);
+    a.part_o = reinterpret_cast<float*>(ws + L.part_o);
+    a.status = status_dev;
+    a.a = params->a; a.beta = params->beta;
+    a.scale = params->scale > 0.f ? params->scale : 1.0f / sqrtf((float)D);
+    a.batch = desc->batch; a.Hq = desc->n_q_heads; a.Hkv = desc->n_kv_heads;
+    a.g_shift = G == 1 ? 0 : (G == 2 ? 1 : (G == 4 ? 2 : 3));
+    a.b_shift = desc->block_size == 32 ? 5 : (desc->block_size == 64 ? 6 : 7);
+    a.t_cap = desc->t_cap; a.n_rows = n_rows;
+    a.ungate = (params->flags & ETA_FLAG_UNGATE_LAST) ? 1 : 0;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (D == 128) return dense ? pf_launch<128, false>(tmQ, tmK, tmV, a, ctas, s) : pf_launch<128, true>(tmQ, tmK, tmV, a, ctas, s);
+    return dense ? pf_launch<64, false>(tmQ, tmK, tmV, a, ctas, s) : pf_launch<64, true>(tmQ, tmK, tmV, a, ctas, s);
+}
+
+}  // extern "C"

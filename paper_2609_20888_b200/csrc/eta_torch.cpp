@@ -542,6 +542,47 @@ PyObject* decode_kv4(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return PyLong_FromLong(rc);
 }
 
+// (address, desc, pages or None, params, q, row_start, seq_lens, granted, K, V, tau, head_const, out, status, workspace) -> return code
+PyObject* prefill(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    using F = int (*)(const eta_cache_desc*, const eta_page_table*, const eta_params*, int32_t, const void*, const int32_t*, const int32_t*,
+                      const int32_t*, const void*, const void*, const float*, const float*, void*, uint32_t*, void*, size_t, void*);
+    F fn;
+    Struct<eta_cache_desc> ds;
+    Struct<eta_page_table> ps;
+    eta_params p;
+    void *q, *K, *V, *out, *workspace;
+    int32_t *row_start, *seq_lens, *granted;
+    float *tau, *head_const;
+    uint32_t* status;
+    if (!count(n, 15) || !entry(v[0], &fn)) return nullptr;
+    const eta_cache_desc* d = ds.get(v[1], g_desc);
+    if (!d) return nullptr;
+    const eta_page_table* pages = nullptr;
+    if (v[2] != Py_None && !(pages = ps.get(v[2], g_pages))) return nullptr;
+    if (!params_of(v[3], &p) || !shaped(v[4], at::kBFloat16, "q", {-1, d->n_q_heads, d->head_dim}, &q)) return nullptr;
+    const at::Tensor& tq = THPVariable_Unpack(v[4]);
+    const int64_t rows = tq.size(0);
+    if (!tq.is_contiguous()) return fail("q", "contiguous"), nullptr;
+    if (rows > INT32_MAX) return fail("q", "of fewer than 2^31 rows"), nullptr;
+    const bool paged = pages != nullptr;
+    if (!VEC(v[5], at::kInt, row_start, (int64_t)d->batch + 1) || !VEC(v[6], at::kInt, seq_lens, d->batch) || !OPT(v[7], at::kInt, granted, d->batch) ||
+        !cache_tensor(v[8], "K", d, paged, &K) || !same_strides(v[8], "K", {d->k_stride_b, d->k_stride_h, d->k_stride_t}) ||
+        !cache_tensor(v[9], "V", d, paged, &V) || !same_strides(v[9], "V", {d->v_stride_b, d->v_stride_h, d->v_stride_t}) ||
+        !OPT(v[10], at::kFloat, tau, rows * d->n_q_heads) || !OPT(v[11], at::kFloat, head_const, d->n_q_heads) ||
+        !VEC(v[12], at::kBFloat16, out, rows * d->n_q_heads * d->head_dim) || !OPT(v[13], at::kInt, status, 1) ||
+        !VEC(v[14], at::kByte, workspace, -1))
+        return nullptr;
+    if (paged && (pages->n_pages > THPVariable_Unpack(v[8]).size(0) || pages->n_pages > THPVariable_Unpack(v[9]).size(0)))
+        return fail("pages", "of a pool with no more pages than K and V"), nullptr;
+    const size_t bytes = (size_t)THPVariable_Unpack(v[14]).numel();
+    void* const s = stream();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn(d, pages, &p, (int32_t)rows, q, row_start, seq_lens, granted, K, V, tau, head_const, out, status, workspace, bytes, s);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
 // the eta_params a call would get, as bytes (for the tests)
 PyObject* params(PyObject*, PyObject* const* v, Py_ssize_t n) {
     eta_params p;
@@ -583,6 +624,7 @@ PyMethodDef methods[] = {
     {"decode_kv4", (PyCFunction)(void (*)(void))guarded<decode_kv4>, METH_FASTCALL, nullptr},
     {"unpack", (PyCFunction)(void (*)(void))guarded<unpack>, METH_FASTCALL, nullptr},
     {"plan", (PyCFunction)(void (*)(void))guarded<plan>, METH_FASTCALL, nullptr},
+    {"prefill", (PyCFunction)(void (*)(void))guarded<prefill>, METH_FASTCALL, nullptr},
     {"params", (PyCFunction)(void (*)(void))guarded<params>, METH_FASTCALL, nullptr},
     {"set_classes", (PyCFunction)(void (*)(void))set_classes, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
