@@ -5,15 +5,25 @@
 //   S~ = S (softmax), or S sigmoid(beta (S - tau_eff)) (Eq. mult_attn), raw for t = p(r) with ETA_FLAG_UNGATE_LAST
 //
 // A work item is 256 query rows of one (sequence, KV head): 256 / G tokens with the G heads of the group packed behind each other, so
-// that a tile of K and V serves them all.  The rows are two halves of 128 with a softmax warpgroup each, a row per thread, and take
-// turns on the tensor core: while one half's scores are turned into weights the other half's products run.
+// that a tile of K and V serves them all.  The rows are two halves of 128, which take turns on the tensor core: while one half's scores
+// are turned into weights the other half's products run.  An item with rows for one half only (a single token) gives them to both
+// halves, which take the tiles in turns; the second hands its sums to the first at the end.
 //   tensor memory   S of each half (128 fp32 columns; its weights, bf16, overwrite the first 64), O of each half (head_dim columns)
 //   shared memory   the queries (two halves), a ring of K and V tiles of 128 tokens (128-byte swizzle, 64-column halves)
-//   warps           0-3, 4-7 softmax and epilogue; 8 copies (TMA, a copy per page and 64 columns); 9 issues the MMAs; 10, 11 clean tiles
+//   warps           0-15 softmax and epilogue, two threads to a row; 16 copies (TMA, a copy per page and 64 columns); 17 issues the MMAs;
+//                   18, 19 clean tiles
 // S = Q K^T has both operands in shared memory; O += P V takes P from tensor memory and V as it lies (token-major).
 // The running maximum moves only when it would by more than 2^8: weights are then at most 2^8 and O is rescaled a few times a row
 // instead of once a tile.  Weights are rounded to bf16 (relative 2^-8, as much as the output's own rounding); their sum, O and
 // the maximum are fp32.
+//
+// What bounds it: a tile of a half is a chain, S (512 cycles at head_dim 128) -> maximum -> weights (1024 cycles of the special function
+// unit for the 128 x 128 exponentials) -> O (512), and there is tensor memory for two halves, not three.  One 8K prompt of 32 / 8
+// heads of 128 takes 560 us (980 TFLOP/s), 32K 7.8 ms (1130, at the power limit: 1.64 GHz); gated scores take two more special functions
+// and a dozen instructions each: 11 packed prompts to 5K 1.09 ms (490).  64 single tokens behind 16K stream at 4.4 TB/s.
+// Tried: a thread per row and eight softmax warps 8.4 to 9.4 ms for 32K; a warp for each half's MMAs, whose halves fall into step, 10.3;
+// a quarter of the exponentials as polynomials on the fp32 pipe 9.2 (power); steps of 64 tokens with the next scores worked out
+// ahead 11.9 (twice the hand-overs; an S of 64 columns runs at two thirds of the rate); all waits and MMAs from one lane 10.5.
 //
 // V rows that some row of the item must not see (behind its position, or behind the sequence) would reach it as 0 * V, which is not 0 for
 // infinities and NaN.  In the one to three tiles of an item where that can be, two warps take them out of the shared-memory tile: rows
@@ -34,15 +44,18 @@ namespace eta {
 constexpr int PF_TILE = 128;               // tokens of a K or V tile
 constexpr int PF_HALF = 128;               // query rows of a half item
 constexpr int PF_ROWS = 2 * PF_HALF;
-constexpr int PF_THREADS = 384;
+constexpr int PF_SOFTMAX_WARPS = 16, PF_WARPS = PF_SOFTMAX_WARPS + 4, PF_THREADS = 32 * PF_WARPS;
+constexpr int PF_COPY = PF_SOFTMAX_WARPS, PF_MMA = PF_COPY + 1, PF_CLEAN = PF_MMA + 1;       // warps
 constexpr int PF_MAX_CTAS = 160;           // sizes the scratch of split items
 constexpr int PF_MAX_BATCH = 1024;         // sequences whose prefix sums a CTA keeps in shared memory
-constexpr int PF_ITEM_COST = 2;            // what an item costs beside its tiles, in tiles: queries, output, a pipeline that runs dry
-constexpr int PF_SPLIT_COST = 4;           // what joining split items costs, in tiles
+// What an item costs beside its tiles, in tiles (queries, output, a pipeline that runs dry): with 1 and 2 the shares of an 8K prompt that hold
+// the short items were late (700, 652 us; 4: 560).  What joining split items costs.
+constexpr int PF_ITEM_COST = 4, PF_SPLIT_COST = 4;
 constexpr int64_t PF_L2_BYTES = 64ll << 20;     // K and V of the heads that are worked on side by side
-// registers: 384 threads start with 168; 256 of them take 208, the others 88 (together what the block was launched with)
-constexpr int PF_REGS = 168, PF_REGS_SOFTMAX = 208, PF_REGS_OTHER = 88;
-static_assert(256 * PF_REGS_SOFTMAX + 128 * PF_REGS_OTHER <= PF_REGS * PF_THREADS, "more registers than the block has");
+// registers: 640 threads start with 96; 512 of them take 104, the others 64 (together what the block was launched with)
+constexpr int PF_REGS = 96, PF_REGS_SOFTMAX = 104, PF_REGS_OTHER = 64;
+static_assert(32 * (PF_SOFTMAX_WARPS * PF_REGS_SOFTMAX + 4 * PF_REGS_OTHER) <= PF_REGS * PF_THREADS, "more registers than the block has");
+constexpr int PF_CHUNKS = 2;              // weights are handed to the tensor core in so many chunks: of both threads' tokens of a row a part each
 constexpr float PF_SLACK = 8.f;            // log2 of how far a weight may exceed 1
 
 struct PrefillArgs {
@@ -72,22 +85,20 @@ struct PfTiles {
         base = max(len - n, 0);
     }
     PF_BOTH int tiles(int t) const { return (int)(((int64_t)base + min((int64_t)(t + 1) * m, (int64_t)n) + PF_TILE - 1) / PF_TILE); }
-    // sum over the first t query tiles, t <= nq
+    // sum of the tiles of the first t query tiles, t < nq (the last one may be shorter)
     PF_BOTH int64_t before(int t) const {
-        int64_t last = 0;
-        if (t == nq && t > 0) { last = tiles(--t); }
         const int64_t b0 = (int64_t)base + m + PF_TILE - 1;
-        int64_t sum;
-        if (m >= PF_TILE) {
-            sum = t * (b0 / PF_TILE) + (int64_t)(m / PF_TILE) * t * (t - 1) / 2;
-        } else {
-            const int p = PF_TILE / m, U = t / p, R = t % p;
-            sum = (int64_t)p * U * (U - 1) / 2 + (int64_t)R * U;
-            for (int v = 0; v < p; ++v) sum += (int64_t)(U + (v < R)) * ((b0 + v * m) / PF_TILE);
-        }
-        return sum + last;
+        if (m >= PF_TILE) return t * (b0 / PF_TILE) + (int64_t)(m / PF_TILE) * t * (t - 1) / 2;
+        const int p = PF_TILE / m, U = t / p, R = t % p;
+        int64_t sum = (int64_t)p * U * (U - 1) / 2 + (int64_t)R * U;
+        for (int v = 0; v < p; ++v) sum += (int64_t)(U + (v < R)) * ((b0 + v * m) / PF_TILE);
+        return sum;
     }
-    PF_BOTH int64_t cost_before(int t) const { return before(t) + (int64_t)t * PF_ITEM_COST; }
+    // cost of the first t query tiles, t <= nq
+    PF_BOTH int64_t cost_before(int t) const {
+        if (t < nq || !t) return before(t) + (int64_t)t * PF_ITEM_COST;
+        return before(t - 1) + tiles(t - 1) + (int64_t)t * PF_ITEM_COST;
+    }
 };
 
 struct PfTables {                          // in shared memory
@@ -101,7 +112,8 @@ struct PfItem {
     int seq, hk, row0, n_tok;              // first row in the packed rows, tokens that count
     int p0;                                // position of the first token
     int kv_end;                            // tokens [0, kv_end) are seen by some row
-    int k0, n[2];                          // first tile, tiles of each half
+    int k0, k1, n[2];                      // tiles [k0, k1); how many of them each half takes
+    bool twin;                             // rows for one half only: both have them and take turns on the tiles
     int clean0;                            // first tile in which not every row sees every token
     int slot;                              // of a part of a split item; -1: whole
     int pieces;                            // the parts of the item that starts here and goes on; 0: none
@@ -113,10 +125,9 @@ struct PfWalk {
     int batch, Hkv, m, cta, ctas;
     int64_t head_bytes;                    // bytes of K and V per token and KV head
     bool whole;                            // items in rounds, or shares
-    int64_t C, x, x1;                      // shares: all cost, the CTA's range
-    int P;
-    int round;
-    int total;
+    int64_t C, x, x1, start;               // shares: all cost, the CTA's range, where the next item starts
+    int P, seq, hk, qt;                    // shares; the next item
+    int round, total;
 
     PF_BOTH PfWalk(const PfTables& t, int batch_, int Hkv_, int g_shift, int D, int cta_, int ctas_) : tab(t) {
         batch = batch_; Hkv = Hkv_; m = PF_ROWS >> g_shift;
@@ -131,7 +142,22 @@ struct PfWalk {
         whole = est_whole <= mean + PF_ITEM_COST + PF_SPLIT_COST;
         P = (int)min((int64_t)ctas, max((int64_t)1, C / (PF_ITEM_COST + 4)));
         x = x1 = C;
-        if (!whole && cta < P) { x = C * cta / P; x1 = C * (cta + 1) / P; }
+        if (whole || cta >= P) return;
+        x = C * cta / P; x1 = C * (cta + 1) / P;
+        if (x >= x1) return;
+        // the item at x; the longest query tile of a head is the first: tile qt lies at [F - cost_before(qt + 1), F - cost_before(qt))
+        seq = last_not_above(tab.cost, x);
+        const PfTiles ti(tab.len[seq], tab.n[seq], m);
+        const int64_t F = ti.cost_before(ti.nq), in_seq = x - tab.cost[seq];
+        hk = (int)(in_seq / F);
+        const int64_t z = F - (in_seq - hk * F);
+        int lo = 0, hi = ti.nq;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (ti.cost_before(mid) < z) lo = mid; else hi = mid;
+        }
+        qt = lo;
+        start = tab.cost[seq] + hk * F + F - ti.cost_before(qt + 1);
     }
     template <typename T>
     PF_BOTH int last_not_above(const T* v, T key) const {
@@ -151,15 +177,19 @@ struct PfWalk {
         it.kv_end = max(0, it.p0 + it.n_tok);
         it.clean0 = it.p0 < 0 ? 0 : (it.p0 + 1) / PF_TILE;
     }
-    // tiles of each half within [k0, k1)
+    // the part of an item within [k0, k1)
     PF_BOTH void clip(PfItem& it, int k0, int k1) const {
         it.k0 = k0;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int tok = min(it.n_tok, (h + 1) * (m / 2));
-            const int end = tok > h * (m / 2) ? max(0, it.p0 + tok) : 0;
-            it.n[h] = max(0, min(k1, end > 0 ? (end - 1) / PF_TILE + 1 : 0) - k0);
+        it.k1 = min(k1, it.kv_end > 0 ? (it.kv_end - 1) / PF_TILE + 1 : 0);
+        const int n = max(0, it.k1 - k0);
+        it.twin = 2 * it.n_tok <= m && n > 1;
+        if (it.twin) {
+            it.n[0] = (n + 1) / 2; it.n[1] = n / 2;
+            return;
         }
+        const int end = it.p0 + min(it.n_tok, m / 2);          // of the first half's rows
+        it.n[0] = max(0, min(it.k1, end > 0 ? (end - 1) / PF_TILE + 1 : 0) - k0);
+        it.n[1] = 2 * it.n_tok > m ? n : 0;
     }
     PF_BOTH bool next(PfItem& it) {
         if (whole) {
@@ -184,32 +214,31 @@ struct PfWalk {
             return false;
         }
         while (x < x1) {
-            const int seq = last_not_above(tab.cost, x);
             const PfTiles ti(tab.len[seq], tab.n[seq], m);
-            const int64_t F = ti.cost_before(ti.nq), in_seq = x - tab.cost[seq];
-            const int hk = (int)(in_seq / F);
-            const int64_t y = in_seq - hk * F, z = F - y;
-            // the longest query tile first: tile qt lies at [F - cost_before(qt + 1), F - cost_before(qt))
-            int lo = 0, hi = ti.nq;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (ti.cost_before(mid) < z) lo = mid; else hi = mid;
+            const int tiles = ti.tiles(qt);
+            const int64_t end = start + PF_ITEM_COST + tiles;
+            const int k0 = (int)max((int64_t)0, x - start - PF_ITEM_COST);
+            const int k1 = (int)max((int64_t)0, min(x1, end) - start - PF_ITEM_COST);
+            if (k1 > k0) {                     // (else the share ends in the fixed part of the item)
+                fill(it, seq, hk, qt);
+                clip(it, k0, k1);
+                it.slot = -1; it.pieces = 0;
+                if (k0 > 0) {
+                    it.slot = 2 * cta;
+                } else if (k1 < tiles) {
+                    it.slot = 2 * cta + 1;
+                    it.pieces = (int)((end * P + C - 1) / C) - cta;          // up to the share that holds the item's last tile
+                }
             }
-            const int qt = lo, tiles = ti.tiles(qt);
-            const int64_t start = tab.cost[seq] + hk * F + F - ti.cost_before(qt + 1), end = start + PF_ITEM_COST + tiles;
-            const int k0 = (int)max((int64_t)0, x - start - PF_ITEM_COST), k1 = (int)max((int64_t)0, min(x1, end) - start - PF_ITEM_COST);
-            x = end;
-            if (k1 <= k0) continue;            // (a share that ends in the fixed part of an item)
-            fill(it, seq, hk, qt);
-            clip(it, k0, k1);
-            it.slot = -1; it.pieces = 0;
-            if (k0 > 0) {
-                it.slot = 2 * cta;
-            } else if (k1 < tiles) {
-                it.slot = 2 * cta + 1;
-                it.pieces = (int)((end * P + C - 1) / C) - cta;          // the share that holds the item's last tile
+            x = start = end;
+            if (--qt < 0) {
+                if (++hk == Hkv) {
+                    hk = 0;
+                    do ++seq; while (seq < batch && !tab.n[seq]);
+                }
+                if (seq < batch) qt = (tab.n[seq] + m - 1) / m - 1;
             }
-            return true;
+            if (k1 > k0) return true;
         }
         return false;
     }
@@ -255,8 +284,15 @@ __device__ __forceinline__ void pf_ld32(uint32_t addr, float* v) {
           "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
           "=r"(r[30]), "=r"(r[31]) : "r"(addr));
 }
+__device__ __forceinline__ void pf_ld16(uint32_t addr, float* v) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr));
+}
 __device__ __forceinline__ void pf_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void pf_st32(uint32_t addr, const uint32_t* r) {
+[[maybe_unused]] __device__ __forceinline__ void pf_st32(uint32_t addr, const uint32_t* r) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
         "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
@@ -278,6 +314,7 @@ __device__ __forceinline__ float pf_ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float pf_max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 __device__ __forceinline__ float pf_rcp(float x) {
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -301,6 +338,15 @@ __device__ __forceinline__ bool pf_elect() {
     return p != 0;
 }
 
+// Whether q holds for any thread of the N warps that share barrier `id`, which meet here
+template <int N>
+__device__ __forceinline__ bool pf_any_of(bool q, int id) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, o;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred o, %2, %3, p;\n\tselp.u32 %0, 1, 0, o;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)q), "r"(id), "n"(32 * N) : "memory");
+    return r != 0;
+}
+
 // A bounded wait that others' failures end too
 __device__ __forceinline__ bool pf_wait(uint64_t* bar, uint32_t parity, const volatile int* dead) {
     for (uint32_t it = 0; it < WAIT_LIMIT; ++it) {
@@ -321,7 +367,7 @@ struct PfSmem {
     static constexpr int RING = 2 * Q_BYTES;
     static constexpr int TABLES = RING + NSTAGE * STAGE;
     static constexpr int BARS = TABLES + (int)((sizeof(PfTables) + 15) / 16 * 16);
-    static constexpr int N_BARS = 3 * NSTAGE + 2 * 5 + 1;
+    static constexpr int N_BARS = 3 * NSTAGE + 2 * (4 + PF_CHUNKS) + 1;
     static constexpr int BYTES = 1024 + BARS + 8 * N_BARS;
     static_assert(BYTES <= 227 * 1024, "too much shared memory");
 };
@@ -338,11 +384,13 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
     uint64_t* const full = reinterpret_cast<uint64_t*>(smem + L::BARS);
     uint64_t *const empty = full + NSTAGE, *const cleaned = empty + NSTAGE;
     uint64_t *const q_full = cleaned + NSTAGE, *const q_empty = q_full + 2, *const s_full = q_empty + 2, *const p_full = s_full + 2,
-             *const o_full = p_full + 2, *const drained = o_full + 2;
+             *const o_full = p_full + 2 * PF_CHUNKS, *const drained = o_full + 2;
     __shared__ uint32_t s_tmem;
     __shared__ int s_dead;
     __shared__ int s_poison[16];               // item (counted from 1) of whose tiles values were taken out
-    __shared__ int64_t s_scan[PF_THREADS / 32][2];
+    __shared__ int64_t s_scan[PF_WARPS][2];
+    __shared__ float s_x[2][PF_ROWS];          // what the two threads of a row tell each other
+    __shared__ float2 s_twin[PF_HALF];         // maximum and sum of a twin item's second half
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int G = 1 << a.g_shift, HT = PF_HALF >> a.g_shift;       // heads of a group, tokens of a half
@@ -352,8 +400,9 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
         for (int k = 0; k < NSTAGE; ++k) { mbar_init(&full[k], 1); mbar_init(&empty[k], k & 1 ? 3 : 1); mbar_init(&cleaned[k], 2); }
         mbar_init(drained, 1);
         for (int k = 0; k < 2; ++k) {
-            mbar_init(&q_full[k], 1); mbar_init(&q_empty[k], 1); mbar_init(&s_full[k], 1);
-            mbar_init(&p_full[k], 4); mbar_init(&o_full[k], 1);
+            mbar_init(&q_full[k], 1); mbar_init(&q_empty[k], 1 + PF_SOFTMAX_WARPS / 2); mbar_init(&s_full[k], 1);
+            for (int c = 0; c < PF_CHUNKS; ++c) mbar_init(&p_full[k * PF_CHUNKS + c], PF_SOFTMAX_WARPS / 2);
+            mbar_init(&o_full[k], 1);
         }
         fence_barrier_init();
         prefetch_tmap(&tmQ); prefetch_tmap(&tmK); prefetch_tmap(&tmV);
@@ -361,7 +410,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
         tab.longest = 0;
     }
     if (tid < 16) s_poison[tid] = 0;
-    if (warp == 9) {
+    if (warp == PF_MMA) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -415,15 +464,15 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
     PfItem it;
     bool ok = true;
 
-    if (warp >= 8) {
+    if (warp >= PF_SOFTMAX_WARPS) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PF_REGS_OTHER));
-        if (warp == 8) {
+        if (warp == PF_COPY) {
             // -------------------------------------------------------------- copies
             uint32_t fill = 0, q_loads[2] = {0, 0};
             int4 split = make_int4(0, 0, 0, 0);
             while (ok && walk.next(it)) {
                 if (it.pieces > 1) split = make_int4(it.pieces, it.row0, it.n_tok, it.hk);
-                const int n = max(it.n[0], it.n[1]);
+                const int n = max(0, it.k1 - it.k0);
                 auto load_q = [&](int h) {
                     if (!ok || !it.n[h]) return;
                     if (q_loads[h] && !pf_wait(&q_empty[h], (q_loads[h] - 1) & 1, &s_dead)) { ok = false; return; }
@@ -434,7 +483,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                         for (int c = 0; c < HALVES; ++c)
                             asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
                                          ::"r"(smem_u32(smem + h * L::Q_BYTES + c * (PF_HALF * 128))), "l"(&tmQ), "r"(smem_u32(&q_full[h])),
-                                           "r"(64 * c), "r"(it.hk * G), "r"(it.row0 + h * HT) : "memory");
+                                           "r"(64 * c), "r"(it.hk * G), "r"(it.row0 + (it.twin ? 0 : h * HT)) : "memory");
                     }
                     __syncwarp();
                 };
@@ -486,81 +535,98 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                     if (q_loads[h]) mbar_wait(&q_full[h], (q_loads[h] - 1) & 1);
             }
             pdl_trigger();
-        } else if (warp == 9) {
+        } else if (warp == PF_MMA) {
             // -------------------------------------------------------------- MMAs; the whole warp walks along, one lane issues
             uint32_t fill = 0, n_clean = 0, q_n[2] = {0, 0}, p_n[2] = {0, 0};
-            const uint64_t q_op[2] = {pf_operand(smem_u32(smem), 16), pf_operand(smem_u32(smem + L::Q_BYTES), 16)};
-            const uint64_t ring_k = pf_operand(smem_u32(smem + L::RING), 16), ring_v = pf_operand(smem_u32(smem + L::RING), PF_TILE * 128);
+            const uint64_t q_op0 = pf_operand(smem_u32(smem), 16), ring_k = pf_operand(smem_u32(smem + L::RING), 16), ring_v = pf_operand(smem_u32(smem + L::RING), PF_TILE * 128);
             auto wait = [&](uint64_t* bar, uint32_t parity) {
                 ok = ok && pf_wait(bar, parity, &s_dead);
                 ok = __all_sync(0xffffffffu, ok);
-                pf_fence_after();
                 return ok;
-            };
-            // S = Q K^T of half h
-            auto scores = [&](int h, int stage, bool last) {
-                const uint64_t k_op = ring_k + (uint32_t)(stage * (L::STAGE >> 4));
-                if (pf_elect()) {
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k)       // 16 columns: 32 bytes along the swizzled row of a 64-column half
-                        pf_mma_ss(tmem + h * PF_TILE, q_op[h] + (k / 4) * (PF_HALF * 128 >> 4) + (k % 4) * 2,
-                                  k_op + (k / 4) * (PF_TILE * 128 >> 4) + (k % 4) * 2, pf_idesc(PF_TILE, false), k > 0);
-                    pf_commit(&s_full[h]);
-                    if (last) pf_commit(&q_empty[h]);
-                }
-                __syncwarp();
-            };
-            // O += P V of half h
-            auto values = [&](int h, int stage, bool first, bool last) {
-                const uint64_t v_op = ring_v + (uint32_t)(stage * (L::STAGE >> 4));
-                if (pf_elect()) {
-#pragma unroll
-                    for (int k = 0; k < PF_TILE / 16; ++k)     // 16 tokens: two groups of eight rows
-                        pf_mma_ts(tmem + 2 * PF_TILE + h * D, tmem + h * PF_TILE + 8 * k, v_op + k * (16 * 128 >> 4), pf_idesc(D, true),
-                                  !first || k > 0);
-                    if (last) pf_commit(&o_full[h]);
-                }
-                __syncwarp();
             };
             auto release = [&](int stage) {
                 if (pf_elect()) pf_commit(&empty[stage]);
                 __syncwarp();
             };
+            // One turn of half h: O += P V (vs: the stage of V; negative: none), then S = Q K^T of its next tile (ks), over the weights.
+            // What the second needs has been waited for, so that it goes out right behind the first.
+            auto turn = [&](int h, int vs, int ks, bool first, bool last_v, bool last_k) {
+                const uint64_t q_op = q_op0 + (uint32_t)(h * (L::Q_BYTES >> 4)), k_op = ring_k + (uint32_t)(max(ks, 0) * (L::STAGE >> 4));
+                const uint64_t v_op = ring_v + (uint32_t)(max(vs, 0) * (L::STAGE >> 4));
+                const uint32_t t_s = tmem + h * PF_TILE, t_o = tmem + 2 * PF_TILE + h * D;
+                constexpr int PER = PF_TILE / 32 / PF_CHUNKS;
+                auto values = [&](int c) {
+#pragma unroll
+                    for (int u = 0; u < 2 * PER; ++u) {        // 16 tokens: two groups of eight rows; a chunk's share of the first 64 tokens, then of the others
+                        const int k = c * PER + u % PER + (u / PER) * (PF_TILE / 32);
+                        pf_mma_ts(t_o, t_s + 8 * k, v_op + k * (16 * 128 >> 4), pf_idesc(D, true), !first || c > 0 || u > 0);
+                    }
+                };
+                if (vs >= 0) {
+#pragma unroll
+                    for (int c = 0; c + 1 < PF_CHUNKS; ++c) {
+                        if (!wait(&p_full[h * PF_CHUNKS + c], p_n[h] & 1)) return;
+                        pf_fence_after();
+                        if (pf_elect()) values(c);
+                        __syncwarp();
+                    }
+                    if (!wait(&p_full[h * PF_CHUNKS + PF_CHUNKS - 1], p_n[h] & 1)) return;
+                    ++p_n[h];
+                    pf_fence_after();
+                }
+                if (pf_elect()) {
+                    if (vs >= 0) {
+                        values(PF_CHUNKS - 1);
+                        if (last_v) pf_commit(&o_full[h]);
+                    }
+                    if (ks >= 0) {
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k)       // 16 columns: 32 bytes along the swizzled row of a 64-column half
+                            pf_mma_ss(t_s, q_op + (k / 4) * (PF_HALF * 128 >> 4) + (k % 4) * 2, k_op + (k / 4) * (PF_TILE * 128 >> 4) + (k % 4) * 2,
+                                      pf_idesc(PF_TILE, false), k > 0);
+                        pf_commit(&s_full[h]);
+                        if (last_k) pf_commit(&q_empty[h]);
+                    }
+                }
+                __syncwarp();
+            };
             while (ok && walk.next(it)) {
-                const int n = max(it.n[0], it.n[1]);
-                if (!n) continue;
-                for (int h = 0; h < 2 && ok; ++h) {
-                    if (!it.n[h] || !wait(&q_full[h], q_n[h]++ & 1) || !wait(&full[fill % NSTAGE], (fill / NSTAGE) & 1)) continue;
-                    scores(h, fill % NSTAGE, it.n[h] == 1);
+                const int n = max(0, it.k1 - it.k0), step = it.twin ? 2 : 1;
+                // tile j: keys in fill base + 2 j, values in the one behind it
+                const uint32_t base = fill;
+                fill += 2 * n;
+                // tile j's keys or values are there
+                auto there = [&](uint32_t f) { return wait(&full[f % NSTAGE], (f / NSTAGE) & 1); };
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t f = base + (it.twin ? 2 * h : 0);
+                    if (!it.n[h] || !wait(&q_full[h], q_n[h]++ & 1) || !there(f)) continue;
+                    turn(h, -1, f % NSTAGE, false, false, it.n[h] == 1);
+                    if (it.twin) release(f % NSTAGE);
                 }
                 if (!ok) break;
-                release(fill % NSTAGE);
-                ++fill;
+                if (n && !it.twin) release(base % NSTAGE);
                 for (int j = 0; j < n; ++j) {
-                    const int vs = fill % NSTAGE;
-                    if (!wait(&full[vs], (fill / NSTAGE) & 1)) break;
+                    const uint32_t f = base + 2 * j + 1, next = base + 2 * (j + step);
+                    const bool more = j + step < n;
+                    if (!there(f)) break;
                     if (it.k0 + j >= it.clean0) {
                         if (!wait(&cleaned[n_clean % NSTAGE], (n_clean / NSTAGE) & 1)) break;
                         ++n_clean;
                     }
-                    ++fill;
-                    const int ks = fill % NSTAGE;
+                    // (where memory is slow the next keys are not there yet: products first then)
+                    const bool ready = more && __all_sync(0xffffffffu, mbar_test(&full[next % NSTAGE], (next / NSTAGE) & 1));
+                    // half after half, so that one half's weights are worked out while the other's products run
                     for (int h = 0; h < 2 && ok; ++h) {
-                        if (j < it.n[h]) {
-                            if (!wait(&p_full[h], p_n[h]++ & 1)) break;
-                            values(h, vs, j == 0, j + 1 == it.n[h]);
-                        }
-                        if (j + 1 < it.n[h]) {
-                            if (!wait(&full[ks], (fill / NSTAGE) & 1)) break;
-                            scores(h, ks, j + 2 == it.n[h]);
-                        }
+                        if (it.twin && h != (j & 1)) continue;
+                        const int i = it.twin ? j >> 1 : j;
+                        if (i >= it.n[h]) continue;
+                        const bool goes_on = i + 1 < it.n[h];
+                        turn(h, f % NSTAGE, goes_on && ready ? (int)(next % NSTAGE) : -1, i == 0, !goes_on, i + 2 == it.n[h]);
+                        if (ok && goes_on && !ready && there(next)) turn(h, -1, next % NSTAGE, false, false, i + 2 == it.n[h]);
                     }
                     if (!ok) break;
-                    release(vs);
-                    if (j + 1 < n) {
-                        release(ks);
-                        ++fill;
-                    }
+                    release(f % NSTAGE);
+                    if (more) release(next % NSTAGE);
                 }
             }
             // what was issued has to end before tensor and shared memory are given back
@@ -575,10 +641,10 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
             // -------------------------------------------------------------- values that not every row may see
             uint32_t fill = 0, n_clean = 0;
             int item = 0;
-            const int w = warp - 10;
+            const int w = warp - PF_CLEAN;             // which half of the tile's rows
             while (ok && walk.next(it)) {
                 ++item;
-                const int n = max(it.n[0], it.n[1]);
+                const int n = max(0, it.k1 - it.k0);
                 for (int j = 0; j < n; ++j) {
                     ++fill;                            // K's
                     const int stage = fill % NSTAGE;
@@ -596,18 +662,20 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                                 uint4* const at = reinterpret_cast<uint4*>(tile + c * (PF_TILE * 128) + r * 128);
                                 if (t0 + r >= it.kv_end) {
                                     *at = make_uint4(0, 0, 0, 0);
-                                } else {
-                                    uint4 v = *at;
+                                    continue;
+                                }
+                                uint4 v = *at;
+                                // an exponent of all ones carries into the sign's place
+                                auto non_finite = [](uint32_t x) { return (x & 0x7f807f80u) + 0x00800080u; };
+                                if ((non_finite(v.x) | non_finite(v.y) | non_finite(v.z) | non_finite(v.w)) & 0x80008000u) {
                                     uint32_t* const x = reinterpret_cast<uint32_t*>(&v);
-                                    uint32_t bad = 0;
 #pragma unroll
                                     for (int u = 0; u < 4; ++u) {
-                                        const uint32_t hi = (x[u] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
-                                        const uint32_t lo = (x[u] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u;
-                                        bad |= hi | lo;
-                                        x[u] &= ~(hi | lo);
+                                        const uint32_t bad = non_finite(x[u]);
+                                        x[u] &= ~(((bad >> 31) * 0xffff0000u) | (((bad >> 15) & 1u) * 0xffffu));
                                     }
-                                    if (bad) { *at = v; found = true; }
+                                    *at = v;
+                                    found = true;
                                 }
                             }
                         if (found) s_poison[item & 15] = item;
@@ -623,17 +691,24 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
             if (!ok && lane == 0) s_dead = 1;
         }
     } else {
-        // ------------------------------------------------------------------ softmax and epilogue: a row per thread
+        // ------------------------------------------------------------------ softmax and epilogue: two threads to a row, 64 tokens of a
+        // tile and half of head_dim each
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PF_REGS_SOFTMAX));
         constexpr float LOG2E = 1.4426950408889634f;
-        const int half = warp >> 2, wrow = (warp & 3) * 32, row = wrow + lane;
-        const uint32_t lanes = (uint32_t)wrow << 16, t_s = tmem + lanes + half * PF_TILE, t_o = tmem + lanes + 2 * PF_TILE + half * D;
+        constexpr int W = PF_TILE / 2, DW = D / 2;
+        const int half = (warp >> 2) & 1, part = warp >> 3, wrow = (warp & 3) * 32, row = wrow + lane;
+        const uint32_t lanes = (uint32_t)wrow << 16;
+        const uint32_t t_s = tmem + lanes + half * PF_TILE + part * W, t_p = tmem + lanes + half * PF_TILE + part * (W / 2);
+        const uint32_t t_o = tmem + lanes + 2 * PF_TILE + half * D + part * DW;
+        const int pair = 1 + (warp & 7);               // the barrier of the two warps that share 32 rows
+        float* const tell = &s_x[part][half * PF_HALF + row];
+        const float* const told = &s_x[part ^ 1][half * PF_HALF + row];
         const float sl2 = a.scale * LOG2E, kb = a.scale * a.beta * LOG2E;
         uint32_t s_n = 0, o_n = 0;
         int item = 0;
         while (ok && walk.next(it)) {
             ++item;
-            const int tok0 = half * HT, toks = min(max(it.n_tok - tok0, 0), HT), rows = toks << a.g_shift;
+            const int tok0 = it.twin ? 0 : half * HT, rows = min(max(it.n_tok - tok0, 0), HT) << a.g_shift;
             if (!rows) continue;
             const int n = it.n[half];
             const bool live = wrow < rows;                  // a warp without rows only keeps step
@@ -650,67 +725,91 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
             float m = -INFINITY, c = -INFINITY;             // running maximum: of q.k, and in the exponents' units
             for (int j = 0; j < n; ++j) {
                 ok = __all_sync(0xffffffffu, pf_wait(&s_full[half], s_n++ & 1, &s_dead));
-                if (!ok) break;
+                if (j == 0 && !it.twin && lane == 0) mbar_arrive(&q_empty[half]);
                 if (live) {
                     pf_fence_after();
-                    float s[PF_TILE];
-#pragma unroll
-                    for (int k = 0; k < PF_TILE; k += 32) pf_ld32(t_s + k, s + k);
+                    float s[W];
+                    pf_ld32(t_s, s);
+                    pf_ld32(t_s + 32, s + 32);
                     pf_wait_ld();
-                    const int nvis = p - (it.k0 + j) * PF_TILE + 1;           // columns that the row sees
-                    const bool edge = __any_sync(0xffffffffu, nvis <= PF_TILE);
+                    const int tile = it.k0 + (it.twin ? 2 * j + half : j);
+                    const int nvis = p - tile * PF_TILE - part * W + 1;                  // columns that the row sees
+                    const bool edge = __any_sync(0xffffffffu, nvis <= W);
                     if constexpr (GATED) {
                         const int own = a.ungate ? nvis - 1 : -1;             // the column that stays raw
+                        float am[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int k = 0; k < W; k += 8)
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) am[u] = pf_max3(am[u], fabsf(s[k + u]), fabsf(s[k + u + 4]));
+                        const bool far = __any_sync(0xffffffffu, !(fmaxf(fmaxf(am[0], am[1]), fmaxf(am[2], am[3])) * sl2 < 0x1p40f));
                         auto gate = [&](auto masked) {
 #pragma unroll
-                            for (int k = 0; k < PF_TILE; k += 2) {
-                                float y0, y1;
-                                pf_fma2(y0, y1, s[k], s[k + 1], -kb, tb);
-                                const float e0 = pf_ex2(y0), e1 = pf_ex2(y1);
-                                // both reciprocals from one of the product; far below the threshold the gate is 0
-                                const float d0 = fminf(1.f + e0, 0x1p62f), d1 = fminf(1.f + e1, 0x1p62f);
-                                const float rr = pf_rcp(d0 * d1);
-                                const float g0 = e0 > 0x1p60f ? 0.f : rr * d1, g1 = e1 > 0x1p60f ? 0.f : rr * d0;
-                                float x0, x1;
-                                pf_fma2(x0, x1, s[k], s[k + 1], sl2, 0.f);
-                                if (decltype(masked)::value) {
-                                    s[k] = k < nvis ? (k == own ? x0 : x0 * g0) : -INFINITY;
-                                    s[k + 1] = k + 1 < nvis ? (k + 1 == own ? x1 : x1 * g1) : -INFINITY;
-                                } else {
-                                    s[k] = x0 * g0; s[k + 1] = x1 * g1;
+                            for (int k0 = 0; k0 < W; k0 += 8) {           // stage by stage, so that 8 / 2 chains run side by side
+                                float x[8], e[8], g[8];
+#pragma unroll
+                                for (int k = 0; k < 8; k += 2) pf_fma2(e[k], e[k + 1], s[k0 + k], s[k0 + k + 1], -kb, tb);
+                                // Both reciprocals of a pair from the one of their product.  So that it stays finite a gate is no smaller than 2^-62:
+                                // a score below 2^40 then counts as 0 all the same.
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) e[k] = pf_ex2(fminf(e[k], 62.f));
+#pragma unroll
+                                for (int k = 0; k < 8; k += 2) { add2(e[k], e[k + 1], 1.f, 1.f); mul2(x[k], x[k + 1], s[k0 + k], s[k0 + k + 1], sl2, sl2); }
+#pragma unroll
+                                for (int k = 0; k < 8; k += 2) g[k] = pf_rcp(e[k] * e[k + 1]);
+#pragma unroll
+                                for (int k = 0; k < 8; k += 2) mul2(e[k + 1], e[k], x[k], x[k + 1], e[k + 1], e[k]);
+#pragma unroll
+                                for (int k = 0; k < 8; k += 2) {
+                                    mul2(s[k0 + k], s[k0 + k + 1], e[k + 1], e[k], g[k], g[k]);
+                                    if (decltype(masked)::value) {
+                                        s[k0 + k] = k0 + k < nvis ? (k0 + k == own ? x[k] : s[k0 + k]) : -INFINITY;
+                                        s[k0 + k + 1] = k0 + k + 1 < nvis ? (k0 + k + 1 == own ? x[k + 1] : s[k0 + k + 1]) : -INFINITY;
+                                    }
                                 }
                             }
                         };
+                        if (far) {
+#pragma unroll
+                            for (int k = 0; k < W; ++k) {
+                                const float x = s[k] * sl2, g = pf_rcp(1.f + pf_ex2(fmaf(s[k], -kb, tb)));
+                                s[k] = k < nvis ? (k == own ? x : x * g) : -INFINITY;
+                            }
+                        } else
                         if (edge) gate(std::true_type{});
                         else gate(std::false_type{});
                     } else if (edge) {
 #pragma unroll
-                        for (int k = 0; k < PF_TILE; ++k) s[k] = k < nvis ? s[k] : -INFINITY;
+                        for (int k = 0; k < W; ++k) s[k] = k < nvis ? s[k] : -INFINITY;
                     }
-                    float x[8];
+                    float x[4];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) x[k] = fmaxf(s[k], s[k + 8]);
+                    for (int k = 0; k < 4; ++k) x[k] = pf_max3(s[k], s[k + 4], s[k + 8]);
 #pragma unroll
-                    for (int k = 16; k < PF_TILE; k += 16)
+                    for (int k = 12; k + 8 <= W; k += 8)
 #pragma unroll
-                        for (int u = 0; u < 8; ++u) x[u] = fmaxf(fmaxf(x[u], s[k + u]), s[k + u + 8]);
-                    const float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-                    const float cx = GATED ? mx : mx * sl2;
-                    if (__any_sync(0xffffffffu, cx > c + PF_SLACK)) {
-                        const float c_new = fmaxf(c, cx);
+                        for (int u = 0; u < 4; ++u) x[u] = pf_max3(x[u], s[k + u], s[k + u + 4]);
+                    float mx = pf_max3(pf_max3(x[0], x[1], x[2]), x[3], pf_max3(s[W - 4], s[W - 3], fmaxf(s[W - 2], s[W - 1])));
+                    // Both threads have their scores when they meet here: weights may overwrite them.  A warp whose wait ran out comes here
+                    // too, so that no meeting is left waiting for it.
+                    if (pf_any_of<2>(!ok || (GATED ? mx : mx * sl2) > c + PF_SLACK, pair)) {
+                        *tell = mx;
+                        if (pf_any_of<2>(!ok, pair)) { ok = false; break; }
+                        mx = fmaxf(mx, *told);
+                        const float c_new = fmaxf(c, GATED ? mx : mx * sl2);
                         const float alpha = c == c_new ? 1.f : pf_ex2(c - c_new);
                         m = fmaxf(m, mx);
                         c = c_new;
                         l0 *= alpha; l1 *= alpha; l2 *= alpha; l3 *= alpha;
                         if (j) {                       // these scores are complete, so is the product before them
 #pragma unroll 1
-                            for (int k = 0; k < D; k += 32) {
-                                float o[32];
-                                pf_ld32(t_o + k, o);
+                            for (int k = 0; k < DW; k += 16) {
+                                float o[16];
+                                pf_ld16(t_o + k, o);
                                 pf_wait_ld();
 #pragma unroll
-                                for (int u = 0; u < 32; ++u) o[u] *= alpha;
-                                pf_st32(t_o + k, reinterpret_cast<const uint32_t*>(o));
+                                for (int u = 0; u < 16; ++u) o[u] *= alpha;
+                                pf_st16(t_o + k, reinterpret_cast<const uint32_t*>(o));
                             }
                         }
                     }
@@ -718,66 +817,112 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                     // q.k scale - maximum in one rounding, off by the rounding of the maximum's product: the same factor for the whole
                     // row, which cancels.  Where that could be a large one the difference is formed first.
                     const bool huge = !GATED && fabsf(cu) > 4194304.f;
-                    const float mu = m == -INFINITY ? 0.f : m;
+                    float mul = GATED ? 1.f : sl2, sub = -cu;
                     if (!GATED && __any_sync(0xffffffffu, huge)) {
+                        const float mu = m == -INFINITY ? 0.f : m;
 #pragma unroll
-                        for (int k = 0; k < PF_TILE; ++k) s[k] = huge ? (s[k] - mu) * sl2 : fmaf(s[k], sl2, -cu);
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < PF_TILE; k += 2) pf_fma2(s[k], s[k + 1], s[k], s[k + 1], GATED ? 1.f : sl2, -cu);
+                        for (int k = 0; k < W; ++k) s[k] = huge ? (s[k] - mu) * sl2 : fmaf(s[k], sl2, sub);
+                        mul = 1.f; sub = 0.f;
                     }
+                    // a chunk's weights are on their way to tensor memory while the next chunk's are worked out
+                    auto hand_over = [&](int chunk) {
+                        pf_wait_st();
+                        pf_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&p_full[half * PF_CHUNKS + chunk]);
+                    };
 #pragma unroll
-                    for (int k = 0; k < PF_TILE; k += 64) {
-                        uint32_t w[32];
+                    for (int k0 = 0; k0 < W; k0 += W / PF_CHUNKS) {
+                        uint32_t w[W / PF_CHUNKS / 2];
 #pragma unroll
-                        for (int u = 0; u < 32; u += 2) {
-                            const float p0 = pf_ex2(s[k + 2 * u]), p1 = pf_ex2(s[k + 2 * u + 1]), p2 = pf_ex2(s[k + 2 * u + 2]), p3 = pf_ex2(s[k + 2 * u + 3]);
-                            add2(l0, l1, p0, p1);
-                            add2(l2, l3, p2, p3);
-                            w[u] = pf_pack(p0, p1);
-                            w[u + 1] = pf_pack(p2, p3);
+                        for (int q0 = 0; q0 < W / PF_CHUNKS; q0 += 8) {
+                            float p[8];
+#pragma unroll
+                            for (int k = 0; k < 8; k += 2) pf_fma2(p[k], p[k + 1], s[k0 + q0 + k], s[k0 + q0 + k + 1], mul, sub);
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) p[k] = pf_ex2(p[k]);
+#pragma unroll
+                            for (int k = 0; k < 8; k += 2) {
+                                if (k & 2) add2(l2, l3, p[k], p[k + 1]);
+                                else add2(l0, l1, p[k], p[k + 1]);
+                                w[(q0 + k) / 2] = pf_pack(p[k], p[k + 1]);
+                            }
                         }
-                        pf_st32(t_s + k / 2, w);
+                        if (k0) hand_over(k0 / (W / PF_CHUNKS) - 1);
+                        pf_st16(t_p + k0 / 2, w);
                     }
-                    pf_wait_st();
-                    pf_fence_before();
+                    hand_over(PF_CHUNKS - 1);
+                } else {
+                    if (!ok) break;
+                    if (lane == 0)
+                        for (int k = 0; k < PF_CHUNKS; ++k) mbar_arrive(&p_full[half * PF_CHUNKS + k]);
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[half]);
+            }
+            if (!ok && !(live && it.twin)) break;
+            if (ok && n) ok = __all_sync(0xffffffffu, pf_wait(&o_full[half], o_n++ & 1, &s_dead));
+            pf_fence_after();
+            const bool mine = row < rows, split = it.slot >= 0;
+            const int64_t at_part = ((int64_t)it.slot * PF_ROWS + (it.twin ? 0 : half * PF_HALF) + row);
+            // In a twin item both halves have the row: the second hands over what it has, through the queries' place (a column's rows side by side).
+            float* const hand = reinterpret_cast<float*>(smem) + part * DW * PF_HALF + row;
+            float l = (l0 + l1) + (l2 + l3), keep = 1.f, take = 0.f;               // what either half's sums count
+            if (live) {
+                *tell = l;
+                if (pf_any_of<2>(!ok, pair)) ok = false;
+                l = part ? *told + l : l + *told;
+                if (it.twin) {
+                    if (half && ok) {
+#pragma unroll 1
+                        for (int k = 0; k < DW; k += 16) {
+                            float o[16];
+                            pf_ld16(t_o + k, o);
+                            pf_wait_ld();
+#pragma unroll
+                            for (int u = 0; u < 16; ++u) hand[(k + u) * PF_HALF] = o[u];
+                        }
+                        if (!part) s_twin[row] = make_float2(c, l);
+                        pf_fence_before();
+                        fence_proxy_async();
+                    }
+                    if (pf_any_of<4>(!ok, 9 + (warp & 3))) ok = false;
+                    if (!half) {
+                        const float2 ml = s_twin[row];
+                        const float M = fmaxf(c, ml.x);
+                        if (M != -INFINITY) { keep = pf_ex2(c - M); take = pf_ex2(ml.x - M); }
+                        l = l * keep + ml.y * take;
+                        c = M;
+                    }
+                }
             }
             if (!ok) break;
-            if (n) {
-                ok = __all_sync(0xffffffffu, pf_wait(&o_full[half], o_n++ & 1, &s_dead));
-                if (!ok) break;
-            }
-            if (!live) continue;
-            pf_fence_after();
-            const float l = (l0 + l1) + (l2 + l3);
-            const bool mine = row < rows, split = it.slot >= 0;
             const bool poison = n && s_poison[item & 15] == item;
-            const int64_t part = ((int64_t)it.slot * PF_ROWS + half * PF_HALF + row);
-            if (split && mine) a.part_ml[part] = make_float2(c, l);
+            if (split && live && mine && !part && !(it.twin && half)) a.part_ml[at_part] = make_float2(c, l);
             const float inv = split ? 1.f : (l == 0.f ? 0.f : 1.f / l);
-            __nv_bfloat16* const to = a.out + ((int64_t)(it.row0 + tok) * a.Hq + h) * D;
+            keep *= inv; take *= inv;
+            const int64_t to = ((int64_t)(it.row0 + tok) * a.Hq + h) * D + part * DW;
 #pragma unroll 1
-            for (int k = 0; k < D; k += 32) {
+            for (int k = 0; k < (live && !(it.twin && half) ? DW : 0); k += 32) {
                 float o[32];
                 if (n) {
                     pf_ld32(t_o + k, o);
                     pf_wait_ld();
 #pragma unroll
-                    for (int u = 0; u < 32; ++u) o[u] *= inv;
+                    for (int u = 0; u < 32; ++u) o[u] *= keep;
+                    if (it.twin) {
+#pragma unroll
+                        for (int u = 0; u < 32; ++u) o[u] = fmaf(hand[(k + u) * PF_HALF], take, o[u]);
+                    }
                 } else {
 #pragma unroll
                     for (int u = 0; u < 32; ++u) o[u] = 0.f;
                 }
                 if (poison) {
-                    const int end = (int)min((int64_t)p + 1, (int64_t)(it.k0 + n) * PF_TILE);
+                    const int end = (int)min((int64_t)p + 1, (int64_t)it.k1 * PF_TILE);
                     for (int t = max(it.clean0, it.k0) * PF_TILE; t < end; ++t) {
                         const int64_t base = a.block_table
                             ? (int64_t)__ldcg(a.block_table + (int64_t)it.seq * a.table_stride + (t >> a.b_shift)) * a.v_sb + (int64_t)(t & ((1 << a.b_shift) - 1)) * a.v_st
                             : (int64_t)it.seq * a.v_sb + (int64_t)t * a.v_st;
-                        const uint4* const from = reinterpret_cast<const uint4*>(a.V + base + it.hk * a.v_sh + k);
+                        const uint4* const from = reinterpret_cast<const uint4*>(a.V + base + it.hk * a.v_sh + part * DW + k);
 #pragma unroll
                         for (int u = 0; u < 4; ++u) {
                             const uint4 v = __ldcg(from + u);
@@ -793,11 +938,11 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                 }
                 if (!mine) continue;
                 if (split) {
-                    float4* const at = reinterpret_cast<float4*>(a.part_o + part * D + k);
+                    float4* const at = reinterpret_cast<float4*>(a.part_o + at_part * D + part * DW + k);
 #pragma unroll
                     for (int u = 0; u < 8; ++u) at[u] = make_float4(o[4 * u], o[4 * u + 1], o[4 * u + 2], o[4 * u + 3]);
                 } else {
-                    uint4* const at = reinterpret_cast<uint4*>(to + k);
+                    uint4* const at = reinterpret_cast<uint4*>(a.out + to + k);
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
                         at[u] = make_uint4(pf_pack(o[8 * u], o[8 * u + 1]), pf_pack(o[8 * u + 2], o[8 * u + 3]), pf_pack(o[8 * u + 4], o[8 * u + 5]),
@@ -805,13 +950,18 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                 }
             }
             pf_fence_before();
+            if (it.twin && !half) {                        // all is read: the next item's queries may come
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) { mbar_arrive(&q_empty[0]); mbar_arrive(&q_empty[1]); }
+            }
         }
         if (!ok && lane == 0) s_dead = 1;
         pdl_trigger();
     }
     pf_fence_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == PF_MMA) {
         pf_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }
@@ -893,6 +1043,8 @@ static int pf_launch(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUten
     if (attr.numRegs < PF_REGS) return ETA_ERR_UNSUPPORTED;
     const int rc = launch_pdl("eta_prefill", prefill_kernel<D, GATED>, dim3(ctas), dim3(PF_THREADS), PfSmem<D>::BYTES, s, tmQ, tmK, tmV, a);
     if (rc != ETA_OK) return rc;
+    // (no item of at most so many tiles is ever split: see PfWalk)
+    if (a.t_cap <= PF_TILE * PF_SPLIT_COST) return ETA_OK;
     return launch_pdl("eta_prefill", prefill_join_kernel<D>, dim3(ctas, PF_ROWS / PF_JOIN_ROWS), dim3(32 * PF_JOIN_WARPS), 0, s, a);
 }
 
@@ -917,13 +1069,13 @@ int eta_selftest_prefill_shares(int batch, int n_kv_heads, int g_shift, int head
         rows += n[i];
         tab.items[i + 1] = tab.items[i] + ti.nq * n_kv_heads;
         tab.cost[i + 1] = tab.cost[i] + n_kv_heads * ti.cost_before(ti.nq);
-        if (n[i] && ti.tiles(ti.nq - 1) > tab.longest) tab.longest = ti.tiles(ti.nq - 1);
         int64_t sum = 0;
         for (int t = 0; t < ti.nq; ++t) {
-            if (ti.before(t) != sum) return 1;
-            sum += ti.tiles(t);
+            if (ti.cost_before(t) != sum) return 1;
+            tab.longest = std::max(tab.longest, ti.tiles(t));
+            sum += ti.tiles(t) + PF_ITEM_COST;
         }
-        if (ti.before(ti.nq) != sum) return 2;
+        if (ti.cost_before(ti.nq) != sum) return 2;
     }
     // per item: next tile expected, parts seen, parts announced
     struct Seen { int next = 0, parts = 0, said = 0, last = -2; };
@@ -938,9 +1090,10 @@ int eta_selftest_prefill_shares(int batch, int n_kv_heads, int g_shift, int head
             const int tok = it.row0 - tab.row0[it.seq];
             if (tok < 0 || tok % m || tok + it.n_tok > n[it.seq] || it.p0 != len[it.seq] - n[it.seq] + tok) return 4;
             Seen& s = seen[(size_t)it.row0 * n_kv_heads + it.hk];
-            const int all = it.p0 + it.n_tok > 0 ? (it.p0 + it.n_tok - 1) / PF_TILE + 1 : 0;
+            const int all = it.p0 + it.n_tok > 0 ? (it.p0 + it.n_tok - 1) / PF_TILE + 1 : 0, got = std::max(0, it.k1 - it.k0);
+            if (it.twin ? it.n[0] + it.n[1] != got || 2 * it.n_tok > m : (2 * it.n_tok > m ? it.n[1] : it.n[0]) != got) return 11;
             if (it.slot < 0) {
-                if (s.parts || it.k0 != 0 || std::max(it.n[0], it.n[1]) != all) return 5;
+                if (s.parts || it.k0 != 0 || got != all) return 5;
                 s.parts = s.said = 1; s.next = all;
                 continue;
             }
@@ -953,7 +1106,7 @@ int eta_selftest_prefill_shares(int batch, int n_kv_heads, int g_shift, int head
             }
             // (a gap is allowed only behind the tiles that count: positions before the sequence's first token)
             if (it.k0 > s.next && s.next < all) return 9;
-            if (it.n[0] || it.n[1]) s.next = it.k0 + std::max(it.n[0], it.n[1]);
+            if (got) s.next = it.k1;
             s.last = c;
             ++s.parts;
         }
