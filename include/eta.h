@@ -471,6 +471,70 @@ int eta_prefill(const eta_cache_desc* desc, const eta_page_table* pages, const e
                 const int32_t* row_start, const int32_t* seq_lens, const int32_t* granted, const void* K, const void* V, const float* tau,
                 const float* head_const, void* out, uint32_t* status_dev, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Pages that several sequences hold (deployment plumbing for the paged cache, beside eta_plan_pages; the paper has no counterpart).  A
+ * page that n sequences hold has shared[page] = n - 1 (int32 [n_pages], 0 for a page of one sequence or of none, negative numbers count as 0; eta_plan_pages hands
+ * out and takes back pages of one sequence and does not look at it: sequences that share pages are let go with eta_free_pages).  Only
+ * full pages are shared: nothing writes to them again, so forks go on with eta_plan_pages and eta_append_tokens like any sequence.
+ * Tables, lengths, free stack and n_pages as in eta_plan_pages; every ..._out may be the array that is read.  Of a table's row the first
+ * ceil(t_cap / block_size) entries are looked at.  All calls are on device memory, allocate nothing, are deterministic, and are launched
+ * with programmatic dependent launch: they wait for everything before them in the stream before they read or write, and release their
+ * successors as they end.  Calls that share a stack, a table, counts or a workspace must not overlap.
+ *
+ * eta_fork_pages: sequence i with parent[i] = u >= 0 becomes a copy of sequence u's first T tokens, T = seq_lens[u], at most take[i] where
+ * take is given (nullable).  Its place has to be empty (seq_lens[i] <= 0), and u a sequence that is not itself a child in this call.
+ *   - the floor(T / block_size) full pages: block_table[i][j] = block_table[u][j], and shared goes up by one;
+ *   - a partly filled last page: a page of its own off the top of the stack, sequence after sequence; copy_src[i] and copy_dst[i] say which
+ *     page is to be copied where (eta_copy_pages with max_moves = batch; for every layer's pools), -1 for sequences that copy none.
+ * granted[i] = T, and the child's length (seq_lens_out[i]) with it; a child that could not be served (not an empty place, no such parent,
+ * no page left) gets granted[i] = 0, shares nothing, keeps its length, and ETA_DEV_REFUSED is set.  batch <= 1024.
+ *
+ * eta_fork_summaries: the block summaries of the children: the records of the granted[i] / block_size full blocks of every KV head, from the parent's
+ * rows of musig and mnorm to the child's (flags: ETA_BUILD_PACKED_SIGMA or 0).  After eta_fork_pages, for every layer.  Of the descriptor the
+ * strides and t_cap are not looked at; unlike a step's, batch * n_kv_heads is not limited.
+ *
+ * eta_free_pages: every sequence with release[i] != 0 lets go of its pages, and its length becomes 0.  A page that nobody holds any more goes onto the
+ * stack, lowest number first; of the others shared goes down.  ETA_DEV_REFUSED: a page number outside the pool (skipped), more
+ * releases of a page than it has holders (it goes back once), or a stack that would overflow.
+ *
+ * eta_compact_pages: with L pages in use, the k-th page in use from L up goes to the k-th free page below L: move_src[k], move_dst[k] (room
+ * for n_pages each), *n_moves of them; entries behind those are left as they are.  Tables of all sequences (block_table_out), counts and
+ * stack (free_pages_out: n_pages - 1, n_pages - 2, .. L, so that the lowest comes off first; entries behind *n_free_out stay) are those
+ * after the move; eta_copy_pages with n_moves does the copies, for every layer's pools.  A page is in use if the stack
+ * does not hold it, in a table or not: whoever keeps pages of his own finds them in the list.  ETA_DEV_REFUSED: a stack that holds a
+ * page twice or a number outside the pool, a table that holds such or a free one.
+ *
+ * eta_copy_pages: page src[k] of every pool to page dst[k], for k < max_moves or, where n_moves (device, nullable) is given, k < *n_moves.  Pairs
+ * with a negative number are skipped; one past n_pages is skipped and sets ETA_DEV_BAD_SLOT.  No destination may be another
+ * pair's source or destination.  A pool's page is n_pieces runs of piece_bytes, piece_stride apart (1 run where a page is contiguous), all
+ * multiples of 16 bytes, as is base; at most 64 pools a call.  The pools array is host memory read during the call.
+ *
+ * workspace: eta_pages_workspace_bytes() bytes, 256-byte aligned, no initialisation needed.
+ */
+typedef struct eta_page_pool {
+    void* base;
+    int64_t page_stride, piece_stride, piece_bytes;
+    int32_t n_pieces;
+} eta_page_pool;
+
+int eta_pages_workspace_bytes(int32_t n_pages, size_t* out_bytes);
+int eta_fork_pages(int32_t batch, int32_t block_size, int32_t t_cap, const int32_t* parent, const int32_t* take, const int32_t* seq_lens,
+                   int32_t* seq_lens_out, int32_t* block_table, int32_t table_stride, const int32_t* shared, int32_t* shared_out,
+                   const int32_t* free_pages, const int32_t* n_free, int32_t* n_free_out, int32_t n_pages, int32_t* copy_src, int32_t* copy_dst,
+                   int32_t* granted, uint32_t* status_dev, void* stream);
+int eta_fork_summaries(const eta_cache_desc* desc, const int32_t* parent, const int32_t* granted, void* musig, float* mnorm, uint32_t flags,
+                       uint32_t* status_dev, void* stream);
+int eta_free_pages(int32_t batch, int32_t block_size, int32_t t_cap, const int32_t* release, const int32_t* seq_lens, int32_t* seq_lens_out,
+                   const int32_t* block_table, int32_t table_stride, const int32_t* shared, int32_t* shared_out, int32_t* free_pages,
+                   const int32_t* n_free, int32_t* n_free_out, int32_t n_pages, uint32_t* status_dev, void* workspace, size_t workspace_bytes,
+                   void* stream);
+int eta_compact_pages(int32_t batch, int32_t block_size, int32_t t_cap, const int32_t* seq_lens, const int32_t* block_table,
+                      int32_t* block_table_out, int32_t table_stride, const int32_t* shared, int32_t* shared_out, const int32_t* free_pages,
+                      int32_t* free_pages_out, const int32_t* n_free, int32_t* n_free_out, int32_t n_pages, int32_t* move_src, int32_t* move_dst,
+                      int32_t* n_moves, uint32_t* status_dev, void* workspace, size_t workspace_bytes, void* stream);
+int eta_copy_pages(const eta_page_pool* pools, int32_t n_pools, int32_t n_pages, const int32_t* src, const int32_t* dst, int32_t max_moves,
+                   const int32_t* n_moves, uint32_t* status_dev, void* stream);
+
 /* Size of the built-in scratch of eta_decode_static, in bytes. */
 size_t eta_static_scratch_bytes(void);
 

@@ -33,7 +33,8 @@ EXPORTS = ("eta_workspace_bytes", "eta_build_block_summaries", "eta_append_summa
            "eta_profile_kernel_name", "eta_set_pdl", "eta_strerror", "eta_last_cuda_error", "eta_plan_pages",
            "eta_append_tokens", "eta_append_tokens_kv4", "eta_kv4_block_bytes", "eta_unpack_kv4",
            "eta_build_block_summaries_kv4", "eta_append_summary_kv4", "eta_decode_kv4", "eta_kv4_workspace_bytes",
-           "eta_prefill", "eta_prefill_workspace_bytes")
+           "eta_prefill", "eta_prefill_workspace_bytes", "eta_fork_pages", "eta_fork_summaries", "eta_free_pages", "eta_compact_pages",
+           "eta_copy_pages", "eta_pages_workspace_bytes")
 
 
 class CacheDesc(ctypes.Structure):
@@ -64,6 +65,11 @@ class TokensDesc(ctypes.Structure):
                 ("k_stride_h", ctypes.c_int64), ("v_stride_r", ctypes.c_int64), ("v_stride_h", ctypes.c_int64), ("eps", ctypes.c_float)]
 
 
+class PagePool(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("piece_stride", ctypes.c_int64), ("piece_bytes", ctypes.c_int64),
+                ("n_pieces", ctypes.c_int32)]
+
+
 class EtaError(RuntimeError):
     pass
 
@@ -72,7 +78,8 @@ _lib = None
 _native = None          # the compiled marshalling module, or what stands for it where it is missing
 _STEP_CALLS = ("eta_append_summary", "eta_append_summary_paged", "eta_predict_threshold", "eta_decode", "eta_decode_paged",
                "eta_decode_static", "eta_plan_pages", "eta_append_tokens", "eta_append_tokens_kv4", "eta_unpack_kv4",
-               "eta_build_block_summaries_kv4", "eta_append_summary_kv4", "eta_decode_kv4", "eta_prefill")
+               "eta_build_block_summaries_kv4", "eta_append_summary_kv4", "eta_decode_kv4", "eta_prefill", "eta_fork_pages", "eta_fork_summaries", "eta_free_pages",
+               "eta_compact_pages", "eta_copy_pages")
 
 
 class _Missing:
@@ -139,6 +146,13 @@ def load(path: str | None = None) -> ctypes.CDLL:
         lib.eta_kv4_block_bytes.restype = ctypes.c_size_t
         lib.eta_prefill_workspace_bytes.argtypes = [D, ctypes.POINTER(ctypes.c_size_t)]
         lib.eta_prefill.argtypes = [D, PT, P, i32, vp, i32p, i32p, i32p, vp, vp, f32p, f32p, vp, vp, vp, ctypes.c_size_t, vp]
+        lib.eta_pages_workspace_bytes.argtypes = [i32, ctypes.POINTER(ctypes.c_size_t)]
+        lib.eta_fork_pages.argtypes = [i32, i32, i32, i32p, i32p, i32p, i32p, i32p, i32, i32p, i32p, i32p, i32p, i32p, i32, i32p, i32p, i32p, vp, vp]
+        lib.eta_fork_summaries.argtypes = [D, i32p, i32p, vp, f32p, ctypes.c_uint32, vp, vp]
+        lib.eta_free_pages.argtypes = [i32, i32, i32, i32p, i32p, i32p, i32p, i32, i32p, i32p, i32p, i32p, i32p, i32, vp, vp, ctypes.c_size_t, vp]
+        lib.eta_compact_pages.argtypes = [i32, i32, i32, i32p, i32p, i32p, i32, i32p, i32p, i32p, i32p, i32p, i32p, i32, i32p, i32p, i32p, vp, vp,
+                                          ctypes.c_size_t, vp]
+        lib.eta_copy_pages.argtypes = [ctypes.POINTER(PagePool), i32, i32, i32p, i32p, i32, i32p, vp, vp]
         lib.eta_decode_static.argtypes = [D, P, vp, vp, vp, i32p, vp, f32p, f32p, f32p, f32p, vp, i32p, vp, vp]
         lib.eta_static_scratch_bytes.restype = ctypes.c_size_t
         lib.eta_decode_kernel_count.restype = ctypes.c_int
@@ -482,6 +496,65 @@ def eta_prefill(desc: CacheDesc, params: DecodeParams, q, K, V, row_start, seq_l
                          status, workspace)
     if rc:
         _check(rc, "eta_prefill")
+
+
+def eta_pages_workspace_bytes(n_pages: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().eta_pages_workspace_bytes(n_pages, ctypes.byref(n)), "eta_pages_workspace_bytes")
+    return n.value
+
+
+def eta_fork_pages(block_size: int, t_cap: int, parent, seq_lens, block_table, shared, free_pages, n_free, copy_src, copy_dst, granted, take=None,
+                   seq_lens_out=None, shared_out=None, n_free_out=None, status=None) -> None:
+    """Sequences that begin as copies of others (see include/eta.h): full pages are shared, copy_src and copy_dst name the last, partly
+    filled ones for eta_copy_pages.  int32 CUDA tensors on the current device; lengths, counts and the free count are updated in place unless
+    outputs are given."""
+    lib = _lib or load()
+    rc = _native.fork_pages(lib.addresses["eta_fork_pages"], block_size, t_cap, parent, take, seq_lens,
+                            seq_lens if seq_lens_out is None else seq_lens_out, block_table, shared, shared if shared_out is None else shared_out,
+                            free_pages, n_free, n_free if n_free_out is None else n_free_out, copy_src, copy_dst, granted, status)
+    if rc:
+        _check(rc, "eta_fork_pages")
+
+
+def eta_fork_summaries(desc: CacheDesc, parent, granted, musig, mnorm, status=None) -> None:
+    """The forks' block summaries, from their parents' rows to theirs; the layout of the records goes by musig's type."""
+    lib = _lib or load()
+    rc = _native.fork_summaries(lib.addresses["eta_fork_summaries"], desc, parent, granted, musig, mnorm, status)
+    if rc:
+        _check(rc, "eta_fork_summaries")
+
+
+def eta_free_pages(block_size: int, t_cap: int, release, seq_lens, block_table, shared, free_pages, n_free, workspace, seq_lens_out=None,
+                   shared_out=None, n_free_out=None, status=None) -> None:
+    """Finished sequences let go of their pages; those that nobody else holds go back to the free stack."""
+    lib = _lib or load()
+    rc = _native.free_pages(lib.addresses["eta_free_pages"], block_size, t_cap, release, seq_lens, seq_lens if seq_lens_out is None else seq_lens_out,
+                            block_table, shared, shared if shared_out is None else shared_out, free_pages, n_free,
+                            n_free if n_free_out is None else n_free_out, status, workspace)
+    if rc:
+        _check(rc, "eta_free_pages")
+
+
+def eta_compact_pages(block_size: int, t_cap: int, seq_lens, block_table, shared, free_pages, n_free, move_src, move_dst, n_moves, workspace,
+                      block_table_out=None, shared_out=None, free_pages_out=None, n_free_out=None, status=None) -> None:
+    """Pages in use move to the low end of the pool: tables, counts and stack after the move, and the list of copies for eta_copy_pages."""
+    lib = _lib or load()
+    rc = _native.compact_pages(lib.addresses["eta_compact_pages"], block_size, t_cap, seq_lens, block_table,
+                               block_table if block_table_out is None else block_table_out, shared, shared if shared_out is None else shared_out,
+                               free_pages, free_pages if free_pages_out is None else free_pages_out, n_free,
+                               n_free if n_free_out is None else n_free_out, move_src, move_dst, n_moves, status, workspace)
+    if rc:
+        _check(rc, "eta_compact_pages")
+
+
+def eta_copy_pages(pools, src, dst, n_moves=None, status=None) -> None:
+    """Page src[k] of every pool (a tensor [pages, ...] of any type whose pages are contiguous but for one axis) to page dst[k]; n_moves: an int32 CUDA
+    tensor that says how many pairs count (None: all).  Negative numbers are skipped."""
+    lib = _lib or load()
+    rc = _native.copy_pages(lib.addresses["eta_copy_pages"], pools, src, dst, n_moves, status)
+    if rc:
+        _check(rc, "eta_copy_pages")
 
 
 def eta_static_scratch_bytes() -> int:

@@ -583,6 +583,204 @@ PyObject* prefill(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return PyLong_FromLong(rc);
 }
 
+// A block table [batch, pages of a sequence] of int32 on the current device, wide enough for t_cap tokens; its rows' stride
+bool table_of(PyObject* o, const char* name, int64_t batch, int32_t block_size, int32_t t_cap, int32_t** out, int64_t* stride) {
+    if (!shaped(o, at::kInt, name, {batch, -1}, (void**)out)) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (batch > 1 && t.stride(0) < t.size(1)) return fail(name, "a tensor whose rows do not overlap");
+    if (t.size(1) * (int64_t)block_size < t_cap) return fail(name, "wide enough for t_cap tokens");
+    *stride = batch > 1 ? t.stride(0) : t.size(1);
+    if (batch > INT32_MAX || *stride > INT32_MAX) return fail(name, "of fewer than 2^31 entries a row");
+    return true;
+}
+
+// (address, block_size, t_cap, parent, take, seq_lens, seq_lens_out, block_table, shared, shared_out, free_pages, n_free, n_free_out, copy_src,
+//  copy_dst, granted, status) -> return code
+PyObject* fork_pages(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    using F = int (*)(int32_t, int32_t, int32_t, const int32_t*, const int32_t*, const int32_t*, int32_t*, int32_t*, int32_t, const int32_t*,
+                      int32_t*, const int32_t*, const int32_t*, int32_t*, int32_t, int32_t*, int32_t*, int32_t*, uint32_t*, void*);
+    F fn;
+    int32_t block_size, t_cap, *parent, *take, *seq_lens, *seq_lens_out, *block_table, *shared, *shared_out, *free_pages, *n_free, *n_free_out,
+        *copy_src, *copy_dst, *granted;
+    uint32_t* status;
+    int64_t stride;
+    if (!count(n, 17) || !entry(v[0], &fn) || !int32_of(v[1], &block_size) || !int32_of(v[2], &t_cap) || !VEC(v[3], at::kInt, parent, -1)) return nullptr;
+    const int64_t batch = THPVariable_Unpack(v[3]).numel();
+    if (!OPT(v[4], at::kInt, take, batch) || !VEC(v[5], at::kInt, seq_lens, batch) || !VEC(v[6], at::kInt, seq_lens_out, batch) ||
+        !table_of(v[7], "block_table", batch, block_size, t_cap, &block_table, &stride) || !VEC(v[8], at::kInt, shared, -1))
+        return nullptr;
+    const int64_t pages = THPVariable_Unpack(v[8]).numel();
+    if (pages > INT32_MAX) return fail("shared", "of fewer than 2^31 pages"), nullptr;
+    if (!VEC(v[9], at::kInt, shared_out, pages) || !VEC(v[10], at::kInt, free_pages, pages) || !VEC(v[11], at::kInt, n_free, 1) ||
+        !VEC(v[12], at::kInt, n_free_out, 1) || !VEC(v[13], at::kInt, copy_src, batch) || !VEC(v[14], at::kInt, copy_dst, batch) ||
+        !VEC(v[15], at::kInt, granted, batch) || !OPT(v[16], at::kInt, status, 1))
+        return nullptr;
+    void* const s = stream();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn((int32_t)batch, block_size, t_cap, parent, take, seq_lens, seq_lens_out, block_table, (int32_t)stride, shared, shared_out, free_pages,
+            n_free, n_free_out, (int32_t)pages, copy_src, copy_dst, granted, status, s);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+// (address, block_size, t_cap, release, seq_lens, seq_lens_out, block_table, shared, shared_out, free_pages, n_free, n_free_out, status, workspace)
+// -> return code
+PyObject* free_pages_(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    using F = int (*)(int32_t, int32_t, int32_t, const int32_t*, const int32_t*, int32_t*, const int32_t*, int32_t, const int32_t*, int32_t*,
+                      int32_t*, const int32_t*, int32_t*, int32_t, uint32_t*, void*, size_t, void*);
+    F fn;
+    int32_t block_size, t_cap, *release, *seq_lens, *seq_lens_out, *block_table, *shared, *shared_out, *free_pages, *n_free, *n_free_out;
+    uint32_t* status;
+    void* workspace;
+    int64_t stride;
+    if (!count(n, 14) || !entry(v[0], &fn) || !int32_of(v[1], &block_size) || !int32_of(v[2], &t_cap) || !VEC(v[3], at::kInt, release, -1)) return nullptr;
+    const int64_t batch = THPVariable_Unpack(v[3]).numel();
+    if (!VEC(v[4], at::kInt, seq_lens, batch) || !VEC(v[5], at::kInt, seq_lens_out, batch) ||
+        !table_of(v[6], "block_table", batch, block_size, t_cap, &block_table, &stride) || !VEC(v[7], at::kInt, shared, -1))
+        return nullptr;
+    const int64_t pages = THPVariable_Unpack(v[7]).numel();
+    if (pages > INT32_MAX) return fail("shared", "of fewer than 2^31 pages"), nullptr;
+    if (!VEC(v[8], at::kInt, shared_out, pages) || !VEC(v[9], at::kInt, free_pages, pages) || !VEC(v[10], at::kInt, n_free, 1) ||
+        !VEC(v[11], at::kInt, n_free_out, 1) || !OPT(v[12], at::kInt, status, 1) || !VEC(v[13], at::kByte, workspace, -1))
+        return nullptr;
+    const size_t bytes = (size_t)THPVariable_Unpack(v[13]).numel();
+    void* const s = stream();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn((int32_t)batch, block_size, t_cap, release, seq_lens, seq_lens_out, block_table, (int32_t)stride, shared, shared_out, free_pages, n_free,
+            n_free_out, (int32_t)pages, status, workspace, bytes, s);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+// (address, block_size, t_cap, seq_lens, block_table, block_table_out, shared, shared_out, free_pages, free_pages_out, n_free, n_free_out, move_src,
+//  move_dst, n_moves, status, workspace) -> return code
+PyObject* compact_pages(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    using F = int (*)(int32_t, int32_t, int32_t, const int32_t*, const int32_t*, int32_t*, int32_t, const int32_t*, int32_t*, const int32_t*,
+                      int32_t*, const int32_t*, int32_t*, int32_t, int32_t*, int32_t*, int32_t*, uint32_t*, void*, size_t, void*);
+    F fn;
+    int32_t block_size, t_cap, *seq_lens, *block_table, *block_table_out, *shared, *shared_out, *free_pages, *free_pages_out, *n_free, *n_free_out,
+        *move_src, *move_dst, *n_moves;
+    uint32_t* status;
+    void* workspace;
+    int64_t stride, stride_out;
+    if (!count(n, 17) || !entry(v[0], &fn) || !int32_of(v[1], &block_size) || !int32_of(v[2], &t_cap) || !VEC(v[3], at::kInt, seq_lens, -1)) return nullptr;
+    const int64_t batch = THPVariable_Unpack(v[3]).numel();
+    if (!table_of(v[4], "block_table", batch, block_size, t_cap, &block_table, &stride) ||
+        !table_of(v[5], "block_table_out", batch, block_size, t_cap, &block_table_out, &stride_out) || !VEC(v[6], at::kInt, shared, -1))
+        return nullptr;
+    if (batch > 1 && stride_out != stride) return fail("block_table_out", "of block_table's strides"), nullptr;
+    const int64_t pages = THPVariable_Unpack(v[6]).numel();
+    if (pages > INT32_MAX) return fail("shared", "of fewer than 2^31 pages"), nullptr;
+    if (!VEC(v[7], at::kInt, shared_out, pages) || !VEC(v[8], at::kInt, free_pages, pages) || !VEC(v[9], at::kInt, free_pages_out, pages) ||
+        !VEC(v[10], at::kInt, n_free, 1) || !VEC(v[11], at::kInt, n_free_out, 1) || !VEC(v[12], at::kInt, move_src, pages) ||
+        !VEC(v[13], at::kInt, move_dst, pages) || !VEC(v[14], at::kInt, n_moves, 1) || !OPT(v[15], at::kInt, status, 1) ||
+        !VEC(v[16], at::kByte, workspace, -1))
+        return nullptr;
+    const size_t bytes = (size_t)THPVariable_Unpack(v[16]).numel();
+    void* const s = stream();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn((int32_t)batch, block_size, t_cap, seq_lens, block_table, block_table_out, (int32_t)stride, shared, shared_out, free_pages, free_pages_out,
+            n_free, n_free_out, (int32_t)pages, move_src, move_dst, n_moves, status, workspace, bytes, s);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+// A tensor [pages, ...] as a pool: runs of contiguous elements at one distance
+bool pool_of(PyObject* o, eta_page_pool* p, int64_t* pages) {
+    if (!THPVariable_Check(o)) {
+        PyErr_SetString(PyExc_TypeError, "pools must be torch.Tensors");
+        return false;
+    }
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_cuda()) return fail("pools", "CUDA tensors (no CPU path exists)");
+    if (t.device().index() != c10::cuda::current_device()) return fail("pools", "on the current CUDA device");
+    if (t.dim() < 2 || t.numel() == 0) return fail("pools", "of shape [pages, ...], not empty");
+    const int64_t size = (int64_t)t.element_size();
+    // a page's axes by their strides: their order does not matter to a copy
+    int64_t axis[64], n_axes = 0;
+    if (t.dim() > 64) return fail("pools", "of at most 64 axes");
+    for (int64_t k = 1; k < t.dim(); ++k) {
+        if (t.size(k) == 1) continue;
+        int64_t at = n_axes++;
+        for (; at > 0 && t.stride(axis[at - 1]) > t.stride(k); --at) axis[at] = axis[at - 1];
+        axis[at] = k;
+    }
+    int64_t run = 1, pieces = 1, step = 0, k = 0;
+    for (; k < n_axes && t.stride(axis[k]) == run; ++k) run *= t.size(axis[k]);
+    for (; k < n_axes; ++k) {
+        if (pieces == 1) step = t.stride(axis[k]);
+        else if (t.stride(axis[k]) != step * pieces) return fail("pools", "of pages that are contiguous but for one axis");
+        pieces *= t.size(axis[k]);
+    }
+    if (pieces > INT32_MAX) return fail("pools", "of pages of fewer than 2^31 runs");
+    p->base = t.data_ptr();
+    p->n_pieces = (int32_t)pieces;
+    p->piece_bytes = run * size;
+    p->piece_stride = pieces > 1 ? step * size : 0;
+    p->page_stride = t.size(0) > 1 ? t.stride(0) * size : 16;
+    if (*pages < 0) *pages = t.size(0);
+    return t.size(0) == *pages || fail("pools", "of the same number of pages");
+}
+
+// (address, pools, src, dst, n_moves, status) -> return code
+PyObject* copy_pages(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    using F = int (*)(const eta_page_pool*, int32_t, int32_t, const int32_t*, const int32_t*, int32_t, const int32_t*, uint32_t*, void*);
+    F fn;
+    eta_page_pool pools[64];
+    int32_t *src, *dst, *n_moves;
+    uint32_t* status;
+    if (!count(n, 6) || !entry(v[0], &fn)) return nullptr;
+    PyObject* const list = PySequence_Fast(v[1], "pools must be a sequence of tensors");
+    if (!list) return nullptr;
+    const Py_ssize_t n_pools = PySequence_Fast_GET_SIZE(list);
+    int64_t pages = -1;
+    bool ok = n_pools >= 1 && n_pools <= 64;
+    if (!ok) fail("pools", "1 to 64 tensors");
+    for (Py_ssize_t k = 0; ok && k < n_pools; ++k) ok = pool_of(PySequence_Fast_GET_ITEM(list, k), &pools[k], &pages);
+    Py_DECREF(list);
+    if (!ok) return nullptr;
+    if (pages > INT32_MAX) return fail("pools", "of fewer than 2^31 pages"), nullptr;
+    if (!VEC(v[2], at::kInt, src, -1)) return nullptr;
+    const int64_t moves = THPVariable_Unpack(v[2]).numel();
+    if (moves > INT32_MAX) return fail("src", "of fewer than 2^31 moves"), nullptr;
+    if (!VEC(v[3], at::kInt, dst, moves) || !OPT(v[4], at::kInt, n_moves, 1) || !OPT(v[5], at::kInt, status, 1)) return nullptr;
+    void* const s = stream();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn(pools, (int32_t)n_pools, (int32_t)pages, src, dst, (int32_t)moves, n_moves, status, s);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+// (address, desc, parent, granted, musig, mnorm, status) -> return code
+PyObject* fork_summaries(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    using F = int (*)(const eta_cache_desc*, const int32_t*, const int32_t*, void*, float*, uint32_t, uint32_t*, void*);
+    F fn;
+    Struct<eta_cache_desc> ds;
+    int32_t *parent, *granted;
+    void* musig;
+    float* mnorm;
+    uint32_t* status;
+    if (!count(n, 7) || !entry(v[0], &fn)) return nullptr;
+    const eta_cache_desc* d = ds.get(v[1], g_desc);
+    if (!d) return nullptr;
+    const int64_t blocks = (int64_t)d->batch * d->n_kv_heads * d->nb_cap;
+    const bool packed = THPVariable_Check(v[4]) && THPVariable_Unpack(v[4]).scalar_type() == at::kByte;
+    if (!VEC(v[2], at::kInt, parent, d->batch) || !VEC(v[3], at::kInt, granted, d->batch) ||
+        !vector(v[4], packed ? at::kByte : at::kHalf, "musig", blocks * d->head_dim * (packed ? 3 : 2), &musig) ||
+        !VEC(v[5], at::kFloat, mnorm, blocks) || !OPT(v[6], at::kInt, status, 1))
+        return nullptr;
+    void* const s = stream();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn(d, parent, granted, musig, mnorm, packed ? ETA_BUILD_PACKED_SIGMA : 0, status, s);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
 // the eta_params a call would get, as bytes (for the tests)
 PyObject* params(PyObject*, PyObject* const* v, Py_ssize_t n) {
     eta_params p;
@@ -624,6 +822,11 @@ PyMethodDef methods[] = {
     {"decode_kv4", (PyCFunction)(void (*)(void))guarded<decode_kv4>, METH_FASTCALL, nullptr},
     {"unpack", (PyCFunction)(void (*)(void))guarded<unpack>, METH_FASTCALL, nullptr},
     {"plan", (PyCFunction)(void (*)(void))guarded<plan>, METH_FASTCALL, nullptr},
+    {"fork_pages", (PyCFunction)(void (*)(void))guarded<fork_pages>, METH_FASTCALL, nullptr},
+    {"fork_summaries", (PyCFunction)(void (*)(void))guarded<fork_summaries>, METH_FASTCALL, nullptr},
+    {"free_pages", (PyCFunction)(void (*)(void))guarded<free_pages_>, METH_FASTCALL, nullptr},
+    {"compact_pages", (PyCFunction)(void (*)(void))guarded<compact_pages>, METH_FASTCALL, nullptr},
+    {"copy_pages", (PyCFunction)(void (*)(void))guarded<copy_pages>, METH_FASTCALL, nullptr},
     {"prefill", (PyCFunction)(void (*)(void))guarded<prefill>, METH_FASTCALL, nullptr},
     {"params", (PyCFunction)(void (*)(void))guarded<params>, METH_FASTCALL, nullptr},
     {"set_classes", (PyCFunction)(void (*)(void))set_classes, METH_FASTCALL, nullptr},
