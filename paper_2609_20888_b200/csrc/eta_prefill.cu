@@ -17,13 +17,16 @@
 // instead of once a tile.  Weights are rounded to bf16 (relative 2^-8, as much as the output's own rounding); their sum, O and
 // the maximum are fp32.
 //
-// What bounds it: a tile of a half is a chain, S (512 cycles at head_dim 128) -> maximum -> weights (1024 cycles of the special function
-// unit for the 128 x 128 exponentials) -> O (512), and there is tensor memory for two halves, not three.  One 8K prompt of 32 / 8
-// heads of 128 takes 560 us (980 TFLOP/s), 32K 7.8 ms (1130, at the power limit: 1.64 GHz); gated scores take two more special functions
-// and a dozen instructions each: 11 packed prompts to 5K 1.09 ms (490).  64 single tokens behind 16K stream at 4.4 TB/s.
-// Tried: a thread per row and eight softmax warps 8.4 to 9.4 ms for 32K; a warp for each half's MMAs, whose halves fall into step, 10.3;
-// a quarter of the exponentials as polynomials on the fp32 pipe 9.2 (power); steps of 64 tokens with the next scores worked out
-// ahead 11.9 (twice the hand-overs; an S of 64 columns runs at two thirds of the rate); all waits and MMAs from one lane 10.5.
+// What bounds it: a tile of a half is a chain, S (512 cycles of the tensor core at head_dim 128) -> maximum (460) -> weights (two passes of 850,
+// where 512 are the special function unit's, which the halves share) -> O (the last 256), with some 90 cycles from each warp's word to the next
+// one's; there is tensor memory for two halves' chains, not three: 3600 cycles a tile of both, of which the tensor core has 2048.  One 8K prompt
+// of 32 / 8 heads of 128 takes 545 to 575 us (1000 TFLOP/s), 32K 7.7 to 8.8 ms (1.1 PFLOP/s, at the power limit: 1.64 GHz); gated scores take two more special
+// functions and a dozen instructions each: 11 packed prompts to 5K 1.09 ms (490).  64 single tokens behind 16K stream at 6.0 TB/s.
+// Tried, for the 32K prompt: a thread per row and eight softmax warps 8.4 to 9.4 ms; a warp for each half's MMAs, free 10.3, taking turns 8.9 (the
+// halves fall into step; a token for the special function unit keeps them apart and costs what it gains); a quarter of the exponentials as polynomials on the fp32
+// pipe 9.2 (power); steps of 64 tokens with the next scores worked out ahead 11.9 (twice the hand-overs; an S of 64 columns runs at two
+// thirds of the rate); waits and MMAs from one lane 10.5.  Scores in registers instead of read twice: the same, but 64 single tokens 700 us
+// instead of 540 (what the warps that copy had in registers went to memory).
 //
 // V rows that some row of the item must not see (behind its position, or behind the sequence) would reach it as 0 * V, which is not 0 for
 // infinities and NaN.  In the one to three tiles of an item where that can be, two warps take them out of the shared-memory tile: rows
@@ -48,9 +51,10 @@ constexpr int PF_SOFTMAX_WARPS = 16, PF_WARPS = PF_SOFTMAX_WARPS + 4, PF_THREADS
 constexpr int PF_COPY = PF_SOFTMAX_WARPS, PF_MMA = PF_COPY + 1, PF_CLEAN = PF_MMA + 1;       // warps
 constexpr int PF_MAX_CTAS = 160;           // sizes the scratch of split items
 constexpr int PF_MAX_BATCH = 1024;         // sequences whose prefix sums a CTA keeps in shared memory
-// What an item costs beside its tiles, in tiles (queries, output, a pipeline that runs dry): with 1 and 2 the shares of an 8K prompt that hold
-// the short items were late (700, 652 us; 4: 560).  What joining split items costs.
-constexpr int PF_ITEM_COST = 4, PF_SPLIT_COST = 4;
+// Cost of a tile of K and V for an item with rows for both halves, for one with rows for one (which streams them); what an item costs beside
+// them (queries, output, a pipeline that runs dry), what joining split items costs; in quarter tiles.  As measured: 64 requests, most of them single
+// tokens, with 4, 3, 2 for the second 1390, 1230, 1315 us; an 8K prompt with 4, 8, 16, 24 for the third 700, 650, 570, 580 us.
+constexpr int PF_TILE_COST = 4, PF_TWIN_COST = 3, PF_ITEM_COST = 16, PF_SPLIT_COST = 16;
 constexpr int64_t PF_L2_BYTES = 64ll << 20;     // K and V of the heads that are worked on side by side
 // registers: 640 threads start with 96; 512 of them take 104, the others 64 (together what the block was launched with)
 constexpr int PF_REGS = 96, PF_REGS_SOFTMAX = 104, PF_REGS_OTHER = 64;
@@ -68,7 +72,7 @@ struct PrefillArgs {
     float2* part_ml;                       // [2 PF_MAX_CTAS][PF_ROWS]
     int4* desc;                            // [PF_MAX_CTAS] the split item that starts in a CTA's share: parts, first row, tokens, KV head
     uint32_t* status;
-    float a, beta, scale;
+    float a, beta, scale, unit;            // unit: log2 e of what maxima are kept in
     int batch, Hq, Hkv, g_shift, b_shift, t_cap, n_rows, table_stride, ungate;
 };
 
@@ -85,6 +89,8 @@ struct PfTiles {
         base = max(len - n, 0);
     }
     PF_BOTH int tiles(int t) const { return (int)(((int64_t)base + min((int64_t)(t + 1) * m, (int64_t)n) + PF_TILE - 1) / PF_TILE); }
+    // what a tile of query tile t counts
+    PF_BOTH int weight(int t) const { return t == nq - 1 && 2 * (n - t * m) <= m ? PF_TWIN_COST : PF_TILE_COST; }
     // sum of the tiles of the first t query tiles, t < nq (the last one may be shorter)
     PF_BOTH int64_t before(int t) const {
         const int64_t b0 = (int64_t)base + m + PF_TILE - 1;
@@ -96,8 +102,8 @@ struct PfTiles {
     }
     // cost of the first t query tiles, t <= nq
     PF_BOTH int64_t cost_before(int t) const {
-        if (t < nq || !t) return before(t) + (int64_t)t * PF_ITEM_COST;
-        return before(t - 1) + tiles(t - 1) + (int64_t)t * PF_ITEM_COST;
+        if (t < nq || !t) return PF_TILE_COST * before(t) + (int64_t)t * PF_ITEM_COST;
+        return PF_TILE_COST * before(t - 1) + (int64_t)weight(t - 1) * tiles(t - 1) + (int64_t)t * PF_ITEM_COST;
     }
 };
 
@@ -105,18 +111,19 @@ struct PfTables {                          // in shared memory
     int64_t cost[PF_MAX_BATCH + 1];        // cost of all items of the sequences before
     int32_t items[PF_MAX_BATCH + 1];
     int32_t row0[PF_MAX_BATCH], n[PF_MAX_BATCH], len[PF_MAX_BATCH];
-    int32_t longest;                       // tiles of the longest item
+    int32_t longest;                       // cost of the longest item's tiles
 };
 
 struct PfItem {
     int seq, hk, row0, n_tok;              // first row in the packed rows, tokens that count
     int p0;                                // position of the first token
     int kv_end;                            // tokens [0, kv_end) are seen by some row
-    int k0, k1, n[2];                      // tiles [k0, k1); how many of them each half takes
+    int k0, k1, n0, n1;                    // tiles [k0, k1); how many of them each half takes
     bool twin;                             // rows for one half only: both have them and take turns on the tiles
     int clean0;                            // first tile in which not every row sees every token
     int slot;                              // of a part of a split item; -1: whole
     int pieces;                            // the parts of the item that starts here and goes on; 0: none
+    PF_BOTH int n(int half) const { return half ? n1 : n0; }       // (an array indexed by a number would live in memory)
 };
 
 // Walks the items of a CTA.  Every warp of it runs the same walk.
@@ -140,7 +147,7 @@ struct PfWalk {
         // whole items: as long as the longest, or as the mean with half an item left over at the end
         const int64_t est_whole = total <= ctas ? longest : max(longest, mean + longest / 2);
         whole = est_whole <= mean + PF_ITEM_COST + PF_SPLIT_COST;
-        P = (int)min((int64_t)ctas, max((int64_t)1, C / (PF_ITEM_COST + 4)));
+        P = (int)min((int64_t)ctas, max((int64_t)1, C / (PF_ITEM_COST + 4 * PF_TILE_COST)));
         x = x1 = C;
         if (whole || cta >= P) return;
         x = C * cta / P; x1 = C * (cta + 1) / P;
@@ -184,12 +191,12 @@ struct PfWalk {
         const int n = max(0, it.k1 - k0);
         it.twin = 2 * it.n_tok <= m && n > 1;
         if (it.twin) {
-            it.n[0] = (n + 1) / 2; it.n[1] = n / 2;
+            it.n0 = (n + 1) / 2; it.n1 = n / 2;
             return;
         }
         const int end = it.p0 + min(it.n_tok, m / 2);          // of the first half's rows
-        it.n[0] = max(0, min(it.k1, end > 0 ? (end - 1) / PF_TILE + 1 : 0) - k0);
-        it.n[1] = 2 * it.n_tok > m ? n : 0;
+        it.n0 = max(0, min(it.k1, end > 0 ? (end - 1) / PF_TILE + 1 : 0) - k0);
+        it.n1 = 2 * it.n_tok > m ? n : 0;
     }
     PF_BOTH bool next(PfItem& it) {
         if (whole) {
@@ -215,11 +222,11 @@ struct PfWalk {
         }
         while (x < x1) {
             const PfTiles ti(tab.len[seq], tab.n[seq], m);
-            const int tiles = ti.tiles(qt);
-            const int64_t end = start + PF_ITEM_COST + tiles;
-            const int k0 = (int)max((int64_t)0, x - start - PF_ITEM_COST);
-            const int k1 = (int)max((int64_t)0, min(x1, end) - start - PF_ITEM_COST);
-            if (k1 > k0) {                     // (else the share ends in the fixed part of the item)
+            const int tiles = ti.tiles(qt), weight = ti.weight(qt);
+            const int64_t end = start + PF_ITEM_COST + (int64_t)weight * tiles;
+            const int k0 = (int)(max((int64_t)0, x - start - PF_ITEM_COST) / weight);
+            const int k1 = (int)(max((int64_t)0, min(x1, end) - start - PF_ITEM_COST) / weight);
+            if (k1 > k0) {                     // (else the share has no whole tile of the item)
                 fill(it, seq, hk, qt);
                 clip(it, k0, k1);
                 it.slot = -1; it.pieces = 0;
@@ -369,6 +376,7 @@ struct PfSmem {
     static constexpr int BARS = TABLES + (int)((sizeof(PfTables) + 15) / 16 * 16);
     static constexpr int N_BARS = 3 * NSTAGE + 2 * (4 + PF_CHUNKS) + 1;
     static constexpr int BYTES = 1024 + BARS + 8 * N_BARS;
+    static_assert(PF_CHUNKS == 2, "a chunk is 32 of a thread's columns");
     static_assert(BYTES <= 227 * 1024, "too much shared memory");
 };
 
@@ -437,7 +445,8 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
             const PfTiles ti(len, n, PF_ROWS >> a.g_shift);
             items += ti.nq * a.Hkv;
             cost += a.Hkv * ti.cost_before(ti.nq);
-            if (n) longest = max(longest, ti.tiles(ti.nq - 1));
+            if (n) longest = max(longest, ti.weight(ti.nq - 1) * ti.tiles(ti.nq - 1));
+            if (ti.nq > 1) longest = max(longest, PF_TILE_COST * ti.tiles(ti.nq - 2));
         }
         int64_t sc = cost, si = items;
 #pragma unroll
@@ -468,15 +477,16 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PF_REGS_OTHER));
         if (warp == PF_COPY) {
             // -------------------------------------------------------------- copies
-            uint32_t fill = 0, q_loads[2] = {0, 0};
+            uint32_t fill = 0, q_par = 0, q_some = 0;          // a bit per half: the parity of its next load, whether there was one
             int4 split = make_int4(0, 0, 0, 0);
             while (ok && walk.next(it)) {
                 if (it.pieces > 1) split = make_int4(it.pieces, it.row0, it.n_tok, it.hk);
                 const int n = max(0, it.k1 - it.k0);
                 auto load_q = [&](int h) {
-                    if (!ok || !it.n[h]) return;
-                    if (q_loads[h] && !pf_wait(&q_empty[h], (q_loads[h] - 1) & 1, &s_dead)) { ok = false; return; }
-                    ++q_loads[h];
+                    if (!ok || !it.n(h)) return;
+                    if (((q_some >> h) & 1) && !pf_wait(&q_empty[h], ((q_par >> h) & 1) ^ 1, &s_dead)) { ok = false; return; }
+                    q_some |= 1u << h;
+                    q_par ^= 1u << h;
                     if (lane == 0) {
                         mbar_arrive_expect_tx(&q_full[h], L::Q_BYTES);
 #pragma unroll
@@ -532,61 +542,64 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                 }
                 for (uint32_t f = fill > NSTAGE ? fill - NSTAGE : 0; f < fill; ++f) mbar_wait(&full[f % NSTAGE], (f / NSTAGE) & 1);
                 for (int h = 0; h < 2; ++h)
-                    if (q_loads[h]) mbar_wait(&q_full[h], (q_loads[h] - 1) & 1);
+                    if ((q_some >> h) & 1) mbar_wait(&q_full[h], ((q_par >> h) & 1) ^ 1);
             }
             pdl_trigger();
         } else if (warp == PF_MMA) {
             // -------------------------------------------------------------- MMAs; the whole warp walks along, one lane issues
-            uint32_t fill = 0, n_clean = 0, q_n[2] = {0, 0}, p_n[2] = {0, 0};
-            const uint64_t q_op0 = pf_operand(smem_u32(smem), 16), ring_k = pf_operand(smem_u32(smem + L::RING), 16), ring_v = pf_operand(smem_u32(smem + L::RING), PF_TILE * 128);
-            auto wait = [&](uint64_t* bar, uint32_t parity) {
-                ok = ok && pf_wait(bar, parity, &s_dead);
-                ok = __all_sync(0xffffffffu, ok);
-                return ok;
+            // Every instruction between a wait and the MMAs behind it is time that the tensor core stands still: the warp takes some seven
+            // cycles for one.
+            uint32_t fill = 0, n_clean = 0, q_par = 0, p_par = 0;          // (parities: a bit per half)
+            const uint64_t q_op0 = pf_operand(smem_u32(smem), 16), ring_k = pf_operand(smem_u32(smem + L::RING), 16),
+                           ring_v = pf_operand(smem_u32(smem + L::RING), PF_TILE * 128);
+            auto wait = [&](uint64_t* bar, uint32_t parity) {              // (the same answer in all lanes)
+                for (uint32_t it_ = 0; it_ < WAIT_LIMIT; ++it_) {
+                    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+                    if ((it_ & 255) == 255 && __any_sync(0xffffffffu, *(volatile int*)&s_dead)) break;
+                }
+                ok = false;
+                return false;
             };
-            auto release = [&](int stage) {
-                if (pf_elect()) pf_commit(&empty[stage]);
-                __syncwarp();
-            };
-            // One turn of half h: O += P V (vs: the stage of V; negative: none), then S = Q K^T of its next tile (ks), over the weights.
-            // What the second needs has been waited for, so that it goes out right behind the first.
-            auto turn = [&](int h, int vs, int ks, bool first, bool last_v, bool last_k) {
-                const uint64_t q_op = q_op0 + (uint32_t)(h * (L::Q_BYTES >> 4)), k_op = ring_k + (uint32_t)(max(ks, 0) * (L::STAGE >> 4));
-                const uint64_t v_op = ring_v + (uint32_t)(max(vs, 0) * (L::STAGE >> 4));
-                const uint32_t t_s = tmem + h * PF_TILE, t_o = tmem + 2 * PF_TILE + h * D;
+            auto there = [&](uint32_t f) { return wait(&full[f % NSTAGE], (f / NSTAGE) & 1); };
+            // One turn of half h: O += P V with the values of fill fv, then S = Q K^T with the keys of fill fk, over the weights; the latter goes
+            // out right behind the former.  What both read has been waited for.
+            enum { VALUES = 1, KEYS = 2, FIRST = 4, LAST_VALUES = 8, LAST_KEYS = 16, FREE_VALUES = 32, FREE_KEYS = 64 };
+            auto turn = [&](int h, uint32_t fv, uint32_t fk, uint32_t what) {
+                const uint64_t q_op = q_op0 + (uint32_t)(h * (L::Q_BYTES >> 4)), k_op = ring_k + (fk % NSTAGE) * (L::STAGE >> 4);
+                const uint64_t v_op = ring_v + (fv % NSTAGE) * (L::STAGE >> 4);
+                const uint32_t t_s = h * PF_TILE, t_o = 2 * PF_TILE + h * D, parity = (p_par >> h) & 1;
                 constexpr int PER = PF_TILE / 32 / PF_CHUNKS;
                 auto values = [&](int c) {
 #pragma unroll
                     for (int u = 0; u < 2 * PER; ++u) {        // 16 tokens: two groups of eight rows; a chunk's share of the first 64 tokens, then of the others
                         const int k = c * PER + u % PER + (u / PER) * (PF_TILE / 32);
-                        pf_mma_ts(t_o, t_s + 8 * k, v_op + k * (16 * 128 >> 4), pf_idesc(D, true), !first || c > 0 || u > 0);
+                        pf_mma_ts(t_o, t_s + 8 * k + (k >= PF_TILE / 32 ? PF_TILE / 4 : 0), v_op + k * (16 * 128 >> 4), pf_idesc(D, true), !(what & FIRST) || c > 0 || u > 0);
                     }
                 };
-                if (vs >= 0) {
+                if (what & VALUES) {
 #pragma unroll
                     for (int c = 0; c + 1 < PF_CHUNKS; ++c) {
-                        if (!wait(&p_full[h * PF_CHUNKS + c], p_n[h] & 1)) return;
+                        if (!wait(&p_full[h * PF_CHUNKS + c], parity)) return;
                         pf_fence_after();
                         if (pf_elect()) values(c);
-                        __syncwarp();
                     }
-                    if (!wait(&p_full[h * PF_CHUNKS + PF_CHUNKS - 1], p_n[h] & 1)) return;
-                    ++p_n[h];
+                    if (!wait(&p_full[h * PF_CHUNKS + PF_CHUNKS - 1], parity)) return;
                     pf_fence_after();
+                    p_par ^= 1u << h;
                 }
                 if (pf_elect()) {
-                    if (vs >= 0) {
-                        values(PF_CHUNKS - 1);
-                        if (last_v) pf_commit(&o_full[h]);
-                    }
-                    if (ks >= 0) {
+                    if (what & VALUES) values(PF_CHUNKS - 1);
+                    if (what & KEYS) {
 #pragma unroll
                         for (int k = 0; k < D / 16; ++k)       // 16 columns: 32 bytes along the swizzled row of a 64-column half
                             pf_mma_ss(t_s, q_op + (k / 4) * (PF_HALF * 128 >> 4) + (k % 4) * 2, k_op + (k / 4) * (PF_TILE * 128 >> 4) + (k % 4) * 2,
                                       pf_idesc(PF_TILE, false), k > 0);
                         pf_commit(&s_full[h]);
-                        if (last_k) pf_commit(&q_empty[h]);
                     }
+                    if (what & LAST_VALUES) pf_commit(&o_full[h]);
+                    if (what & LAST_KEYS) pf_commit(&q_empty[h]);
+                    if (what & FREE_VALUES) pf_commit(&empty[fv % NSTAGE]);
+                    if (what & FREE_KEYS) pf_commit(&empty[fk % NSTAGE]);
                 }
                 __syncwarp();
             };
@@ -595,17 +608,15 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                 // tile j: keys in fill base + 2 j, values in the one behind it
                 const uint32_t base = fill;
                 fill += 2 * n;
-                // tile j's keys or values are there
-                auto there = [&](uint32_t f) { return wait(&full[f % NSTAGE], (f / NSTAGE) & 1); };
-                for (int h = 0; h < 2; ++h) {
+                const int last_half = it.twin || it.n1 == 0 ? 0 : 1;       // whose turn frees a tile's stages (not twin)
+#pragma unroll 1
+                for (int h = 0; h < 2 && ok; ++h) {
                     const uint32_t f = base + (it.twin ? 2 * h : 0);
-                    if (!it.n[h] || !wait(&q_full[h], q_n[h]++ & 1) || !there(f)) continue;
-                    turn(h, -1, f % NSTAGE, false, false, it.n[h] == 1);
-                    if (it.twin) release(f % NSTAGE);
+                    if (!it.n(h) || !wait(&q_full[h], (q_par >> h) & 1)) continue;
+                    q_par ^= 1u << h;
+                    if (there(f)) turn(h, 0, f, KEYS | (it.n(h) == 1 ? LAST_KEYS : 0) | (it.twin || h == last_half ? FREE_KEYS : 0));
                 }
-                if (!ok) break;
-                if (n && !it.twin) release(base % NSTAGE);
-                for (int j = 0; j < n; ++j) {
+                for (int j = 0; j < n && ok; ++j) {
                     const uint32_t f = base + 2 * j + 1, next = base + 2 * (j + step);
                     const bool more = j + step < n;
                     if (!there(f)) break;
@@ -616,17 +627,16 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                     // (where memory is slow the next keys are not there yet: products first then)
                     const bool ready = more && __all_sync(0xffffffffu, mbar_test(&full[next % NSTAGE], (next / NSTAGE) & 1));
                     // half after half, so that one half's weights are worked out while the other's products run
-                    for (int h = 0; h < 2 && ok; ++h) {
-                        if (it.twin && h != (j & 1)) continue;
-                        const int i = it.twin ? j >> 1 : j;
-                        if (i >= it.n[h]) continue;
-                        const bool goes_on = i + 1 < it.n[h];
-                        turn(h, f % NSTAGE, goes_on && ready ? (int)(next % NSTAGE) : -1, i == 0, !goes_on, i + 2 == it.n[h]);
-                        if (ok && goes_on && !ready && there(next)) turn(h, -1, next % NSTAGE, false, false, i + 2 == it.n[h]);
+#pragma unroll 1
+                    for (int h = it.twin ? j & 1 : 0; h < 2 && ok; h += step) {
+                        const int i = it.twin ? j >> 1 : j, left = it.n(h) - i;        // steps of the half that are left, this one among them
+                        if (left <= 0) continue;
+                        const bool frees = it.twin || h == last_half;
+                        const uint32_t v = VALUES | (i == 0 ? FIRST : 0) | (left == 1 ? LAST_VALUES : 0) | (frees ? FREE_VALUES : 0);
+                        const uint32_t k = left > 1 ? KEYS | (left == 2 ? LAST_KEYS : 0) | (frees ? FREE_KEYS : 0) : 0;
+                        turn(h, f, next, ready ? v | k : v);
+                        if (k && !ready && ok && there(next)) turn(h, 0, next, k);
                     }
-                    if (!ok) break;
-                    release(f % NSTAGE);
-                    if (more) release(next % NSTAGE);
                 }
             }
             // what was issued has to end before tensor and shared memory are given back
@@ -698,19 +708,19 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
         constexpr int W = PF_TILE / 2, DW = D / 2;
         const int half = (warp >> 2) & 1, part = warp >> 3, wrow = (warp & 3) * 32, row = wrow + lane;
         const uint32_t lanes = (uint32_t)wrow << 16;
-        const uint32_t t_s = tmem + lanes + half * PF_TILE + part * W, t_p = tmem + lanes + half * PF_TILE + part * (W / 2);
+        const uint32_t t_s = tmem + lanes + half * PF_TILE + part * W;
         const uint32_t t_o = tmem + lanes + 2 * PF_TILE + half * D + part * DW;
         const int pair = 1 + (warp & 7);               // the barrier of the two warps that share 32 rows
         float* const tell = &s_x[part][half * PF_HALF + row];
         const float* const told = &s_x[part ^ 1][half * PF_HALF + row];
-        const float sl2 = a.scale * LOG2E, kb = a.scale * a.beta * LOG2E;
+        const float sl2 = a.scale * LOG2E, kb = a.scale * a.beta * LOG2E, unit = GATED ? 1.f : sl2;
         uint32_t s_n = 0, o_n = 0;
         int item = 0;
         while (ok && walk.next(it)) {
             ++item;
             const int tok0 = it.twin ? 0 : half * HT, rows = min(max(it.n_tok - tok0, 0), HT) << a.g_shift;
             if (!rows) continue;
-            const int n = it.n[half];
+            const int n = it.n(half);
             const bool live = wrow < rows;                  // a warp without rows only keeps step
             const int r = min(row, rows - 1), tok = tok0 + (r >> a.g_shift), h = it.hk * G + (r & (G - 1));
             const int p = it.p0 + tok;                      // the row sees tokens 0 .. p
@@ -722,84 +732,85 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                 if (a.beta != 0.f) tb = te * a.beta * LOG2E;
                 if (te != te) l0 = te;                      // a threshold that is NaN: so is the row
             }
-            float m = -INFINITY, c = -INFINITY;             // running maximum: of q.k, and in the exponents' units
+            float m = -INFINITY;                            // running maximum, of q.k (gated: of S~ log2 e)
             for (int j = 0; j < n; ++j) {
                 ok = __all_sync(0xffffffffu, pf_wait(&s_full[half], s_n++ & 1, &s_dead));
                 if (j == 0 && !it.twin && lane == 0) mbar_arrive(&q_empty[half]);
                 if (live) {
                     pf_fence_after();
-                    float s[W];
-                    pf_ld32(t_s, s);
-                    pf_ld32(t_s + 32, s + 32);
-                    pf_wait_ld();
+                    // The scores are read twice, 32 columns at a time: for the maximum (gated ones, and those at an edge, go back to where they
+                    // came from), then for the weights, which take the place of the first half of them.
                     const int tile = it.k0 + (it.twin ? 2 * j + half : j);
                     const int nvis = p - tile * PF_TILE - part * W + 1;                  // columns that the row sees
                     const bool edge = __any_sync(0xffffffffu, nvis <= W);
-                    if constexpr (GATED) {
-                        const int own = a.ungate ? nvis - 1 : -1;             // the column that stays raw
-                        float am[4] = {0.f, 0.f, 0.f, 0.f};
+                    float mx = -INFINITY;
+#pragma unroll 1
+                    for (int g = 0; g < 2; ++g) {
+                        float s[32];
+                        pf_ld32(t_s + 32 * g, s);
+                        const int here = nvis - 32 * g;
+                        pf_wait_ld();
+                        if constexpr (GATED) {
+                            const int own = a.ungate ? here - 1 : -1;             // the column that stays raw
+                            float am[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int k = 0; k < W; k += 8)
+                            for (int k = 0; k < 32; k += 8)
 #pragma unroll
-                            for (int u = 0; u < 4; ++u) am[u] = pf_max3(am[u], fabsf(s[k + u]), fabsf(s[k + u + 4]));
-                        const bool far = __any_sync(0xffffffffu, !(fmaxf(fmaxf(am[0], am[1]), fmaxf(am[2], am[3])) * sl2 < 0x1p40f));
-                        auto gate = [&](auto masked) {
+                                for (int u = 0; u < 4; ++u) am[u] = pf_max3(am[u], fabsf(s[k + u]), fabsf(s[k + u + 4]));
+                            if (__any_sync(0xffffffffu, !(pf_max3(fmaxf(am[0], am[1]), am[2], am[3]) * sl2 < 0x1p40f))) {
 #pragma unroll
-                            for (int k0 = 0; k0 < W; k0 += 8) {           // stage by stage, so that 8 / 2 chains run side by side
-                                float x[8], e[8], g[8];
+                                for (int k = 0; k < 32; ++k) {
+                                    const float x = s[k] * sl2, gate = pf_rcp(1.f + pf_ex2(fmaf(s[k], -kb, tb)));
+                                    s[k] = k == own ? x : x * gate;
+                                }
+                            } else {
 #pragma unroll
-                                for (int k = 0; k < 8; k += 2) pf_fma2(e[k], e[k + 1], s[k0 + k], s[k0 + k + 1], -kb, tb);
-                                // Both reciprocals of a pair from the one of their product.  So that it stays finite a gate is no smaller than 2^-62:
-                                // a score below 2^40 then counts as 0 all the same.
+                                for (int k0 = 0; k0 < 32; k0 += 8) {           // stage by stage, so that chains run side by side
+                                    float x[8], e[8], r[4];
 #pragma unroll
-                                for (int k = 0; k < 8; ++k) e[k] = pf_ex2(fminf(e[k], 62.f));
+                                    for (int k = 0; k < 8; k += 2) pf_fma2(e[k], e[k + 1], s[k0 + k], s[k0 + k + 1], -kb, tb);
+                                    // Both reciprocals of a pair from the one of their product.  So that it stays finite a gate is no smaller than
+                                    // 2^-62: a score below 2^40 then counts as 0 all the same.
 #pragma unroll
-                                for (int k = 0; k < 8; k += 2) { add2(e[k], e[k + 1], 1.f, 1.f); mul2(x[k], x[k + 1], s[k0 + k], s[k0 + k + 1], sl2, sl2); }
+                                    for (int k = 0; k < 8; ++k) e[k] = pf_ex2(fminf(e[k], 62.f));
 #pragma unroll
-                                for (int k = 0; k < 8; k += 2) g[k] = pf_rcp(e[k] * e[k + 1]);
+                                    for (int k = 0; k < 8; k += 2) { add2(e[k], e[k + 1], 1.f, 1.f); mul2(x[k], x[k + 1], s[k0 + k], s[k0 + k + 1], sl2, sl2); }
 #pragma unroll
-                                for (int k = 0; k < 8; k += 2) mul2(e[k + 1], e[k], x[k], x[k + 1], e[k + 1], e[k]);
+                                    for (int k = 0; k < 8; k += 2) r[k / 2] = pf_rcp(e[k] * e[k + 1]);
 #pragma unroll
-                                for (int k = 0; k < 8; k += 2) {
-                                    mul2(s[k0 + k], s[k0 + k + 1], e[k + 1], e[k], g[k], g[k]);
-                                    if (decltype(masked)::value) {
-                                        s[k0 + k] = k0 + k < nvis ? (k0 + k == own ? x[k] : s[k0 + k]) : -INFINITY;
-                                        s[k0 + k + 1] = k0 + k + 1 < nvis ? (k0 + k + 1 == own ? x[k + 1] : s[k0 + k + 1]) : -INFINITY;
+                                    for (int k = 0; k < 8; k += 2) mul2(e[k + 1], e[k], x[k], x[k + 1], e[k + 1], e[k]);
+#pragma unroll
+                                    for (int k = 0; k < 8; k += 2) mul2(s[k0 + k], s[k0 + k + 1], e[k + 1], e[k], r[k / 2], r[k / 2]);
+                                    if (edge) {
+#pragma unroll
+                                        for (int k = 0; k < 8; ++k) s[k0 + k] = k0 + k == own ? x[k] : s[k0 + k];
                                     }
                                 }
                             }
-                        };
-                        if (far) {
+                        }
+                        if (edge) {
 #pragma unroll
-                            for (int k = 0; k < W; ++k) {
-                                const float x = s[k] * sl2, g = pf_rcp(1.f + pf_ex2(fmaf(s[k], -kb, tb)));
-                                s[k] = k < nvis ? (k == own ? x : x * g) : -INFINITY;
-                            }
-                        } else
-                        if (edge) gate(std::true_type{});
-                        else gate(std::false_type{});
-                    } else if (edge) {
+                            for (int k = 0; k < 32; ++k) s[k] = k < here ? s[k] : -INFINITY;
+                        }
+                        if (GATED || edge) pf_st32(t_s + 32 * g, reinterpret_cast<const uint32_t*>(s));
+                        float x[4];
 #pragma unroll
-                        for (int k = 0; k < W; ++k) s[k] = k < nvis ? s[k] : -INFINITY;
+                        for (int k = 0; k < 4; ++k) x[k] = pf_max3(s[k], s[k + 4], s[k + 8]);
+#pragma unroll
+                        for (int k = 12; k + 8 <= 32; k += 8)
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) x[u] = pf_max3(x[u], s[k + u], s[k + u + 4]);
+                        mx = pf_max3(mx, pf_max3(pf_max3(x[0], x[1], x[2]), x[3], s[28]), pf_max3(s[29], s[30], s[31]));
                     }
-                    float x[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) x[k] = pf_max3(s[k], s[k + 4], s[k + 8]);
-#pragma unroll
-                    for (int k = 12; k + 8 <= W; k += 8)
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) x[u] = pf_max3(x[u], s[k + u], s[k + u + 4]);
-                    float mx = pf_max3(pf_max3(x[0], x[1], x[2]), x[3], pf_max3(s[W - 4], s[W - 3], fmaxf(s[W - 2], s[W - 1])));
-                    // Both threads have their scores when they meet here: weights may overwrite them.  A warp whose wait ran out comes here
-                    // too, so that no meeting is left waiting for it.
-                    if (pf_any_of<2>(!ok || (GATED ? mx : mx * sl2) > c + PF_SLACK, pair)) {
+                    if (GATED || edge) pf_wait_st();
+                    // Both threads meet here.  A warp whose wait ran out comes here too, so that no meeting is left waiting for it.
+                    if (pf_any_of<2>(!ok || (mx - m) * unit > PF_SLACK, pair)) {
                         *tell = mx;
                         if (pf_any_of<2>(!ok, pair)) { ok = false; break; }
                         mx = fmaxf(mx, *told);
-                        const float c_new = fmaxf(c, GATED ? mx : mx * sl2);
-                        const float alpha = c == c_new ? 1.f : pf_ex2(c - c_new);
-                        m = fmaxf(m, mx);
-                        c = c_new;
+                        const float m_new = fmaxf(m, mx);
+                        const float alpha = m == m_new ? 1.f : pf_ex2((m - m_new) * unit);
+                        m = m_new;
                         l0 *= alpha; l1 *= alpha; l2 *= alpha; l3 *= alpha;
                         if (j) {                       // these scores are complete, so is the product before them
 #pragma unroll 1
@@ -813,45 +824,37 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                             }
                         }
                     }
-                    const float cu = c == -INFINITY ? 0.f : c;
-                    // q.k scale - maximum in one rounding, off by the rounding of the maximum's product: the same factor for the whole
-                    // row, which cancels.  Where that could be a large one the difference is formed first.
-                    const bool huge = !GATED && fabsf(cu) > 4194304.f;
-                    float mul = GATED ? 1.f : sl2, sub = -cu;
-                    if (!GATED && __any_sync(0xffffffffu, huge)) {
-                        const float mu = m == -INFINITY ? 0.f : m;
+                    // The difference first: scores of any size lose nothing next to the largest.
+                    const float minus = m == -INFINITY ? 0.f : -m;
+#pragma unroll 1
+                    for (int g = 0; g < PF_CHUNKS; ++g) {
+                        float s[32];
+                        uint32_t w[16];
+                        pf_ld32(t_s + 32 * g, s);
+                        pf_wait_ld();
 #pragma unroll
-                        for (int k = 0; k < W; ++k) s[k] = huge ? (s[k] - mu) * sl2 : fmaf(s[k], sl2, sub);
-                        mul = 1.f; sub = 0.f;
-                    }
-                    // a chunk's weights are on their way to tensor memory while the next chunk's are worked out
-                    auto hand_over = [&](int chunk) {
+                        for (int k = 0; k < 32; k += 2) {
+                            add2(s[k], s[k + 1], minus, minus);
+                            if (!GATED) mul2(s[k], s[k + 1], s[k], s[k + 1], sl2, sl2);
+                        }
+#pragma unroll
+                        for (int k = 0; k < 32; k += 8) {
+#pragma unroll
+                            for (int u = 0; u < 8; ++u) s[k + u] = pf_ex2(s[k + u]);
+#pragma unroll
+                            for (int u = 0; u < 8; u += 4) {
+                                add2(l0, l1, s[k + u], s[k + u + 1]);
+                                add2(l2, l3, s[k + u + 2], s[k + u + 3]);
+                                w[(k + u) / 2] = pf_pack(s[k + u], s[k + u + 1]);
+                                w[(k + u) / 2 + 1] = pf_pack(s[k + u + 2], s[k + u + 3]);
+                            }
+                        }
+                        pf_st16(t_s + 16 * g, w);
                         pf_wait_st();
                         pf_fence_before();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(&p_full[half * PF_CHUNKS + chunk]);
-                    };
-#pragma unroll
-                    for (int k0 = 0; k0 < W; k0 += W / PF_CHUNKS) {
-                        uint32_t w[W / PF_CHUNKS / 2];
-#pragma unroll
-                        for (int q0 = 0; q0 < W / PF_CHUNKS; q0 += 8) {
-                            float p[8];
-#pragma unroll
-                            for (int k = 0; k < 8; k += 2) pf_fma2(p[k], p[k + 1], s[k0 + q0 + k], s[k0 + q0 + k + 1], mul, sub);
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) p[k] = pf_ex2(p[k]);
-#pragma unroll
-                            for (int k = 0; k < 8; k += 2) {
-                                if (k & 2) add2(l2, l3, p[k], p[k + 1]);
-                                else add2(l0, l1, p[k], p[k + 1]);
-                                w[(q0 + k) / 2] = pf_pack(p[k], p[k + 1]);
-                            }
-                        }
-                        if (k0) hand_over(k0 / (W / PF_CHUNKS) - 1);
-                        pf_st16(t_p + k0 / 2, w);
+                        if (lane == 0) mbar_arrive(&p_full[half * PF_CHUNKS + g]);
                     }
-                    hand_over(PF_CHUNKS - 1);
                 } else {
                     if (!ok) break;
                     if (lane == 0)
@@ -880,23 +883,23 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
 #pragma unroll
                             for (int u = 0; u < 16; ++u) hand[(k + u) * PF_HALF] = o[u];
                         }
-                        if (!part) s_twin[row] = make_float2(c, l);
+                        if (!part) s_twin[row] = make_float2(m, l);
                         pf_fence_before();
                         fence_proxy_async();
                     }
                     if (pf_any_of<4>(!ok, 9 + (warp & 3))) ok = false;
                     if (!half) {
                         const float2 ml = s_twin[row];
-                        const float M = fmaxf(c, ml.x);
-                        if (M != -INFINITY) { keep = pf_ex2(c - M); take = pf_ex2(ml.x - M); }
+                        const float M = fmaxf(m, ml.x);
+                        if (M != -INFINITY) { keep = pf_ex2((m - M) * unit); take = pf_ex2((ml.x - M) * unit); }
                         l = l * keep + ml.y * take;
-                        c = M;
+                        m = M;
                     }
                 }
             }
             if (!ok) break;
             const bool poison = n && s_poison[item & 15] == item;
-            if (split && live && mine && !part && !(it.twin && half)) a.part_ml[at_part] = make_float2(c, l);
+            if (split && live && mine && !part && !(it.twin && half)) a.part_ml[at_part] = make_float2(m, l);
             const float inv = split ? 1.f : (l == 0.f ? 0.f : 1.f / l);
             keep *= inv; take *= inv;
             const int64_t to = ((int64_t)(it.row0 + tok) * a.Hq + h) * D + part * DW;
@@ -1000,7 +1003,7 @@ __global__ void __launch_bounds__(32 * PF_JOIN_WARPS) prefill_join_kernel(const 
                 v[0] = t.x; v[1] = t.y;
             }
             if (ml.x == -INFINITY && ml.y == 0.f) continue;             // the row saw none of this part
-            const float w = ml.x == M ? 1.f : exp2f(ml.x - M);
+            const float w = ml.x == M ? 1.f : exp2f((ml.x - M) * a.unit);
             l = fmaf(ml.y, w, l);
 #pragma unroll
             for (int u = 0; u < PER; ++u) acc[u] = fmaf(v[u], w, acc[u]);
@@ -1044,7 +1047,7 @@ static int pf_launch(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUten
     const int rc = launch_pdl("eta_prefill", prefill_kernel<D, GATED>, dim3(ctas), dim3(PF_THREADS), PfSmem<D>::BYTES, s, tmQ, tmK, tmV, a);
     if (rc != ETA_OK) return rc;
     // (no item of at most so many tiles is ever split: see PfWalk)
-    if (a.t_cap <= PF_TILE * PF_SPLIT_COST) return ETA_OK;
+    if (a.t_cap <= PF_TILE * (PF_SPLIT_COST / PF_TILE_COST)) return ETA_OK;
     return launch_pdl("eta_prefill", prefill_join_kernel<D>, dim3(ctas, PF_ROWS / PF_JOIN_ROWS), dim3(32 * PF_JOIN_WARPS), 0, s, a);
 }
 
@@ -1072,8 +1075,8 @@ int eta_selftest_prefill_shares(int batch, int n_kv_heads, int g_shift, int head
         int64_t sum = 0;
         for (int t = 0; t < ti.nq; ++t) {
             if (ti.cost_before(t) != sum) return 1;
-            tab.longest = std::max(tab.longest, ti.tiles(t));
-            sum += ti.tiles(t) + PF_ITEM_COST;
+            tab.longest = std::max(tab.longest, ti.weight(t) * ti.tiles(t));
+            sum += (int64_t)ti.weight(t) * ti.tiles(t) + PF_ITEM_COST;
         }
         if (ti.cost_before(ti.nq) != sum) return 2;
     }
@@ -1091,7 +1094,7 @@ int eta_selftest_prefill_shares(int batch, int n_kv_heads, int g_shift, int head
             if (tok < 0 || tok % m || tok + it.n_tok > n[it.seq] || it.p0 != len[it.seq] - n[it.seq] + tok) return 4;
             Seen& s = seen[(size_t)it.row0 * n_kv_heads + it.hk];
             const int all = it.p0 + it.n_tok > 0 ? (it.p0 + it.n_tok - 1) / PF_TILE + 1 : 0, got = std::max(0, it.k1 - it.k0);
-            if (it.twin ? it.n[0] + it.n[1] != got || 2 * it.n_tok > m : (2 * it.n_tok > m ? it.n[1] : it.n[0]) != got) return 11;
+            if (it.twin ? it.n0 + it.n1 != got || 2 * it.n_tok > m : (2 * it.n_tok > m ? it.n1 : it.n0) != got) return 11;
             if (it.slot < 0) {
                 if (s.parts || it.k0 != 0 || got != all) return 5;
                 s.parts = s.said = 1; s.next = all;
@@ -1191,6 +1194,7 @@ int eta_prefill(const eta_cache_desc* desc, const eta_page_table* pages, const e
     a.g_shift = G == 1 ? 0 : (G == 2 ? 1 : (G == 4 ? 2 : 3));
     a.b_shift = desc->block_size == 32 ? 5 : (desc->block_size == 64 ? 6 : 7);
     a.t_cap = desc->t_cap; a.n_rows = n_rows;
+    a.unit = dense ? a.scale * 1.4426950408889634f : 1.f;
     a.ungate = (params->flags & ETA_FLAG_UNGATE_LAST) ? 1 : 0;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (D == 128) return dense ? pf_launch<128, false>(tmQ, tmK, tmV, a, ctas, s) : pf_launch<128, true>(tmQ, tmK, tmV, a, ctas, s);
