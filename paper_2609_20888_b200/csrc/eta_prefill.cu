@@ -17,11 +17,13 @@
 // instead of once a tile.  Weights are rounded to bf16 (relative 2^-8, as much as the output's own rounding); their sum, O and
 // the maximum are fp32.
 //
-// What bounds it: a tile of a half is a chain, S (512 cycles of the tensor core at head_dim 128) -> maximum (460) -> weights (two passes of 850,
-// where 512 are the special function unit's, which the halves share) -> O (the last 256), with some 90 cycles from each warp's word to the next
-// one's; there is tensor memory for two halves' chains, not three: 3600 cycles a tile of both, of which the tensor core has 2048.  One 8K prompt
-// of 32 / 8 heads of 128 takes 545 to 575 us (1000 TFLOP/s), 32K 7.7 to 8.8 ms (1.1 PFLOP/s, at the power limit: 1.64 GHz); gated scores take two more special
-// functions and a dozen instructions each: 11 packed prompts to 5K 1.09 ms (490).  64 single tokens behind 16K stream at 6.0 TB/s.
+// What bounds it: a tile of a half is a chain, S -> maximum (480 to 570 cycles) -> the two threads of a row meet (200) -> weights (830 to 1000
+// for each chunk, with the other half's beside them) -> O, and 500 more until the next S is there, in the clock of the softmax warps at head_dim 128;
+// there is tensor memory for two halves' chains, not three.  Tensor core and special function unit have 2048 cycles of work a tile each and are
+// busy 51 % of the time.  One 8K prompt of 32 / 8 heads of 128 takes 530 to 600 us, 32K 7.7 to 8.9 ms (1.0 to 1.1 PFLOP/s; by the power limit).  With parts
+// taken out 32K takes 6.3 to 6.8 ms without the products, as much without the softmax, 3.8 without both and without copies.  Gated scores take
+// one and a half more special functions each (65 % busy) and 930 instructions a thread and tile instead of 490: 11 packed prompts to 5K 1.03 ms (520 TFLOP/s).
+// 64 single tokens behind 16K stream at 6.0 TB/s.
 // Tried, for the 32K prompt: a thread per row and eight softmax warps 8.4 to 9.4 ms; a warp for each half's MMAs, free 10.3, taking turns 8.9 (the
 // halves fall into step; a token for the special function unit keeps them apart and costs what it gains); a quarter of the exponentials as polynomials on the fp32
 // pipe 9.2 (power); steps of 64 tokens with the next scores worked out ahead 11.9 (twice the hand-overs; an S of 64 columns runs at two
@@ -51,10 +53,12 @@ constexpr int PF_SOFTMAX_WARPS = 16, PF_WARPS = PF_SOFTMAX_WARPS + 4, PF_THREADS
 constexpr int PF_COPY = PF_SOFTMAX_WARPS, PF_MMA = PF_COPY + 1, PF_CLEAN = PF_MMA + 1;       // warps
 constexpr int PF_MAX_CTAS = 160;           // sizes the scratch of split items
 constexpr int PF_MAX_BATCH = 1024;         // sequences whose prefix sums a CTA keeps in shared memory
-// Cost of a tile of K and V for an item with rows for both halves, for one with rows for one (which streams them); what an item costs beside
-// them (queries, output, a pipeline that runs dry), what joining split items costs; in quarter tiles.  As measured: 64 requests, most of them single
-// tokens, with 4, 3, 2 for the second 1390, 1230, 1315 us; an 8K prompt with 4, 8, 16, 24 for the third 700, 650, 570, 580 us.
-constexpr int PF_TILE_COST = 4, PF_TWIN_COST = 3, PF_ITEM_COST = 16, PF_SPLIT_COST = 16;
+// Cost of a tile of K and V for an item with rows for both halves, for one with rows for one (which streams them); what joining split items
+// costs; what an item costs beside its tiles (queries, output, a pipeline that runs dry); in quarter tiles.  A gated tile takes twice as long, so
+// an item's own cost is worth half as many of them.  As measured: 64 requests, most of them single tokens, with 4, 3, 2 for the second 1427,
+// 1228, 1322 us; with 4, 8, 16, 24, 32 for the last an 8K prompt 644, 605, 558, 579, 586 us, 11 gated prompts 1036, 1034, 1101, 1172, 1205 us.
+constexpr int PF_TILE_COST = 4, PF_TWIN_COST = 3, PF_SPLIT_COST = 16;
+template <bool GATED> constexpr int PF_ITEM_COST = GATED ? 8 : 16;
 constexpr int64_t PF_L2_BYTES = 64ll << 20;     // K and V of the heads that are worked on side by side
 // registers: 640 threads start with 96; 512 of them take 104, the others 64 (together what the block was launched with)
 constexpr int PF_REGS = 96, PF_REGS_SOFTMAX = 104, PF_REGS_OTHER = 64;
@@ -81,6 +85,7 @@ struct PrefillArgs {
 #define PF_BOTH __host__ __device__ __forceinline__
 
 // Tiles of K that query tile t of a sequence needs, and what all before it need, for n new tokens behind ctx; m tokens per query tile.
+template <int ITEM_COST>
 struct PfTiles {
     int nq, m, n, base;
     PF_BOTH PfTiles(int len, int n_, int m_) {
@@ -102,8 +107,8 @@ struct PfTiles {
     }
     // cost of the first t query tiles, t <= nq
     PF_BOTH int64_t cost_before(int t) const {
-        if (t < nq || !t) return PF_TILE_COST * before(t) + (int64_t)t * PF_ITEM_COST;
-        return PF_TILE_COST * before(t - 1) + (int64_t)weight(t - 1) * tiles(t - 1) + (int64_t)t * PF_ITEM_COST;
+        if (t < nq || !t) return PF_TILE_COST * before(t) + (int64_t)t * ITEM_COST;
+        return PF_TILE_COST * before(t - 1) + (int64_t)weight(t - 1) * tiles(t - 1) + (int64_t)t * ITEM_COST;
     }
 };
 
@@ -127,7 +132,9 @@ struct PfItem {
 };
 
 // Walks the items of a CTA.  Every warp of it runs the same walk.
+template <int ITEM_COST>
 struct PfWalk {
+    using Tiles = PfTiles<ITEM_COST>;
     const PfTables& tab;
     int batch, Hkv, m, cta, ctas;
     int64_t head_bytes;                    // bytes of K and V per token and KV head
@@ -143,18 +150,18 @@ struct PfWalk {
         C = tab.cost[batch];
         total = tab.items[batch];
         round = 0;
-        const int64_t longest = tab.longest + PF_ITEM_COST, mean = C / ctas;
+        const int64_t longest = tab.longest + ITEM_COST, mean = C / ctas;
         // whole items: as long as the longest, or as the mean with half an item left over at the end
         const int64_t est_whole = total <= ctas ? longest : max(longest, mean + longest / 2);
-        whole = est_whole <= mean + PF_ITEM_COST + PF_SPLIT_COST;
-        P = (int)min((int64_t)ctas, max((int64_t)1, C / (PF_ITEM_COST + 4 * PF_TILE_COST)));
+        whole = est_whole <= mean + ITEM_COST + PF_SPLIT_COST;
+        P = (int)min((int64_t)ctas, max((int64_t)1, C / (ITEM_COST + 4 * PF_TILE_COST)));
         x = x1 = C;
         if (whole || cta >= P) return;
         x = C * cta / P; x1 = C * (cta + 1) / P;
         if (x >= x1) return;
         // the item at x; the longest query tile of a head is the first: tile qt lies at [F - cost_before(qt + 1), F - cost_before(qt))
         seq = last_not_above(tab.cost, x);
-        const PfTiles ti(tab.len[seq], tab.n[seq], m);
+        const Tiles ti(tab.len[seq], tab.n[seq], m);
         const int64_t F = ti.cost_before(ti.nq), in_seq = x - tab.cost[seq];
         hk = (int)(in_seq / F);
         const int64_t z = F - (in_seq - hk * F);
@@ -206,7 +213,7 @@ struct PfWalk {
                 ++round;
                 if (idx >= total) continue;
                 const int seq = last_not_above(tab.items, idx);
-                const PfTiles ti(tab.len[seq], tab.n[seq], m);
+                const Tiles ti(tab.len[seq], tab.n[seq], m);
                 // heads in groups whose K and V the L2 holds, within a group the longest query tiles first
                 const int group = (int)max((int64_t)1, min((int64_t)Hkv, PF_L2_BYTES / (head_bytes * max(1, tab.len[seq]))));
                 int l = idx - tab.items[seq];
@@ -221,11 +228,11 @@ struct PfWalk {
             return false;
         }
         while (x < x1) {
-            const PfTiles ti(tab.len[seq], tab.n[seq], m);
+            const Tiles ti(tab.len[seq], tab.n[seq], m);
             const int tiles = ti.tiles(qt), weight = ti.weight(qt);
-            const int64_t end = start + PF_ITEM_COST + (int64_t)weight * tiles;
-            const int k0 = (int)(max((int64_t)0, x - start - PF_ITEM_COST) / weight);
-            const int k1 = (int)(max((int64_t)0, min(x1, end) - start - PF_ITEM_COST) / weight);
+            const int64_t end = start + ITEM_COST + (int64_t)weight * tiles;
+            const int k0 = (int)(max((int64_t)0, x - start - ITEM_COST) / weight);
+            const int k1 = (int)(max((int64_t)0, min(x1, end) - start - ITEM_COST) / weight);
             if (k1 > k0) {                     // (else the share has no whole tile of the item)
                 fill(it, seq, hk, qt);
                 clip(it, k0, k1);
@@ -442,7 +449,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
             if (n > len) flags |= ETA_DEV_EMPTY_ROW;
             tab.row0[i] = r0; tab.n[i] = n; tab.len[i] = len;
             tab.items[i] = items; tab.cost[i] = cost;
-            const PfTiles ti(len, n, PF_ROWS >> a.g_shift);
+            const PfTiles<PF_ITEM_COST<GATED>> ti(len, n, PF_ROWS >> a.g_shift);
             items += ti.nq * a.Hkv;
             cost += a.Hkv * ti.cost_before(ti.nq);
             if (n) longest = max(longest, ti.weight(ti.nq - 1) * ti.tiles(ti.nq - 1));
@@ -469,7 +476,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
     __syncthreads();
     pf_fence_after();
     const uint32_t tmem = s_tmem;
-    PfWalk walk(tab, a.batch, a.Hkv, a.g_shift, D, blockIdx.x, gridDim.x);
+    PfWalk<PF_ITEM_COST<GATED>> walk(tab, a.batch, a.Hkv, a.g_shift, D, blockIdx.x, gridDim.x);
     PfItem it;
     bool ok = true;
 
@@ -1051,23 +1058,15 @@ static int pf_launch(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUten
     return launch_pdl("eta_prefill", prefill_join_kernel<D>, dim3(ctas, PF_ROWS / PF_JOIN_ROWS), dim3(32 * PF_JOIN_WARPS), 0, s, a);
 }
 
-}  // namespace eta
-
-extern "C" {
-
-// Host-only check of how work is shared out: for made-up lengths every tile of every item is in exactly one share, the parts of a split
-// item have slots of their own, in order, and whoever has the first part knows their number.  Not part of the public interface; called by the
-// CPU test-suite.  n, len: [batch] new tokens and tokens cached.  -> 0, or the number of the first expectation that failed.
-int eta_selftest_prefill_shares(int batch, int n_kv_heads, int g_shift, int head_dim, int ctas, const int32_t* n, const int32_t* len,
-                                int* whole) {
-    using namespace eta;
+template <int ITEM_COST>
+static int check_shares(int batch, int n_kv_heads, int g_shift, int head_dim, int ctas, const int32_t* n, const int32_t* len, int* whole) {
     static PfTables tab;
     const int m = PF_ROWS >> g_shift;
     tab.longest = 0;
     tab.items[0] = 0; tab.cost[0] = 0;
     int rows = 0;
     for (int i = 0; i < batch; ++i) {
-        const PfTiles ti(len[i], n[i], m);
+        const PfTiles<ITEM_COST> ti(len[i], n[i], m);
         tab.row0[i] = rows; tab.n[i] = n[i]; tab.len[i] = len[i];
         rows += n[i];
         tab.items[i + 1] = tab.items[i] + ti.nq * n_kv_heads;
@@ -1076,7 +1075,7 @@ int eta_selftest_prefill_shares(int batch, int n_kv_heads, int g_shift, int head
         for (int t = 0; t < ti.nq; ++t) {
             if (ti.cost_before(t) != sum) return 1;
             tab.longest = std::max(tab.longest, ti.weight(t) * ti.tiles(t));
-            sum += (int64_t)ti.weight(t) * ti.tiles(t) + PF_ITEM_COST;
+            sum += (int64_t)ti.weight(t) * ti.tiles(t) + ITEM_COST;
         }
         if (ti.cost_before(ti.nq) != sum) return 2;
     }
@@ -1084,7 +1083,7 @@ int eta_selftest_prefill_shares(int batch, int n_kv_heads, int g_shift, int head
     struct Seen { int next = 0, parts = 0, said = 0, last = -2; };
     std::vector<Seen> seen((size_t)rows * n_kv_heads + 1);
     for (int c = 0; c < ctas; ++c) {
-        PfWalk w(tab, batch, n_kv_heads, g_shift, head_dim, c, ctas);
+        PfWalk<ITEM_COST> w(tab, batch, n_kv_heads, g_shift, head_dim, c, ctas);
         *whole = w.whole;
         PfItem it;
         int starts = 0;
@@ -1122,6 +1121,20 @@ int eta_selftest_prefill_shares(int batch, int n_kv_heads, int g_shift, int head
                 if (!s.parts || s.parts != s.said || s.next != all) return 10;
             }
     return 0;
+}
+
+}  // namespace eta
+
+extern "C" {
+
+// Host-only check of how work is shared out: for made-up lengths every tile of every item is in exactly one share, the parts of a split
+// item have slots of their own, in order, and whoever has the first part knows their number.  Not part of the public interface; called by the
+// CPU test-suite.  n, len: [batch] new tokens and tokens cached.  -> 0, or the number of the first expectation that failed.
+int eta_selftest_prefill_shares(int batch, int n_kv_heads, int g_shift, int head_dim, int ctas, const int32_t* n, const int32_t* len,
+                                int* whole) {
+    int gated_whole;
+    const int rc = eta::check_shares<eta::PF_ITEM_COST<true>>(batch, n_kv_heads, g_shift, head_dim, ctas, n, len, &gated_whole);
+    return rc ? rc : eta::check_shares<eta::PF_ITEM_COST<false>>(batch, n_kv_heads, g_shift, head_dim, ctas, n, len, whole);
 }
 
 int eta_prefill_workspace_bytes(const eta_cache_desc* desc, size_t* out_bytes) {
