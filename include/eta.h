@@ -459,7 +459,8 @@ int eta_decode_kv4(const eta_cache_desc* desc, const eta_kv4_desc* kv4, const et
  * Rows that do not count, and those behind the last sequence, are left as they are.  A row whose position is negative (more new tokens
  * than seq_lens) sees nothing: zeros, and ETA_DEV_EMPTY_ROW.  A length past t_cap is clamped (ETA_DEV_LEN_CLAMPED).
  * Cache: contiguous, or with `pages` not NULL paged, as for eta_decode; table entries behind the last token are not read.  What the cache
- * holds behind a row's position, NaN and infinities included, does not reach the row.
+ * holds behind a row's position, NaN and infinities included, does not reach the row.  An infinite value that a row sees arrives as itself, or as
+ * NaN where its weight underflows.
  * bf16 operands, fp32 scores and sums; weights enter the second product as bf16 (2^-8 of each, as much as rounding the output).
  * Deterministic for a given device.  batch <= 1024, n_kv_heads <= 1024, n_rows <= 2^30; nb_cap is not looked at.
  * Two kernels, launched with programmatic dependent launch: the first waits for everything before it in the stream before it reads or

@@ -402,7 +402,10 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
              *const o_full = p_full + 2 * PF_CHUNKS, *const drained = o_full + 2;
     __shared__ uint32_t s_tmem;
     __shared__ int s_dead;
-    __shared__ int s_poison[16];               // item (counted from 1) of whose tiles values were taken out
+    // The item of whose tiles values were taken out, of those with tiles, counted from 1.  The cleaning warps are no more such items ahead of the
+    // epilogue than the ring has tiles.
+    __shared__ int s_poison[16];
+    static_assert(NSTAGE / 2 + 1 < 16, "an item's mark would be overwritten before it is read");
     __shared__ int64_t s_scan[PF_WARPS][2];
     __shared__ float s_x[2][PF_ROWS];          // what the two threads of a row tell each other
     __shared__ float2 s_twin[PF_HALF];         // maximum and sum of a twin item's second half
@@ -660,8 +663,8 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
             int item = 0;
             const int w = warp - PF_CLEAN;             // which half of the tile's rows
             while (ok && walk.next(it)) {
-                ++item;
                 const int n = max(0, it.k1 - it.k0);
+                item += n > 0;
                 for (int j = 0; j < n; ++j) {
                     ++fill;                            // K's
                     const int stage = fill % NSTAGE;
@@ -724,7 +727,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
         uint32_t s_n = 0, o_n = 0;
         int item = 0;
         while (ok && walk.next(it)) {
-            ++item;
+            item += it.k1 > it.k0;
             const int tok0 = it.twin ? 0 : half * HT, rows = min(max(it.n_tok - tok0, 0), HT) << a.g_shift;
             if (!rows) continue;
             const int n = it.n(half);

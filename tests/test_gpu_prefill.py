@@ -214,6 +214,33 @@ def test_infinities_of_both_signs_in_a_split_item():
     assert torch.isfinite(out[0, :, 5:].float()).all()
 
 
+@pytest.mark.parametrize("gated,size", [(False, 1.0), (True, 1.0), (True, 1e13)])
+def test_infinities_on_both_sides_of_a_sequence_that_sees_nothing(gated, size):
+    """A long sequence, one whose row has no tokens at all, a short one, over and over: what was taken out of the long one's last tile is not
+    forgotten over the short one's, which may be there before the long one's end (with 15 heads they are 16 items apart).  Scores of 10^13: weights
+    underflow, and 0 * inf is NaN where the parts of an item are joined; what was forgotten would be finite."""
+    H, G, times = 15, 8, 100
+    new, lens = [32, 1, 32] * times, [2040, 0, 40] * times
+    starts = [0]
+    for n in new:
+        starts.append(starts[-1] + n)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    K, V = (torch.randn((3 * times, H, 2048, 64), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    V[::3, :, 2030, 5] = V[2::3, :, 35, 5] = math.inf
+    q = (torch.randn((starts[-1], H * G, 64), generator=gen, device="cuda") * size).bfloat16()
+    p = torch.cat([torch.arange(t - n, t) for n, t in zip(new, lens)]).cuda()          # the rows' positions
+    at = torch.cat([torch.full((n,), 2030 if t > 40 else 35) for n, t in zip(new, lens)]).cuda()
+    desc = eb.cache_desc(K, V, H * G, 64)
+    ws, out, starts, lens, const = workspace(desc), torch.zeros_like(q), ints(starts), ints(lens), torch.zeros(H * G, device="cuda")
+    for _ in range(5):
+        out.fill_(CANARY)
+        eb.eta_prefill(desc, eb.DecodeParams() if gated else DENSE, q, K, V, starts, lens, out, ws, head_const=const if gated else None)
+        got = out[p >= at][:, :, 5].float()
+        assert (got == math.inf).all() if size == 1.0 else not torch.isfinite(got).any()
+        assert torch.isfinite(out[p < at].float()).all() and torch.all(out[p < 0] == 0)
+        assert torch.isfinite(out[:, :, 6:].float()).all()
+
+
 @pytest.mark.parametrize("new,n", [(40, 5), (300, 5), (3, 3)])
 def test_more_new_tokens_than_the_sequence_has(new, n):
     """The first rows stand before the sequence's first token: zeros, and a flag."""
