@@ -458,7 +458,7 @@ int eta_decode_kv4(const eta_cache_desc* desc, const eta_kv4_desc* kv4, const et
  * Exactly one of tau / head_const unless ETA_FLAG_DENSE, which looks at neither.  z, lwb and rescue_window are not looked at.
  * Rows that do not count, and those behind the last sequence, are left as they are.  A row whose position is negative (more new tokens
  * than seq_lens) sees nothing: zeros, and ETA_DEV_EMPTY_ROW.  A length past t_cap is clamped (ETA_DEV_LEN_CLAMPED).
- * Cache: contiguous, or with `pages` not NULL paged, as for eta_decode; table entries behind the last token are not read.  What the cache
+ * Cache: contiguous, or with `pages` not NULL paged, as for eta_decode; table entries behind the last token are not read, a page outside the pool reads as zeros.  What the cache
  * holds behind a row's position, NaN and infinities included, does not reach the row.  An infinite value that a row sees arrives as itself, or as
  * NaN where its weight underflows.
  * bf16 operands, fp32 scores and sums; weights enter the second product as bf16 (2^-8 of each, as much as rounding the output).

@@ -77,7 +77,7 @@ struct PrefillArgs {
     int4* desc;                            // [PF_MAX_CTAS] the split item that starts in a CTA's share: parts, first row, tokens, KV head
     uint32_t* status;
     float a, beta, scale, unit;            // unit: log2 e of what maxima are kept in
-    int batch, Hq, Hkv, g_shift, b_shift, t_cap, n_rows, table_stride, ungate;
+    int batch, Hq, Hkv, g_shift, b_shift, t_cap, n_rows, table_stride, n_pages, ungate;
 };
 
 // ------------------------------------------------------------------------------------------------ work items
@@ -932,9 +932,12 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                 if (poison) {
                     const int end = (int)min((int64_t)p + 1, (int64_t)it.k1 * PF_TILE);
                     for (int t = max(it.clean0, it.k0) * PF_TILE; t < end; ++t) {
-                        const int64_t base = a.block_table
-                            ? (int64_t)__ldcg(a.block_table + (int64_t)it.seq * a.table_stride + (t >> a.b_shift)) * a.v_sb + (int64_t)(t & ((1 << a.b_shift) - 1)) * a.v_st
-                            : (int64_t)it.seq * a.v_sb + (int64_t)t * a.v_st;
+                        int64_t base = (int64_t)it.seq * a.v_sb + (int64_t)t * a.v_st;
+                        if (a.block_table) {
+                            const int page = __ldcg(a.block_table + (int64_t)it.seq * a.table_stride + (t >> a.b_shift));
+                            if (page < 0 || page >= a.n_pages) continue;       // the copies read zeros there
+                            base = (int64_t)page * a.v_sb + (int64_t)(t & ((1 << a.b_shift) - 1)) * a.v_st;
+                        }
                         const uint4* const from = reinterpret_cast<const uint4*>(a.V + base + it.hk * a.v_sh + part * DW + k);
 #pragma unroll
                         for (int u = 0; u < 4; ++u) {
@@ -1196,6 +1199,7 @@ int eta_prefill(const eta_cache_desc* desc, const eta_page_table* pages, const e
     a.row_start = row_start; a.seq_lens = seq_lens; a.granted = granted;
     a.block_table = pages ? pages->block_table : nullptr;
     a.table_stride = pages ? pages->table_stride : 0;
+    a.n_pages = n_pages;
     a.tau = tau; a.head_const = head_const;
     a.V = static_cast<const __nv_bfloat16*>(V);
     a.v_sb = desc->v_stride_b; a.v_sh = desc->v_stride_h; a.v_st = desc->v_stride_t;

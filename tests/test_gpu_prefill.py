@@ -241,6 +241,25 @@ def test_infinities_on_both_sides_of_a_sequence_that_sees_nothing(gated, size):
         assert torch.isfinite(out[:, :, 6:].float()).all()
 
 
+@pytest.mark.parametrize("bad", [-1, 0])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_page_outside_the_pool_reads_as_zeros(d, bad):
+    """Next to an infinity that is taken out of the same tile and added again: the page's values are not looked for then either."""
+    s = make([60], [200], 2, 4, d, 32, True, seed=21)
+    s["V"][s["table"][0, 7].item(), :, 16, 7] = math.inf             # token 240, of the tile of 128 .. 255
+    pages = s["K"].shape[0]
+    spare = [i for i in range(pages) if i not in s["table"][0, :9].tolist()][0]
+    s["K"][spare], s["V"][spare] = 0, 0
+    for block in (6, 1):
+        s["table"][0, block] = spare
+    want, _ = call(s, DENSE)
+    for block in (6, 1):
+        s["table"][0, block] = bad if bad < 0 else pages + block
+    out, status = call(s, DENSE)
+    assert status == 0 and torch.equal(out, want)
+    assert (out[40:, :, 7].float() == math.inf).all() and torch.isfinite(out[:40].float()).all()
+
+
 @pytest.mark.parametrize("new,n", [(40, 5), (300, 5), (3, 3)])
 def test_more_new_tokens_than_the_sequence_has(new, n):
     """The first rows stand before the sequence's first token: zeros, and a flag."""
