@@ -22,7 +22,8 @@
 // there is tensor memory for two halves' chains, not three.  Tensor core and special function unit have 2048 cycles of work a tile each and are
 // busy 51 % of the time.  One 8K prompt of 32 / 8 heads of 128 takes 530 to 600 us, 32K 7.7 to 8.9 ms (1.0 to 1.1 PFLOP/s; by the power limit).  With parts
 // taken out 32K takes 6.3 to 6.8 ms without the products, as much without the softmax, 3.8 without both and without copies.  Gated scores take
-// one and a half more special functions each (65 % busy) and 930 instructions a thread and tile instead of 490: 11 packed prompts to 5K 1.03 ms (520 TFLOP/s).
+// one and a quarter more special functions each (60 to 68 % busy) and 960 instructions a thread and tile instead of 490: 11 packed prompts to 5K
+// 1.00 ms (530 TFLOP/s; with a reciprocal for two gates instead of four 1.03), 2 x 1111 tokens behind 32K at head_dim 64 650 us (320 TFLOP/s).
 // 64 single tokens behind 16K stream at 6.0 TB/s.
 // Tried, for the 32K prompt: a thread per row and eight softmax warps 8.4 to 9.4 ms; a warp for each half's MMAs, free 10.3, taking turns 8.9 (the
 // halves fall into step; a token for the special function unit keeps them apart and costs what it gains); a quarter of the exponentials as polynomials on the fp32
@@ -767,7 +768,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                             for (int k = 0; k < 32; k += 8)
 #pragma unroll
                                 for (int u = 0; u < 4; ++u) am[u] = pf_max3(am[u], fabsf(s[k + u]), fabsf(s[k + u + 4]));
-                            if (__any_sync(0xffffffffu, !(pf_max3(fmaxf(am[0], am[1]), am[2], am[3]) * sl2 < 0x1p40f))) {
+                            if (__any_sync(0xffffffffu, !(pf_max3(fmaxf(am[0], am[1]), am[2], am[3]) * sl2 < 0x1p11f))) {
 #pragma unroll
                                 for (int k = 0; k < 32; ++k) {
                                     const float x = s[k] * sl2, gate = pf_rcp(1.f + pf_ex2(fmaf(s[k], -kb, tb)));
@@ -779,14 +780,18 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                                     float x[8], e[8], r[4];
 #pragma unroll
                                     for (int k = 0; k < 8; k += 2) pf_fma2(e[k], e[k + 1], s[k0 + k], s[k0 + k + 1], -kb, tb);
-                                    // Both reciprocals of a pair from the one of their product.  So that it stays finite a gate is no smaller than
-                                    // 2^-62: a score below 2^40 then counts as 0 all the same.
+                                    // The reciprocals of four from the one of their product.  So that it stays finite a gate is no smaller than
+                                    // 2^-31: a score below 2^11 then counts as 0 all the same (2^-20 of a weight).
 #pragma unroll
-                                    for (int k = 0; k < 8; ++k) e[k] = pf_ex2(fminf(e[k], 62.f));
+                                    for (int k = 0; k < 8; ++k) e[k] = pf_ex2(fminf(e[k], 31.f));
 #pragma unroll
                                     for (int k = 0; k < 8; k += 2) { add2(e[k], e[k + 1], 1.f, 1.f); mul2(x[k], x[k + 1], s[k0 + k], s[k0 + k + 1], sl2, sl2); }
 #pragma unroll
-                                    for (int k = 0; k < 8; k += 2) r[k / 2] = pf_rcp(e[k] * e[k + 1]);
+                                    for (int k = 0; k < 8; k += 4) {
+                                        const float p0 = e[k] * e[k + 1], p1 = e[k + 2] * e[k + 3], both = pf_rcp(p0 * p1);
+                                        r[k / 2] = both * p1;
+                                        r[k / 2 + 1] = both * p0;
+                                    }
 #pragma unroll
                                     for (int k = 0; k < 8; k += 2) mul2(e[k + 1], e[k], x[k], x[k + 1], e[k + 1], e[k]);
 #pragma unroll

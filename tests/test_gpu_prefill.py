@@ -170,6 +170,15 @@ def test_gate_at_its_ends(te, beta):
         check(s, eb.DecodeParams(beta=beta), const=const)
 
 
+@pytest.mark.parametrize("size", [30.0, 300.0, 3e4, 1e12])
+@pytest.mark.parametrize("te", [0.0, 2000.0])
+def test_gate_of_large_scores(size, te):
+    """Scores on both sides of 2^11, up to which four gates share a reciprocal and none is smaller than 2^-31 (|S| 2^-31, within the bound)."""
+    s = make([140], [60], 1, 4, 128, 64, False, seed=22)
+    s["q"] = (s["q"].float() * size).bfloat16()
+    check(s, eb.DecodeParams(beta=0.5), const=torch.full((4,), te, device="cuda"))
+
+
 def test_a_threshold_that_is_nan_is_a_row_that_is_nan():
     s = make([70], [0], 1, 4, 128, 64, False, seed=9)
     tau = torch.zeros((70, 4), device="cuda")
