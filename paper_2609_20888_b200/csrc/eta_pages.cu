@@ -340,8 +340,9 @@ struct CopyArgs {
     uint32_t* status;
 };
 
-// A page of all pools is cut into pieces of 32 KB, which the CTAs take in turns.  Bound by memory: 2 x 186 MB (1.4 thousand pages of 128 KB)
-// in 70 us, 5.3 TB/s.
+// A page of all pools is cut into pieces of 32 KB, which the CTAs take in turns.  Bound by memory: some
+// 371 MB (read and written) in 60 us, 6.2 TB/s.  Other numbers of CTAs, threads and loads under way: moves 83 to 89 us in all instead of 85, forks 148
+// to 167 instead of 144; with streaming hints 93 and 205.
 __global__ void __launch_bounds__(PC_THREADS) copy_pages_kernel(const __grid_constant__ CopyArgs a) {
     pdl_wait();
     const int n = a.n_moves ? pg_clamped(__ldcg(a.n_moves), a.max_moves) : a.max_moves, per = a.first[a.n_pools];
