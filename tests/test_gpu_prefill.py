@@ -364,3 +364,25 @@ def test_offsets_past_two_to_the_31():
         # 2 M additions of about one in fp32, several partial sums of 2^13 or fewer tiles: 2^-24 times a few thousand at most
         assert ((out[r].double().view(4, 2, d) - want).abs() <= (2 * 2.0 ** -8 + 2.0 ** -10) * mass + 1e-9).all()
     assert torch.all(out[:130] == 0)
+
+
+def test_two_calls_at_once():
+    """On two streams, each with a workspace of its own, split items in both: what either gives alone."""
+    both = [make([300, 1, 45], [900, 3000, 0], 2, 4, 128, 64, True, seed=23), make([77, 1], [5000, 4000], 4, 2, 64, 32, False, seed=24)]
+    want = [call(s, DENSE)[0] for s in both]
+    streams = [torch.cuda.Stream() for _ in both]
+    args = []
+    for s in both:
+        if s["paged"]:
+            desc, pages = eb.paged_cache_desc(s["K"], s["V"], s["B"], s["Hq"], t_cap=s["NB"] * s["b"]), eb.page_table(s["table"], s["K"].shape[0])
+        else:
+            desc, pages = eb.cache_desc(s["K"], s["V"], s["Hq"], s["b"]), None
+        args.append((desc, pages, ints(s["starts"]), ints(s["lens"]), workspace(desc), [torch.full_like(s["q"], CANARY) for _ in range(10)]))
+    torch.cuda.synchronize()
+    for k in range(10):
+        for s, stream, (desc, pages, starts, lens, ws, outs) in zip(both, streams, args):
+            with torch.cuda.stream(stream):
+                eb.eta_prefill(desc, DENSE, s["q"], s["K"], s["V"], starts, lens, outs[k], ws, pages=pages)
+    torch.cuda.synchronize()
+    for w, a in zip(want, args):
+        assert all(torch.equal(w, x) for x in a[-1])
