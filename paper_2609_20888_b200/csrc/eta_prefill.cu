@@ -59,6 +59,7 @@ constexpr int PF_MAX_BATCH = 1024;         // sequences whose prefix sums a CTA 
 // an item's own cost is worth half as many of them.  As measured: 64 requests, most of them single tokens, with 4, 3, 2 for the second 1427,
 // 1228, 1322 us; with 4, 8, 16, 24, 32 for the last an 8K prompt 644, 605, 558, 579, 586 us, 11 gated prompts 1036, 1034, 1101, 1172, 1205 us.
 constexpr int PF_TILE_COST = 4, PF_TWIN_COST = 3, PF_SPLIT_COST = 16;
+constexpr int PF_WHOLE_TOKENS = PF_TILE * (PF_SPLIT_COST / PF_TILE_COST);    // no item that sees at most so many tokens is ever split: see PfWalk
 template <bool GATED> constexpr int PF_ITEM_COST = GATED ? 8 : 16;
 constexpr int64_t PF_L2_BYTES = 64ll << 20;     // K and V of the heads that are worked on side by side
 // registers: 640 threads start with 96; 512 of them take 104, the others 64 (together what the block was launched with)
@@ -85,21 +86,28 @@ struct PrefillArgs {
 
 #define PF_BOTH __host__ __device__ __forceinline__
 
-// Tiles of K that query tile t of a sequence needs, and what all before it need, for n new tokens behind ctx; m tokens per query tile.
+// Tiles of K that query tile t of a sequence needs, and what all before it need, for the n newest of len tokens; m tokens per query tile.
+// Where n > len the first rows stand before the sequence's first token and see nothing: query tiles of such rows alone have no tiles.
 template <int ITEM_COST>
 struct PfTiles {
-    int nq, m, n, base;
+    int nq, m, n, p0, blind;               // p0: position of the first token; blind: query tiles that see nothing, as far as they are whole
     PF_BOTH PfTiles(int len, int n_, int m_) {
         n = n_; m = m_;
         nq = (n + m - 1) / m;
-        base = max(len - n, 0);
+        p0 = len - n;
+        blind = p0 < 0 ? -p0 / m : 0;
     }
-    PF_BOTH int tiles(int t) const { return (int)(((int64_t)base + min((int64_t)(t + 1) * m, (int64_t)n) + PF_TILE - 1) / PF_TILE); }
+    PF_BOTH int tiles(int t) const {
+        const int64_t end = p0 + min((int64_t)(t + 1) * m, (int64_t)n);
+        return end > 0 ? (int)((end + PF_TILE - 1) / PF_TILE) : 0;
+    }
     // what a tile of query tile t counts
     PF_BOTH int weight(int t) const { return t == nq - 1 && 2 * (n - t * m) <= m ? PF_TWIN_COST : PF_TILE_COST; }
     // sum of the tiles of the first t query tiles, t < nq (the last one may be shorter)
     PF_BOTH int64_t before(int t) const {
-        const int64_t b0 = (int64_t)base + m + PF_TILE - 1;
+        t -= blind;
+        if (t <= 0) return 0;
+        const int64_t b0 = (int64_t)p0 + (int64_t)blind * m + m + PF_TILE - 1;         // at least PF_TILE
         if (m >= PF_TILE) return t * (b0 / PF_TILE) + (int64_t)(m / PF_TILE) * t * (t - 1) / 2;
         const int p = PF_TILE / m, U = t / p, R = t % p;
         int64_t sum = (int64_t)p * U * (U - 1) / 2 + (int64_t)R * U;
@@ -234,7 +242,9 @@ struct PfWalk {
             const int64_t end = start + ITEM_COST + (int64_t)weight * tiles;
             const int k0 = (int)(max((int64_t)0, x - start - ITEM_COST) / weight);
             const int k1 = (int)(max((int64_t)0, min(x1, end) - start - ITEM_COST) / weight);
-            if (k1 > k0) {                     // (else the share has no whole tile of the item)
+            // an item without tiles is done where it starts; of others the share may have no whole tile
+            const bool here = k1 > k0 || (!tiles && x == start);
+            if (here) {
                 fill(it, seq, hk, qt);
                 clip(it, k0, k1);
                 it.slot = -1; it.pieces = 0;
@@ -253,7 +263,7 @@ struct PfWalk {
                 }
                 if (seq < batch) qt = (tab.n[seq] + m - 1) / m - 1;
             }
-            if (k1 > k0) return true;
+            if (here) return true;
         }
         return false;
     }
@@ -1064,8 +1074,7 @@ static int pf_launch(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUten
     if (attr.numRegs < PF_REGS) return ETA_ERR_UNSUPPORTED;
     const int rc = launch_pdl("eta_prefill", prefill_kernel<D, GATED>, dim3(ctas), dim3(PF_THREADS), PfSmem<D>::BYTES, s, tmQ, tmK, tmV, a);
     if (rc != ETA_OK) return rc;
-    // (no item of at most so many tiles is ever split: see PfWalk)
-    if (a.t_cap <= PF_TILE * (PF_SPLIT_COST / PF_TILE_COST)) return ETA_OK;
+    if (a.t_cap <= PF_WHOLE_TOKENS) return ETA_OK;         // nothing to join
     return launch_pdl("eta_prefill", prefill_join_kernel<D>, dim3(ctas, PF_ROWS / PF_JOIN_ROWS), dim3(32 * PF_JOIN_WARPS), 0, s, a);
 }
 
@@ -1075,8 +1084,9 @@ static int check_shares(int batch, int n_kv_heads, int g_shift, int head_dim, in
     const int m = PF_ROWS >> g_shift;
     tab.longest = 0;
     tab.items[0] = 0; tab.cost[0] = 0;
-    int rows = 0;
+    int rows = 0, longest = 0;             // the longest sequence, the least t_cap
     for (int i = 0; i < batch; ++i) {
+        longest = std::max(longest, len[i]);
         const PfTiles<ITEM_COST> ti(len[i], n[i], m);
         tab.row0[i] = rows; tab.n[i] = n[i]; tab.len[i] = len[i];
         rows += n[i];
@@ -1111,15 +1121,14 @@ static int check_shares(int batch, int n_kv_heads, int g_shift, int head_dim, in
                 continue;
             }
             if (it.slot != 2 * c && it.slot != 2 * c + 1) return 6;
+            if (longest <= PF_WHOLE_TOKENS || !got) return 12;
             if (it.slot == 2 * c + 1) {
                 if (it.k0 != 0 || s.parts || ++starts > 1 || it.pieces < 2 || c + it.pieces > ctas) return 7;
                 s.said = it.pieces;
-            } else if (!s.parts || it.k0 < s.next || s.last != c - 1) {
+            } else if (!s.parts || it.k0 != s.next || s.last != c - 1) {
                 return 8;
             }
-            // (a gap is allowed only behind the tiles that count: positions before the sequence's first token)
-            if (it.k0 > s.next && s.next < all) return 9;
-            if (got) s.next = it.k1;
+            s.next = it.k1;
             s.last = c;
             ++s.parts;
         }
@@ -1140,7 +1149,7 @@ extern "C" {
 
 // Host-only check of how work is shared out: for made-up lengths every tile of every item is in exactly one share, the parts of a split
 // item have slots of their own, in order, and whoever has the first part knows their number.  Not part of the public interface; called by the
-// CPU test-suite.  n, len: [batch] new tokens and tokens cached.  -> 0, or the number of the first expectation that failed.
+// CPU test-suite.  Where the second kernel is not launched, no item is split.  n, len: [batch] new tokens and tokens cached.  -> 0, or the number of the first expectation that failed.
 int eta_selftest_prefill_shares(int batch, int n_kv_heads, int g_shift, int head_dim, int ctas, const int32_t* n, const int32_t* len,
                                 int* whole) {
     int gated_whole;
