@@ -894,7 +894,9 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
             // In a twin item both halves have the row: the second hands over what it has, through the queries' place (a column's rows side by side).
             float* const hand = reinterpret_cast<float*>(smem) + part * DW * PF_HALF + row;
             float l = (l0 + l1) + (l2 + l3), keep = 1.f, take = 0.f;               // what either half's sums count
-            if (live) {
+            // Without tiles there is nothing to tell (l is the same in both threads), and it would be told over what a slow partner has yet to read of
+            // the item before: only items with tiles meet again, at their first maximum, before the next of them is told anything.
+            if (live && n) {
                 *tell = l;
                 if (pf_any_of<2>(!ok, pair)) ok = false;
                 l = part ? *told + l : l + *told;
