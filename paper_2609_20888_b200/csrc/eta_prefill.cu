@@ -392,7 +392,7 @@ struct PfSmem {
     static constexpr int RING = 2 * Q_BYTES;
     static constexpr int TABLES = RING + NSTAGE * STAGE;
     static constexpr int BARS = TABLES + (int)((sizeof(PfTables) + 15) / 16 * 16);
-    static constexpr int N_BARS = 3 * NSTAGE + 2 * (4 + PF_CHUNKS) + 1;
+    static constexpr int N_BARS = 3 * NSTAGE + 2 * (4 + PF_CHUNKS) + 1 + 4;
     static constexpr int BYTES = 1024 + BARS + 8 * N_BARS;
     static_assert(PF_CHUNKS == 2, "a chunk is 32 of a thread's columns");
     static_assert(BYTES <= 227 * 1024, "too much shared memory");
@@ -410,7 +410,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
     uint64_t* const full = reinterpret_cast<uint64_t*>(smem + L::BARS);
     uint64_t *const empty = full + NSTAGE, *const cleaned = empty + NSTAGE;
     uint64_t *const q_full = cleaned + NSTAGE, *const q_empty = q_full + 2, *const s_full = q_empty + 2, *const p_full = s_full + 2,
-             *const o_full = p_full + 2 * PF_CHUNKS, *const drained = o_full + 2;
+             *const o_full = p_full + 2 * PF_CHUNKS, *const drained = o_full + 2, *const handed = drained + 1;
     __shared__ uint32_t s_tmem;
     __shared__ int s_dead;
     // The item of whose tiles values were taken out, of those with tiles, counted from 1.  The cleaning warps are no more such items ahead of the
@@ -428,6 +428,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
         // (tiles of K and V take turns, so the odd stages hold V: the cleaning warps let go of those too)
         for (int k = 0; k < NSTAGE; ++k) { mbar_init(&full[k], 1); mbar_init(&empty[k], k & 1 ? 3 : 1); mbar_init(&cleaned[k], 2); }
         mbar_init(drained, 1);
+        for (int k = 0; k < 4; ++k) mbar_init(&handed[k], 2);
         for (int k = 0; k < 2; ++k) {
             mbar_init(&q_full[k], 1); mbar_init(&q_empty[k], 1 + PF_SOFTMAX_WARPS / 2); mbar_init(&s_full[k], 1);
             for (int c = 0; c < PF_CHUNKS; ++c) mbar_init(&p_full[k * PF_CHUNKS + c], PF_SOFTMAX_WARPS / 2);
@@ -735,7 +736,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
         float* const tell = &s_x[part][half * PF_HALF + row];
         const float* const told = &s_x[part ^ 1][half * PF_HALF + row];
         const float sl2 = a.scale * LOG2E, kb = a.scale * a.beta * LOG2E, unit = GATED ? 1.f : sl2;
-        uint32_t s_n = 0, o_n = 0;
+        uint32_t s_n = 0, o_n = 0, h_n = 0;
         int item = 0;
         while (ok && walk.next(it)) {
             item += it.k1 > it.k0;
@@ -878,7 +879,11 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                         pf_wait_st();
                         pf_fence_before();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(&p_full[half * PF_CHUNKS + g]);
+                        bool hands_over = lane == 0;
+#ifdef ETA_TEST_SKIP_WEIGHTS_ARRIVE
+                        hands_over = hands_over && (blockIdx.x || warp != 4);          // (a warp of the second half)
+#endif
+                        if (hands_over) mbar_arrive(&p_full[half * PF_CHUNKS + g]);
                     }
                 } else {
                     if (!ok) break;
@@ -886,8 +891,8 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                         for (int k = 0; k < PF_CHUNKS; ++k) mbar_arrive(&p_full[half * PF_CHUNKS + k]);
                 }
             }
-            if (!ok && !(live && it.twin)) break;
-            if (ok && n) ok = __all_sync(0xffffffffu, pf_wait(&o_full[half], o_n++ & 1, &s_dead));
+            if (!ok) break;
+            if (n) ok = __all_sync(0xffffffffu, pf_wait(&o_full[half], o_n++ & 1, &s_dead));
             pf_fence_after();
             const bool mine = row < rows, split = it.slot >= 0;
             const int64_t at_part = ((int64_t)it.slot * PF_ROWS + (it.twin ? 0 : half * PF_HALF) + row);
@@ -897,11 +902,14 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
             // Without tiles there is nothing to tell (l is the same in both threads), and it would be told over what a slow partner has yet to read of
             // the item before: only items with tiles meet again, at their first maximum, before the next of them is told anything.
             if (live && n) {
+                // The two warps of a row agree on whether a wait ran out: what both have waited for comes before they meet.  Halves do not meet: one may
+                // have left over an earlier item.
+                if (it.twin && !half && ok) ok = __all_sync(0xffffffffu, pf_wait(&handed[warp & 3], h_n++ & 1, &s_dead));
                 *tell = l;
                 if (pf_any_of<2>(!ok, pair)) ok = false;
                 l = part ? *told + l : l + *told;
-                if (it.twin) {
-                    if (half && ok) {
+                if (it.twin && ok) {
+                    if (half) {
 #pragma unroll 1
                         for (int k = 0; k < DW; k += 16) {
                             float o[16];
@@ -913,9 +921,9 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                         if (!part) s_twin[row] = make_float2(m, l);
                         pf_fence_before();
                         fence_proxy_async();
-                    }
-                    if (pf_any_of<4>(!ok, 9 + (warp & 3))) ok = false;
-                    if (!half) {
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&handed[warp & 3]);
+                    } else {
                         const float2 ml = s_twin[row];
                         const float M = fmaxf(m, ml.x);
                         if (M != -INFINITY) { keep = pf_ex2((m - M) * unit); take = pf_ex2((ml.x - M) * unit); }
