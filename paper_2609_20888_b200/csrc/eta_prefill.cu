@@ -500,13 +500,16 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
         if (warp == PF_COPY) {
             // -------------------------------------------------------------- copies
             uint32_t fill = 0, q_par = 0, q_some = 0;          // a bit per half: the parity of its next load, whether there was one
+            auto wait = [&](uint64_t* bar, uint32_t parity) {  // (the same answer in all lanes)
+                return ok = __all_sync(0xffffffffu, pf_wait(bar, parity, &s_dead));
+            };
             int4 split = make_int4(0, 0, 0, 0);
             while (ok && walk.next(it)) {
                 if (it.pieces > 1) split = make_int4(it.pieces, it.row0, it.n_tok, it.hk);
                 const int n = max(0, it.k1 - it.k0);
                 auto load_q = [&](int h) {
                     if (!ok || !it.n(h)) return;
-                    if (((q_some >> h) & 1) && !pf_wait(&q_empty[h], ((q_par >> h) & 1) ^ 1, &s_dead)) { ok = false; return; }
+                    if (((q_some >> h) & 1) && !wait(&q_empty[h], ((q_par >> h) & 1) ^ 1)) return;
                     q_some |= 1u << h;
                     q_par ^= 1u << h;
                     if (lane == 0) {
@@ -524,7 +527,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                 auto load_tile = [&](const CUtensorMap* tm, int j, int page) {
                     if (!ok) return;
                     const int stage = fill % NSTAGE;
-                    if (!pf_wait(&empty[stage], ((fill / NSTAGE) & 1) ^ 1, &s_dead)) { ok = false; return; }
+                    if (!wait(&empty[stage], ((fill / NSTAGE) & 1) ^ 1)) return;
                     ++fill;
                     int copies = HALVES, bytes = L::STAGE;
                     if (a.block_table) {
