@@ -559,17 +559,15 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                 }
             }
             if (lane == 0) a.desc[blockIdx.x] = split;
-            if (!ok) {
-                // give up: report, and let the copies that are on their way land before the shared memory is given back
-                if (lane == 0) {
-                    s_dead = 1;
-                    if (a.status) atomicOr(a.status, ETA_DEV_TIMEOUT);
-                }
-                for (uint32_t f = fill > NSTAGE ? fill - NSTAGE : 0; f < fill; ++f) mbar_wait(&full[f % NSTAGE], (f / NSTAGE) & 1);
-                for (int h = 0; h < 2; ++h)
-                    if ((q_some >> h) & 1) mbar_wait(&q_full[h], ((q_par >> h) & 1) ^ 1);
-            }
             pdl_trigger();
+            if (!ok && lane == 0) {
+                s_dead = 1;
+                if (a.status) atomicOr(a.status, ETA_DEV_TIMEOUT);
+            }
+            // The copies that are on their way land before the shared memory is given back: whoever they are for may have given up, or may yet.
+            for (uint32_t f = fill > NSTAGE ? fill - NSTAGE : 0; f < fill; ++f) mbar_wait(&full[f % NSTAGE], (f / NSTAGE) & 1);
+            for (int h = 0; h < 2; ++h)
+                if ((q_some >> h) & 1) mbar_wait(&q_full[h], ((q_par >> h) & 1) ^ 1);
         } else if (warp == PF_MMA) {
             // -------------------------------------------------------------- MMAs; the whole warp walks along, one lane issues
             // Every instruction between a wait and the MMAs behind it is time that the tensor core stands still: the warp takes some seven
