@@ -15,9 +15,11 @@ HEADER = os.path.join(os.path.dirname(HERE), "include", "eta.h")
 
 
 # Copies of the library for tests.  Two in which a consumer warp, of the streaming kernel and of prompt attention or of the one-kernel step,
-# skips a barrier arrival and the bounded waits are short (2^16 polls, a few milliseconds), so that a give-up path runs and can be checked.
+# skips a barrier arrival (and, of prompt attention, one last product is never announced) and the bounded waits are short (2^16 polls, a few
+# milliseconds), so that a give-up path runs and can be checked.
 GIVEUP_LIB = os.path.join(HERE, "libeta_b200_test_giveup.so")
-GIVEUP_FLAGS = ["-DETA_TEST_SKIP_FLUSH_ARRIVE", "-DETA_TEST_SKIP_WEIGHTS_ARRIVE", "-DETA_TEST_GENERAL_PATH", "-DETA_WAIT_LIMIT=65536"]
+GIVEUP_FLAGS = ["-DETA_TEST_SKIP_FLUSH_ARRIVE", "-DETA_TEST_SKIP_WEIGHTS_ARRIVE", "-DETA_TEST_SKIP_LAST_COMMIT", "-DETA_TEST_GENERAL_PATH",
+                "-DETA_WAIT_LIMIT=65536"]
 GIVEUP_STEP_LIB = os.path.join(HERE, "libeta_b200_test_giveup_step.so")
 GIVEUP_STEP_FLAGS = ["-DETA_TEST_SKIP_STAGE_ARRIVE", "-DETA_WAIT_LIMIT=65536"]
 # And one that takes the general path whatever the size: small problems reach its edges too.
