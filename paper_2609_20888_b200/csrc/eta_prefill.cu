@@ -778,6 +778,11 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                         const int here = nvis - 32 * g;
                         pf_wait_ld();
                         if constexpr (GATED) {
+                            // what the row does not see is out before anything is taken of several columns together
+                            if (edge) {
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) s[k] = k < here ? s[k] : 0.f;
+                            }
                             const int own = a.ungate ? here - 1 : -1;             // the column that stays raw
                             float am[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
