@@ -789,39 +789,47 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                             for (int k = 0; k < 32; k += 8)
 #pragma unroll
                                 for (int u = 0; u < 4; ++u) am[u] = pf_max3(am[u], fabsf(s[k + u]), fabsf(s[k + u + 4]));
-                            if (__any_sync(0xffffffffu, !(pf_max3(fmaxf(am[0], am[1]), am[2], am[3]) * sl2 < 0x1p11f))) {
+                            auto exact = [&](float sk) { return sk * sl2 * pf_rcp(1.f + pf_ex2(fmaf(sk, -kb, tb))); };
+                            auto eight = [&](int k0) {                         // stage by stage, so that chains run side by side
+                                float x[8], e[8], r[4];
 #pragma unroll
-                                for (int k = 0; k < 32; ++k) {
-                                    const float x = s[k] * sl2, gate = pf_rcp(1.f + pf_ex2(fmaf(s[k], -kb, tb)));
-                                    s[k] = k == own ? x : x * gate;
+                                for (int k = 0; k < 8; k += 2) pf_fma2(e[k], e[k + 1], s[k0 + k], s[k0 + k + 1], -kb, tb);
+                                // The reciprocals of four from the one of their product.  So that it stays finite a gate is no smaller than
+                                // 2^-31: a score below 2^11 then counts as 0 all the same (2^-20 of a weight).
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) e[k] = pf_ex2(fminf(e[k], 31.f));
+#pragma unroll
+                                for (int k = 0; k < 8; k += 2) { add2(e[k], e[k + 1], 1.f, 1.f); mul2(x[k], x[k + 1], s[k0 + k], s[k0 + k + 1], sl2, sl2); }
+#pragma unroll
+                                for (int k = 0; k < 8; k += 4) {
+                                    const float p0 = e[k] * e[k + 1], p1 = e[k + 2] * e[k + 3], both = pf_rcp(p0 * p1);
+                                    r[k / 2] = both * p1;
+                                    r[k / 2 + 1] = both * p0;
+                                }
+#pragma unroll
+                                for (int k = 0; k < 8; k += 2) mul2(e[k + 1], e[k], x[k], x[k + 1], e[k + 1], e[k]);
+#pragma unroll
+                                for (int k = 0; k < 8; k += 2) mul2(s[k0 + k], s[k0 + k + 1], e[k + 1], e[k], r[k / 2], r[k / 2]);
+                                if (edge) {
+#pragma unroll
+                                    for (int k = 0; k < 8; ++k) s[k0 + k] = k0 + k == own ? x[k] : s[k0 + k];
+                                }
+                            };
+                            // Which of the two a thread's scores take is a matter of its own row: a row's bits do not hang on its neighbours.
+                            const bool large = !(pf_max3(fmaxf(am[0], am[1]), am[2], am[3]) * sl2 < 0x1p11f);
+                            if (__any_sync(0xffffffffu, large)) {
+#pragma unroll
+                                for (int k0 = 0; k0 < 32; k0 += 8) {
+                                    float y[8];
+#pragma unroll
+                                    for (int k = 0; k < 8; ++k) y[k] = k0 + k == own ? s[k0 + k] * sl2 : exact(s[k0 + k]);
+                                    eight(k0);
+#pragma unroll
+                                    for (int k = 0; k < 8; ++k) s[k0 + k] = large ? y[k] : s[k0 + k];
                                 }
                             } else {
 #pragma unroll
-                                for (int k0 = 0; k0 < 32; k0 += 8) {           // stage by stage, so that chains run side by side
-                                    float x[8], e[8], r[4];
-#pragma unroll
-                                    for (int k = 0; k < 8; k += 2) pf_fma2(e[k], e[k + 1], s[k0 + k], s[k0 + k + 1], -kb, tb);
-                                    // The reciprocals of four from the one of their product.  So that it stays finite a gate is no smaller than
-                                    // 2^-31: a score below 2^11 then counts as 0 all the same (2^-20 of a weight).
-#pragma unroll
-                                    for (int k = 0; k < 8; ++k) e[k] = pf_ex2(fminf(e[k], 31.f));
-#pragma unroll
-                                    for (int k = 0; k < 8; k += 2) { add2(e[k], e[k + 1], 1.f, 1.f); mul2(x[k], x[k + 1], s[k0 + k], s[k0 + k + 1], sl2, sl2); }
-#pragma unroll
-                                    for (int k = 0; k < 8; k += 4) {
-                                        const float p0 = e[k] * e[k + 1], p1 = e[k + 2] * e[k + 3], both = pf_rcp(p0 * p1);
-                                        r[k / 2] = both * p1;
-                                        r[k / 2 + 1] = both * p0;
-                                    }
-#pragma unroll
-                                    for (int k = 0; k < 8; k += 2) mul2(e[k + 1], e[k], x[k], x[k + 1], e[k + 1], e[k]);
-#pragma unroll
-                                    for (int k = 0; k < 8; k += 2) mul2(s[k0 + k], s[k0 + k + 1], e[k + 1], e[k], r[k / 2], r[k / 2]);
-                                    if (edge) {
-#pragma unroll
-                                        for (int k = 0; k < 8; ++k) s[k0 + k] = k0 + k == own ? x[k] : s[k0 + k];
-                                    }
-                                }
+                                for (int k0 = 0; k0 < 32; k0 += 8) eight(k0);
                             }
                         }
                         if (edge) {
@@ -844,7 +852,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
                         *tell = mx;
                         if (pf_any_of<2>(!ok, pair)) { ok = false; break; }
                         mx = fmaxf(mx, *told);
-                        const float m_new = fmaxf(m, mx);
+                        const float m_new = (mx - m) * unit > PF_SLACK ? mx : m;      // (by the row's own scores, whoever of the others asked for it)
                         const float alpha = m == m_new ? 1.f : pf_ex2((m - m_new) * unit);
                         m = m_new;
                         l0 *= alpha; l1 *= alpha; l2 *= alpha; l3 *= alpha;

@@ -1,4 +1,5 @@
-"""A row of prompt attention has the bits that its own query, threshold and the tokens up to its position give it, whatever a page held before."""
+"""A row of prompt attention has the bits that its own query, threshold and the tokens up to its position give it, whatever else stands in the call: tokens behind
+it, what a page held before, other rows of the same tiles."""
 import math
 
 import pytest
@@ -26,6 +27,21 @@ def fill(x, what, seed):
 
 @pytest.mark.parametrize("mode", list(MODES))
 @pytest.mark.parametrize("what", ["other", "large", "huge", "nan", "inf", "zero"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_tokens_behind_a_row(mode, what, d):
+    s = make([300], [150], 1, 4, d, 64, False, seed=62)
+    kw = args(s, mode)
+    want, _ = call(s, MODES[mode], **kw)
+    for t in (445, 383, 300, 231, 170):
+        fill(s["K"][:, :, t:], what, t)
+        if what in ("other", "large", "huge", "zero"):
+            fill(s["V"][:, :, t:], what, t + 1)
+        out, _ = call(s, MODES[mode], **kw)
+        assert torch.equal(out[:t - 150], want[:t - 150]), (t, (out[:t - 150] != want[:t - 150]).any(2).sum().item())
+
+
+@pytest.mark.parametrize("mode", list(MODES))
+@pytest.mark.parametrize("what", ["other", "large", "huge", "nan", "inf", "zero"])
 @pytest.mark.parametrize("paged", [False, True])
 def test_what_a_page_held_before(mode, what, paged):
     """Behind the last token: of single tokens, of a chunk, of a share of a long one."""
@@ -40,3 +56,25 @@ def test_what_a_page_held_before(mode, what, paged):
                 fill(x[i, :, T:], what, i)
     out, _ = call(s, MODES[mode], **kw)
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("mode", list(MODES))
+@pytest.mark.parametrize("what", ["other", "large", "huge", "nan", "inf", "zero"])
+def test_other_rows(mode, what):
+    """Queries and thresholds of every third row change, rows that do not count among them: the others' outputs stay."""
+    s = make([50, 1, 21, 200], [100, 300, 7, 0], 2, 4, 128, 64, False, seed=64, pad=19, granted=[50, 1, 20, 200])
+    kw = args(s, mode)
+    want, _ = call(s, MODES[mode], **kw)
+    rows = torch.arange(s["q"].shape[0], device="cuda")
+    for k in range(3):
+        t = {**s, "q": s["q"].clone()}
+        x = torch.empty_like(t["q"][k::3])
+        fill(x, what, k)
+        t["q"][k::3] = x
+        kept = dict(kw)
+        if kw["tau"] is not None:
+            kept["tau"] = kw["tau"].clone()
+            kept["tau"][k::3] = x[..., 0].float()
+        out, _ = call(t, MODES[mode], **kept)
+        same = rows % 3 != k
+        assert torch.equal(out[same], want[same]), (out[same] != want[same]).any(2).sum().item()
