@@ -73,6 +73,16 @@ __device__ __forceinline__ void pg_refuse(bool refused, const PagesArgs& a) {
     if (__any_sync(0xffffffffu, refused) && (threadIdx.x & 31) == 0 && a.status) atomicOr(a.status, ETA_DEV_REFUSED);
 }
 
+// Counts as they come out; negative ones count as 0.
+template <int NT>
+__device__ __forceinline__ void pg_counts(const PagesArgs& a, int tid) {
+#pragma unroll 4
+    for (int p = tid; p < a.n_pages; p += NT) {
+        const int n = __ldcg(a.shared + p);
+        if (n < 0 || a.shared_out != a.shared) a.shared_out[p] = max(n, 0);
+    }
+}
+
 // Free pages by number: word w of the bits belongs to CTA w / per.  f(word's index, its bits, free pages before it).
 template <int N, typename F>
 __device__ __forceinline__ int pg_bits(const PagesArgs& a, int rank, int* s_warp, F f) {
@@ -114,10 +124,7 @@ __global__ void __launch_bounds__(PG_THREADS) free_pages_kernel(const PagesArgs 
     bool refused = false;
     pdl_wait();
     const int n_free = pg_clamped(__ldcg(a.n_free), a.n_pages);
-    for (int p = tid; p < a.n_pages; p += NT) {
-        const int n = __ldcg(a.shared + p);
-        if (n < 0 || a.shared_out != a.shared) a.shared_out[p] = max(n, 0);
-    }
+    pg_counts<NT>(a, tid);
     pg_sync<N>();
     // Everyone that lets go counts down, without looking: a count that ends below zero has nobody left.  (Looking at what each
     // atomic returns, 800 sequences took 54 us.)
@@ -213,8 +220,7 @@ __global__ void __launch_bounds__(PG_THREADS) fork_pages_kernel(const PagesArgs 
         src = __ldcg(a.table + (int64_t)u * a.stride + whole);
         dst = __ldcg(a.free_pages + n_free - 1 - nth);
     }
-    if (a.shared_out != a.shared)
-        for (int p = tid; p < a.n_pages; p += NT) a.shared_out[p] = __ldcg(a.shared + p);
+    pg_counts<NT>(a, tid);
     pg_sync<N>();          // all is read that may be written in place
     if (rank == 0 && i < a.batch) {
         a.granted[i] = ok ? T : 0;
@@ -283,12 +289,12 @@ __global__ void __launch_bounds__(PG_THREADS) compact_pages_kernel(const PagesAr
             const int k = p < live ? free_before(p) : p - live - (free_before(p) - moves);
             (p < live ? a.move_dst : a.move_src)[k] = p;
         } else if (a.shared_out != a.shared) {
-            a.shared_out[p] = __ldcg(a.shared + p);
+            a.shared_out[p] = max(__ldcg(a.shared + p), 0);
         }
     }
     pg_sync<N>();
     for (int k = tid; k < moves; k += NT) {
-        const int src = __ldcg(a.move_src + k), dst = __ldcg(a.move_dst + k), held = __ldcg(a.shared + src);
+        const int src = __ldcg(a.move_src + k), dst = __ldcg(a.move_dst + k), held = max(__ldcg(a.shared + src), 0);
         a.to[src] = dst;
         a.shared_out[dst] = held;
         a.shared_out[src] = 0;
