@@ -488,7 +488,9 @@ int eta_prefill(const eta_cache_desc* desc, const eta_page_table* pages, const e
  *   - a partly filled last page: a page of its own off the top of the stack, sequence after sequence; copy_src[i] and copy_dst[i] say which
  *     page is to be copied where (eta_copy_pages with max_moves = batch; for every layer's pools), -1 for sequences that copy none.
  * granted[i] = T, and the child's length (seq_lens_out[i]) with it; a child that could not be served (not an empty place, no such parent,
- * no page left) gets granted[i] = 0, shares nothing, keeps its length, and ETA_DEV_REFUSED is set.  batch <= 1024.
+ * no page left, a partly filled page of its parent or one off the stack whose number is outside the pool) gets granted[i] = 0, shares nothing, keeps its
+ * length, and ETA_DEV_REFUSED is set (a number outside the pool is off the stack then).  Numbers of full pages are handed on as they are; one outside
+ * the pool sets ETA_DEV_REFUSED and the child has it like its parent.  batch <= 1024.
  *
  * eta_fork_summaries: the block summaries of the children: the records of the granted[i] / block_size full blocks of every KV head, from the parent's
  * rows of musig and mnorm to the child's (flags: ETA_BUILD_PACKED_SIGMA or 0).  After eta_fork_pages, for every layer.  Of the descriptor the

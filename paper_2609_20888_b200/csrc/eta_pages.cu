@@ -207,25 +207,31 @@ __global__ void __launch_bounds__(PG_THREADS) fork_pages_kernel(const PagesArgs 
             }
         }
     }
-    const int whole = T >> a.b_shift, tail = (T & ((1 << a.b_shift) - 1)) != 0;
+    // Both pages of a copy have to be ones: the parent's last, before the child counts as one that wants a page, and the one off the stack.
+    auto is_page = [&](int page) { return page >= 0 && page < a.n_pages; };
+    const int whole = T >> a.b_shift;
+    int tail = (T & ((1 << a.b_shift) - 1)) != 0, src = -1, dst = -1;
+    if (tail) {
+        src = __ldcg(a.table + (int64_t)u * a.stride + whole);
+        if (!is_page(src)) { refused = true; u = -1; tail = 0; }
+    }
     int wanted;
     const int nth = pg_scan(tail, wanted, s_warp);
-    const bool ok = u >= 0 && (!tail || nth < n_free);
+    bool ok = u >= 0 && (!tail || nth < n_free);
+    if (ok && tail) {
+        dst = __ldcg(a.free_pages + n_free - 1 - nth);
+        ok = is_page(dst);
+    }
     refused = refused || (u >= 0 && !ok);
     s_parent[i] = u;
     s_whole[i] = ok ? whole : 0;
-    int src = -1, dst = -1;
     const bool copies = ok && tail;
-    if (copies && rank == 0) {
-        src = __ldcg(a.table + (int64_t)u * a.stride + whole);
-        dst = __ldcg(a.free_pages + n_free - 1 - nth);
-    }
     pg_counts<NT>(a, tid);
     pg_sync<N>();          // all is read that may be written in place
     if (rank == 0 && i < a.batch) {
         a.granted[i] = ok ? T : 0;
-        a.copy_src[i] = src;
-        a.copy_dst[i] = dst;
+        a.copy_src[i] = copies ? src : -1;
+        a.copy_dst[i] = copies ? dst : -1;
         if (copies) a.table_out[(int64_t)i * a.stride + whole] = dst;
         if (ok) a.seq_lens_out[i] = T;
         else if (a.seq_lens_out != a.seq_lens) a.seq_lens_out[i] = mine;
