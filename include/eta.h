@@ -498,7 +498,7 @@ int eta_prefill(const eta_cache_desc* desc, const eta_page_table* pages, const e
  *
  * eta_free_pages: every sequence with release[i] != 0 lets go of its pages, and its length becomes 0.  A page that nobody holds any more goes onto the
  * stack, lowest number first; of the others shared goes down.  ETA_DEV_REFUSED: a page number outside the pool (skipped), more
- * releases of a page than it has holders (it goes back once), or a stack that would overflow.
+ * releases of a page than it has holders (it goes back once, or not at all if it is on the stack already), or a stack that would overflow.
  *
  * eta_compact_pages: with L pages in use, the k-th page in use from L up goes to the k-th free page below L: move_src[k], move_dst[k] (room
  * for n_pages each), *n_moves of them; entries behind those are left as they are.  Tables of all sequences (block_table_out), counts and

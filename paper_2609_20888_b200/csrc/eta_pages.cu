@@ -124,8 +124,16 @@ __global__ void __launch_bounds__(PG_THREADS) free_pages_kernel(const PagesArgs 
     bool refused = false;
     pdl_wait();
     const int n_free = pg_clamped(__ldcg(a.n_free), a.n_pages);
+    const int top = tid < n_free ? __ldcg(a.free_pages + tid) : -1;
+    for (int w = tid; w < (a.n_pages + 31) / 32; w += NT) a.bits[w] = 0u;
     pg_counts<NT>(a, tid);
     pg_sync<N>();
+    // a bit per page on the stack: those that come back must not be among them
+    auto mark = [&](int page) {
+        if (page >= 0 && page < a.n_pages) atomicOr(a.bits + page / 32, 1u << (page & 31));
+    };
+    mark(top);
+    for (int k = tid + NT; k < n_free; k += NT) mark(__ldcg(a.free_pages + k));
     // Everyone that lets go counts down, without looking: a count that ends below zero has nobody left.  (Looking at what each
     // atomic returns, 800 sequences took 54 us.)
     const int chunks = (a.most + PG_CHUNK - 1) / PG_CHUNK;
@@ -154,13 +162,14 @@ __global__ void __launch_bounds__(PG_THREADS) free_pages_kernel(const PagesArgs 
     }
     pg_sync<N>();
     {
-        // a bit per page that is free now, of the words that this CTA goes on with
+        // a bit per page that comes back, of the words that this CTA goes on with
         const int words = (a.n_pages + 31) / 32, per = (words + N - 1) / N, w1 = min(words, (rank + 1) * per);
         for (int w = rank * per + (int)threadIdx.x / 32; w < w1; w += PG_WARPS) {
             const int p = 32 * w + lane, n = p < a.n_pages ? __ldcg(a.shared_out + p) : 0;
+            const uint32_t stack = __ldcg(a.bits + w);
             if (n < 0) a.shared_out[p] = 0;
-            refused = refused || n < -1;
-            const uint32_t v = __ballot_sync(0xffffffffu, n < 0);
+            refused = refused || n < -1 || (n < 0 && ((stack >> lane) & 1u));
+            const uint32_t v = __ballot_sync(0xffffffffu, n < 0) & ~stack;
             if (lane == 0) a.bits[w] = v;
         }
         __syncthreads();
