@@ -486,8 +486,18 @@ static int pages_workspace(PagesArgs& a, void* workspace, size_t bytes) {
     a.count = reinterpret_cast<int32_t*>(ws + s.count);
     return ETA_OK;
 }
+static bool pages_one_cta(int64_t entries, int clusters) {
+#ifdef ETA_TEST_GENERAL_PATH
+    clusters = 0;
+#endif
+    return entries <= PG_SMALL || clusters < 1;
+}
 static int pages_launch(const char* what, void (*one)(PagesArgs), void (*cluster)(PagesArgs), const PagesArgs& a, void* stream) {
-    const bool small = (int64_t)a.batch * a.most + a.n_pages <= PG_SMALL;
+    // a part of a GPU may hold no cluster of this size: one CTA does any size then, if slowly
+    const int64_t entries = (int64_t)a.batch * a.most + a.n_pages;
+    int fit[MAX_CLUSTER + 1] = {};
+    if (entries > PG_SMALL) clusters_that_fit(reinterpret_cast<const void*>(cluster), PG_THREADS, 0, fit);
+    const bool small = pages_one_cta(entries, fit[PG_CLUSTER]);
     const void* const kernel = reinterpret_cast<const void*>(small ? one : cluster);
     const int rc = configure_kernel(kernel, 0);
     if (rc != ETA_OK) return rc;
@@ -521,6 +531,10 @@ int eta_pages_workspace_bytes(int32_t n_pages, size_t* out_bytes) {
     *out_bytes = eta::pages_scratch(n_pages).total;
     return ETA_OK;
 }
+
+// Host-only check of how the calls on pages are launched: one CTA where there is little to do or where no cluster fits.  Not part of the public
+// interface; called by the CPU test-suite.  -> 1: one CTA, 0: a cluster.
+int eta_selftest_pages_one_cta(int64_t entries, int clusters) { return eta::pages_one_cta(entries, clusters); }
 
 int eta_free_pages(int32_t batch, int32_t block_size, int32_t t_cap, const int32_t* release, const int32_t* seq_lens, int32_t* seq_lens_out,
                    const int32_t* block_table, int32_t table_stride, const int32_t* shared, int32_t* shared_out, int32_t* free_pages,
