@@ -12,7 +12,9 @@ namespace eta {
 constexpr int PG_THREADS = 1024, PG_WARPS = PG_THREADS / 32, PG_CLUSTER = 8;
 constexpr int PG_MAX_BATCH = 1024;         // of a fork: a sequence per thread
 constexpr int PG_CHUNK = 128;              // pages of a sequence that a warp takes at a time
-// entries (pages and table) up to which one CTA does it
+// Entries (pages and table) up to which one CTA does it.  One CTA against a cluster, us in a row of calls, for forks, releases and compaction: at 2.7K
+// entries 3.9 / 4.6, 4.2 / 7.0, 6.3 / 9.8; at 5.5K 5.0 / 5.8, 5.3 / 8.1, 8.3 / 10.5; at 11K 7.3 / 6.5, 6.9 / 8.3, 11.8 / 10.3; at 22K 11.8 / 6.6,
+// 10.5 / 8.6, 20.7 / 11.5.
 constexpr int64_t PG_SMALL = 4096;
 
 template <int N>
