@@ -1108,7 +1108,7 @@ static int pf_launch(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUten
 
 template <int ITEM_COST>
 static int check_shares(int batch, int n_kv_heads, int g_shift, int head_dim, int ctas, const int32_t* n, const int32_t* len, int* whole) {
-    static PfTables tab;
+    static thread_local PfTables tab;
     const int m = PF_ROWS >> g_shift;
     tab.longest = 0;
     tab.items[0] = 0; tab.cost[0] = 0;
@@ -1177,12 +1177,18 @@ extern "C" {
 
 // Host-only check of how work is shared out: for made-up lengths every tile of every item is in exactly one share, the parts of a split
 // item have slots of their own, in order, and whoever has the first part knows their number.  Not part of the public interface; called by the
-// CPU test-suite.  Where the second kernel is not launched, no item is split.  n, len: [batch] new tokens and tokens cached.  -> 0, or the number of the first expectation that failed.
+// CPU test-suite.  Where the second kernel is not launched, no item is split.  n, len: [batch] new tokens and tokens cached.  -> 0, the number of the first expectation that failed, or -1: not a problem that
+// it can take.
 int eta_selftest_prefill_shares(int batch, int n_kv_heads, int g_shift, int head_dim, int ctas, const int32_t* n, const int32_t* len,
                                 int* whole) {
-    int gated_whole;
-    const int rc = eta::check_shares<eta::PF_ITEM_COST<true>>(batch, n_kv_heads, g_shift, head_dim, ctas, n, len, &gated_whole);
-    return rc ? rc : eta::check_shares<eta::PF_ITEM_COST<false>>(batch, n_kv_heads, g_shift, head_dim, ctas, n, len, whole);
+    if (batch <= 0 || batch > eta::PF_MAX_BATCH || ctas <= 0 || ctas > eta::PF_MAX_CTAS) return -1;
+    try {
+        int gated_whole;
+        const int rc = eta::check_shares<eta::PF_ITEM_COST<true>>(batch, n_kv_heads, g_shift, head_dim, ctas, n, len, &gated_whole);
+        return rc ? rc : eta::check_shares<eta::PF_ITEM_COST<false>>(batch, n_kv_heads, g_shift, head_dim, ctas, n, len, whole);
+    } catch (...) {                        // no memory for what it keeps per item
+        return -1;
+    }
 }
 
 int eta_prefill_workspace_bytes(const eta_cache_desc* desc, size_t* out_bytes) {

@@ -47,3 +47,11 @@ def test_far_fewer_tokens_than_rows(lib):
     for g_shift in range(4):
         rc, whole = shares(lib, 2, g_shift, 128, 148, [100000, 1, 7, 3000], [50000, 100000, 3, 40])
         assert rc == 0 and not whole
+
+
+def test_what_the_check_cannot_take(lib):
+    """More sequences or CTAs than the kernel has tables for: refused."""
+    whole = ctypes.c_int(0)
+    ints = ctypes.c_int32 * 1025
+    assert lib.eta_selftest_prefill_shares(1025, 1, 0, 64, 148, ints(), ints(), ctypes.byref(whole)) == -1
+    assert shares(lib, 1, 0, 64, 161, [1], [1])[0] == -1 and shares(lib, 1, 0, 64, 0, [1], [1])[0] == -1
