@@ -62,9 +62,10 @@ typedef enum eta_status {
 /* bits written to *status_dev by the kernels */
 #define ETA_DEV_TIMEOUT      1u  /* a bounded wait inside a kernel ran out; outputs are not valid */
 #define ETA_DEV_LEN_CLAMPED  2u  /* some seq_lens[i] exceeded t_cap and was clamped */
-#define ETA_DEV_EMPTY_ROW    4u  /* some seq_lens[i] <= 0: that sequence's output is zero */
+#define ETA_DEV_EMPTY_ROW    4u  /* some seq_lens[i] <= 0: that sequence's output is zero; of eta_prefill, a row before its sequence's first token: zeros */
 #define ETA_DEV_BAD_SLOT     8u  /* a slot of eta_append_tokens lies past the cache: that row was skipped */
-#define ETA_DEV_REFUSED     16u  /* eta_plan_pages could not serve some sequence (granted says which), or more pages came back than exist */
+#define ETA_DEV_REFUSED     16u  /* eta_plan_pages or eta_fork_pages could not serve some sequence (granted says which), more pages came back than
+                                        exist or are held, or a table or the free stack holds what it cannot (each call says what it looks at) */
 
 /* flags of eta_params.flags */
 #define ETA_FLAG_DENSE           1u  /* baseline: admit every block and switch the gate off (softmax attention) */
@@ -317,7 +318,8 @@ int eta_decode_paged(const eta_cache_desc* desc, const eta_page_table* pages, co
  * counterpart).  Device memory throughout, so that a serving loop can capture it with the step it prepares.  In order:
  *   1. Sequences with release[i] != 0 (release nullable) are over: their ceil(seq_lens[i] / block_size) pages go on top of the free
  *      stack (free_pages int32 [n_pages], of which the first *n_free are free), sequence after sequence, block after
- *      block, and their length becomes 0.  A place in the batch can take a new request in the same call.
+ *      block, and their length becomes 0.  A place in the batch can take a new request in the same call.  Sequences that share pages (see
+ *      eta_fork_pages) go with eta_free_pages instead: this call does not look at who else holds a page.
  *   2. Sequence i asks for new_lens[i] tokens (negative: none).  It gets all of them or none: all if its length stays within t_cap,
  *      its rows lie within n_rows, and it needs no page or the stack still holds what it and the sequences before it ask for.
  *      (Once one goes without for want of pages, so do all later ones that need any.)  Pages come off the top of the stack into
@@ -463,9 +465,11 @@ int eta_decode_kv4(const eta_cache_desc* desc, const eta_kv4_desc* kv4, const et
  * NaN where its weight underflows.
  * bf16 operands, fp32 scores and sums; weights enter the second product as bf16 (2^-8 of each, as much as rounding the output).
  * Deterministic for a given device.  batch <= 1024, n_kv_heads <= 1024, n_rows <= 2^30; nb_cap is not looked at.
- * Two kernels, launched with programmatic dependent launch: the first waits for everything before it in the stream before it reads or
- * writes, the second releases its successors as it ends.  workspace: eta_prefill_workspace_bytes() bytes, 256-byte aligned, no
- * initialisation needed; two calls that can overlap need one each.
+ * Two kernels, or the first alone where t_cap <= 512, launched with programmatic dependent launch: the first waits for everything before it in the
+ * stream before it reads or writes.  The second releases its successors as it ends; the first alone does so when everything before it is complete but
+ * its own outputs are not yet: whoever is launched that way behind it waits (as all of this library's calls do before they write, or read what a call before
+ * them may have written).  workspace: eta_prefill_workspace_bytes() bytes, 256-byte aligned, no initialisation needed; two calls that can overlap need
+ * one each.
  */
 int eta_prefill_workspace_bytes(const eta_cache_desc* desc, size_t* out_bytes);
 int eta_prefill(const eta_cache_desc* desc, const eta_page_table* pages, const eta_params* params, int32_t n_rows, const void* q,
