@@ -21,8 +21,8 @@
 // for each chunk, with the other half's beside them) -> O, and 500 more until the next S is there, in the clock of the softmax warps at head_dim 128;
 // there is tensor memory for two halves' chains, not three.  Tensor core and special function unit have 2048 cycles of work a tile each and are
 // busy 51 % of the time.  One 8K prompt of 32 / 8 heads of 128 takes 530 to 600 us, 32K 7.7 to 8.9 ms (1.0 to 1.1 PFLOP/s; by the power limit).  With parts
-// taken out 32K takes 6.3 to 6.8 ms without the products, as much without the softmax, 3.8 without both and without copies.  Gated scores take
-// one and a quarter more special functions each (60 to 68 % busy) and 960 instructions a thread and tile instead of 490: 11 packed prompts to 5K
+// taken out of a kernel two steps earlier 32K took 6.3 to 6.8 ms without the products, as much without the softmax, 3.8 without both and without copies.  Gated scores take
+// one and a quarter more special functions each (60 to 69 % busy) and 980 instructions a thread and tile instead of 490: 11 packed prompts to 5K
 // 1.00 ms (530 TFLOP/s; with a reciprocal for two gates instead of four 1.03), 2 x 1111 tokens behind 32K at head_dim 64 650 us (320 TFLOP/s).
 // 64 single tokens behind 16K stream at 6.0 TB/s.
 // Tried, for the 32K prompt: a thread per row and eight softmax warps 8.4 to 9.4 ms; a warp for each half's MMAs, free 10.3, taking turns 8.9 (the
